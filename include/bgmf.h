@@ -412,6 +412,133 @@ int bgmf_get_trace(bgmf_t *h, int64_t *begin, int64_t *end, int64_t *ticks_per_s
  * Needs ratings. */
 int bgmf_chain_stats(bgmf_t *h, int64_t out[4]);
 
+/* ------------------------------------------------------------------------
+ * Ranking: answers from learned factors, and gradients for training them on
+ * choices in place of ratings.  The calls below take matrices in device
+ * memory (scores x_rj of users r over the catalogue of items j, factor rows)
+ * and need no handle:
+ *   - All work is ordered on hip_stream (NULL: the default stream), whose
+ *     device must be the current one.  A call returns without waiting,
+ *     allocates nothing and keeps no pointer; its buffers and workspace must
+ *     outlive the work.  Two calls may overlap if they share no output and
+ *     no workspace.  Every call can be captured into a HIP graph.
+ *   - Matrices are row-major with a row stride in elements; a stride of an
+ *     input may be anything from 0 up, that of an output is at least the
+ *     row's length.  Pointers need the alignment of their element type only;
+ *     rows that start on 16-byte boundaries are read faster.
+ *   - A workspace (ws) starts on a 256-byte boundary and has at least the
+ *     bytes that the call's ..._workspace function returns for the same
+ *     sizes; what it holds before and after is of no meaning.
+ *   - Sizes of zero are valid and do what the formulas say of empty sums.
+ *   - Errors are reported by bgmf_last_error(NULL).  BGMF_E_ARG for what the
+ *     descriptions exclude, BGMF_E_BUDGET for a workspace that is too small.
+ *   - The same inputs give the same bits.
+ * ------------------------------------------------------------------------ */
+
+/* Types of matrix elements. */
+#define BGMF_TYPE_F32  0
+#define BGMF_TYPE_BF16 1
+#define BGMF_TYPE_F16  2
+#define BGMF_TYPE_I8   3
+
+/* Largest number of top alternatives, and longest row of a product (its sums
+ * are exact in 32-bit integers). */
+#define BGMF_TOP_MAX 128
+#define BGMF_PRODUCT_K_MAX 131071
+
+/* Per row r of scores (rows x cols, F32, BF16 or F16), with temperature t > 0
+ * and the items with excluded[r][j] != 0 left out (bytes, NULL: none are):
+ *   M = max_j x_j      d_j = (x_j - M) / t      S = sum_j exp(d_j)
+ *   log_prob[r] = d_g - ln S, g = given[r]: the item's log probability
+ *   entropy[r]  = ln S - sum_j exp(d_j) d_j / S
+ *   top_item[r][0..top), top_log_prob[r][0..top): the items with the largest
+ *     scores, ties to the lower item, and their log probabilities
+ *   row_max[r] = M, row_sum[r] = S: what bgmf_log_probs_grad needs
+ * (sums and statistics in fp32, formed in one pass over the scores).
+ *   given[r] = -1: log_prob[r] = 0; another item outside [0, cols): NaN; an
+ *     excluded item, or one with score -inf: -inf.
+ *   An item with score -inf has probability 0 and is never an alternative;
+ *     where fewer than `top` are left, top_item is -1 and top_log_prob -inf.
+ *   A row with nothing left (all items excluded or -inf, or cols = 0) has
+ *     log_prob -inf (0 for given -1, NaN outside), entropy 0, M = -inf, S = 0.
+ *   A NaN or +inf among the items that are not excluded makes log_prob (but
+ *     for given -1), entropy and the alternatives' log probabilities NaN; NaN
+ *     is never an alternative.  Values of excluded items do not matter.
+ * 0 <= top <= BGMF_TOP_MAX; rows, cols < 2^31.  given may be NULL if
+ * log_prob is; any output may be NULL, top_item and top_log_prob only if top
+ * is 0. */
+int64_t bgmf_log_probs_workspace(int64_t rows, int64_t cols, int32_t top);
+int bgmf_log_probs(const void *scores, int32_t type, int64_t rows, int64_t cols,
+                   int64_t row_stride, const uint8_t *excluded, int64_t excluded_stride,
+                   const int32_t *given, float temperature, int32_t top, float *log_prob,
+                   float *entropy, float *row_max, float *row_sum, int32_t *top_item,
+                   float *top_log_prob, void *ws, int64_t ws_bytes, void *hip_stream);
+
+/* Gradient of sum_r (grad_log_prob[r] log_prob[r] + grad_entropy[r]
+ * entropy[r]) with respect to the scores, from the same inputs and the
+ * forward call's row_max, row_sum and entropy, p_j = exp(d_j) / S:
+ *   grad_scores[r][j] = ( grad_log_prob[r] (1[j = given[r]] - p_j)
+ *                         - grad_entropy[r] p_j (ln p_j + entropy[r]) ) / t
+ * and 0 for excluded items and in rows with nothing left.  given[r] = -1
+ * takes no part in the first term, another item outside [0, cols) makes the
+ * row NaN.  Either gradient may be NULL (zero); entropy may be NULL if
+ * grad_entropy is.  grad_scores has the type of the scores, rounded once, and
+ * may be the scores themselves (same pointer and stride). */
+int bgmf_log_probs_grad(const void *scores, int32_t type, int64_t rows, int64_t cols,
+                        int64_t row_stride, const uint8_t *excluded, int64_t excluded_stride,
+                        const int32_t *given, float temperature, const float *row_max,
+                        const float *row_sum, const float *entropy, const float *grad_log_prob,
+                        const float *grad_entropy, void *grad_scores, int64_t grad_stride,
+                        void *hip_stream);
+
+/* Rows in 8-bit integers (x: rows x k, F32, BF16 or F16):
+ *   scale[r] = max_c |x_rc| / 127,   q_rc = x_rc / scale[r] rounded to the
+ *   nearest integer, ties to even, within [-127, 127]
+ * with both quotients rounded to fp32 first.  scale 0 (a row of zeros, or of
+ * values below 8e-44): q = 0.  A NaN or an infinity in a row: scale = NaN, q =
+ * 0.  k >= 1; q's row stride at least k. */
+int bgmf_quantize_rows(const void *x, int32_t type, int64_t rows, int64_t k, int64_t row_stride,
+                       int8_t *q, int64_t q_stride, float *scale, void *hip_stream);
+
+/* Scores of users over items, both in 8-bit integers:
+ *   out[r][j] = float(sum_c a_rc b_jc) * row_scale[r] * item_scale[j]
+ * with the sum exact in 32-bit integers, then rounded to fp32, multiplied in
+ * this order in fp32 and rounded once to out's type (F32, BF16 or F16).
+ *   x: rows x k, BGMF_TYPE_I8 (a = x, with row_scale), or F32, BF16 or F16:
+ *     then the rows are quantised as by bgmf_quantize_rows within the call
+ *     and row_scale must be NULL;
+ *   items: item_count x k signed bytes, item_scale item_count floats.
+ * 1 <= k <= BGMF_PRODUCT_K_MAX; rows, item_count < 2^31. */
+int64_t bgmf_quantized_scores_workspace(int64_t rows, int64_t item_count, int64_t k, int32_t type);
+int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
+                          int64_t row_stride, const float *row_scale, const int8_t *items,
+                          int64_t item_count, int64_t items_stride, const float *item_scale,
+                          void *out, int32_t out_type, int64_t out_stride, void *ws,
+                          int64_t ws_bytes, void *hip_stream);
+
+/* One gradient of bgmf_clip_grad_norm: a rows x cols matrix in (row stride
+ * in_stride) and the place out of its clipped values (out_stride), which may
+ * be in itself (with the same stride).  A vector is one row. */
+typedef struct {
+  const void *in;
+  void *out;
+  int64_t rows, cols;
+  int64_t in_stride, out_stride;
+  int32_t type; /* BGMF_TYPE_F32, BF16 or F16, of in and out */
+} bgmf_grad_t;
+
+/* Clipping by the global norm, over `count` gradients (grads: a host array,
+ * read during the call):
+ *   *norm = sqrt(sum over all elements of g^2)       (device, fp32)
+ *   out = g * (max_norm / *norm) if *norm > max_norm, else g
+ * with the squares summed in fp64 in a fixed order, and the factor in fp32.
+ * A norm that is NaN or infinite leaves the gradients as they are (out = g):
+ * the caller reads *norm.  max_norm >= 0, not NaN (infinity: never clips).
+ * No out may overlap another gradient. */
+int64_t bgmf_clip_grad_norm_workspace(int64_t count);
+int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm, float *norm,
+                        void *ws, int64_t ws_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -44,14 +44,30 @@ BGMF_OPT_ALLOC_COUNT = 14
 BGMF_OPT_LOAD_PEAK = 15
 BGMF_OPT_LOAD_GROUPS = 16
 
+BGMF_TYPE_F32 = 0
+BGMF_TYPE_BF16 = 1
+BGMF_TYPE_F16 = 2
+BGMF_TYPE_I8 = 3
+BGMF_TOP_MAX = 128
+BGMF_PRODUCT_K_MAX = 131071
+
 EXPORTED = (
     "bgmf_create", "bgmf_destroy", "bgmf_last_error", "bgmf_set_stream", "bgmf_set_factors",
     "bgmf_load_coo", "bgmf_epoch", "bgmf_rmse", "bgmf_get_factors", "bgmf_get_layout",
     "bgmf_sync", "bgmf_factor_ptrs", "bgmf_set_option", "bgmf_get_option", "bgmf_get_timing",
     "bgmf_chain_stats", "bgmf_rmse_coo", "bgmf_fit", "bgmf_set_cuts", "bgmf_get_cuts",
     "bgmf_balanced_cuts", "bgmf_get_trace", "bgmf_query_sizes", "bgmf_bind",
-    "bgmf_rmse_coo_dev", "bgmf_reorder_ids",
+    "bgmf_rmse_coo_dev", "bgmf_reorder_ids", "bgmf_log_probs_workspace", "bgmf_log_probs",
+    "bgmf_log_probs_grad", "bgmf_quantize_rows", "bgmf_quantized_scores_workspace",
+    "bgmf_quantized_scores", "bgmf_clip_grad_norm_workspace", "bgmf_clip_grad_norm",
 )
+
+
+class Grad(ctypes.Structure):
+    """bgmf_grad_t of include/bgmf.h."""
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("in_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("type", ctypes.c_int32)]
 
 
 class BgmfError(RuntimeError):
@@ -97,6 +113,17 @@ def _load() -> ctypes.CDLL:
                               ctypes.POINTER(ctypes.c_size_t), ctypes.POINTER(ctypes.c_size_t),
                               ctypes.POINTER(ctypes.c_size_t)], c_int),
         "bgmf_bind": ([vp, vp, vp, vp, ctypes.c_size_t, vp, ctypes.c_size_t, vp], c_int),
+        "bgmf_log_probs_workspace": ([I64, I64, I32], I64),
+        "bgmf_log_probs": ([vp, I32, I64, I64, I64, vp, I64, vp, F32, I32, vp, vp, vp, vp, vp, vp,
+                            vp, I64, vp], c_int),
+        "bgmf_log_probs_grad": ([vp, I32, I64, I64, I64, vp, I64, vp, F32, vp, vp, vp, vp, vp, vp,
+                                 I64, vp], c_int),
+        "bgmf_quantize_rows": ([vp, I32, I64, I64, I64, vp, I64, vp, vp], c_int),
+        "bgmf_quantized_scores_workspace": ([I64, I64, I64, I32], I64),
+        "bgmf_quantized_scores": ([vp, I32, I64, I64, I64, vp, vp, I64, I64, vp, vp, I32, I64, vp,
+                                   I64, vp], c_int),
+        "bgmf_clip_grad_norm_workspace": ([I64], I64),
+        "bgmf_clip_grad_norm": ([vp, I64, F32, vp, vp, I64, vp], c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -318,6 +345,56 @@ def bgmf_reorder_ids(n: int, m: int, p: int, rows, cols):
         msg = _lib.bgmf_last_error(None)
         raise BgmfError(rc, msg.decode() if msg else "bgmf_reorder_ids failed")
     return rn, cn
+
+
+# The ranking calls take device addresses as integers (``tensor.data_ptr()``),
+# 0 for a null pointer, strides in elements, ``stream`` an integer hipStream_t
+# (0: the default stream); paper_2304_13724_amd.ranking calls them on tensors.
+
+def bgmf_log_probs_workspace(rows: int, cols: int, top: int) -> int:
+    return _lib.bgmf_log_probs_workspace(rows, cols, top)
+
+
+def bgmf_log_probs(scores, type_, rows, cols, row_stride, excluded, excluded_stride, given,
+                   temperature, top, log_prob, entropy, row_max, row_sum, top_item, top_log_prob,
+                   ws, ws_bytes, stream) -> None:
+    _check(None, _lib.bgmf_log_probs(
+        scores, type_, rows, cols, row_stride, excluded, excluded_stride, given, temperature, top,
+        log_prob, entropy, row_max, row_sum, top_item, top_log_prob, ws, ws_bytes, stream))
+
+
+def bgmf_log_probs_grad(scores, type_, rows, cols, row_stride, excluded, excluded_stride, given,
+                        temperature, row_max, row_sum, entropy, grad_log_prob, grad_entropy,
+                        grad_scores, grad_stride, stream) -> None:
+    _check(None, _lib.bgmf_log_probs_grad(
+        scores, type_, rows, cols, row_stride, excluded, excluded_stride, given, temperature,
+        row_max, row_sum, entropy, grad_log_prob, grad_entropy, grad_scores, grad_stride, stream))
+
+
+def bgmf_quantize_rows(x, type_, rows, k, row_stride, q, q_stride, scale, stream) -> None:
+    _check(None, _lib.bgmf_quantize_rows(x, type_, rows, k, row_stride, q, q_stride, scale,
+                                         stream))
+
+
+def bgmf_quantized_scores_workspace(rows: int, item_count: int, k: int, type_: int) -> int:
+    return _lib.bgmf_quantized_scores_workspace(rows, item_count, k, type_)
+
+
+def bgmf_quantized_scores(x, type_, rows, k, row_stride, row_scale, items, item_count,
+                          items_stride, item_scale, out, out_type, out_stride, ws, ws_bytes,
+                          stream) -> None:
+    _check(None, _lib.bgmf_quantized_scores(
+        x, type_, rows, k, row_stride, row_scale, items, item_count, items_stride, item_scale,
+        out, out_type, out_stride, ws, ws_bytes, stream))
+
+
+def bgmf_clip_grad_norm_workspace(count: int) -> int:
+    return _lib.bgmf_clip_grad_norm_workspace(count)
+
+
+def bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream) -> None:
+    """``grads``: a ctypes array of ``Grad``."""
+    _check(None, _lib.bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream))
 
 
 # --- convenience wrapper -----------------------------------------------------

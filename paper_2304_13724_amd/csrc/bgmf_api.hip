@@ -17,6 +17,7 @@
 
 #include "../../include/bgmf.h"
 #include "bgmf_handle.h"
+#include "bgmf_rank.h"
 
 using namespace bgmfk;
 
@@ -128,6 +129,23 @@ int fail(bgmf_t *h, int code, const char *fmt, ...) {
   else g_create_error = buf;
   return code;
 }
+
+}  // namespace
+
+int bgmfk::fail_call(int code, const char *fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  try {
+    g_create_error = buf;
+  } catch (...) {  // no memory for the message: the code alone is returned
+  }
+  return code;
+}
+
+namespace {
 
 #define HIP_TRY(h, call)                                                                   \
   do {                                                                                     \

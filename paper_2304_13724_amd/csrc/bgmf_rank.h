@@ -1,0 +1,69 @@
+// Shared by the HIP sources of the ranking operators (not part of the ABI):
+// element types, vector loads and stores, and the checks of their arguments.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/bgmf.h"
+
+namespace bgmfk {
+
+// Sets the calling thread's message (bgmf_last_error(NULL)) and returns code.
+int fail_call(int code, const char *fmt, ...) __attribute__((format(printf, 2, 3)));
+
+inline int64_t type_bytes(int32_t type) {
+  return type == BGMF_TYPE_F32 ? 4 : type == BGMF_TYPE_I8 ? 1 : 2;
+}
+inline bool is_float_type(int32_t type) {
+  return type == BGMF_TYPE_F32 || type == BGMF_TYPE_BF16 || type == BGMF_TYPE_F16;
+}
+
+// A matrix argument: a non-null pointer aligned to its elements (unless the
+// matrix is empty) and a row stride of at least min_stride whose last element
+// has an offset below 2^62 bytes.
+inline bool bad_matrix(const void *p, int64_t rows, int64_t cols, int64_t stride,
+                       int64_t min_stride, int64_t esize) {
+  if (rows <= 0 || cols <= 0) return false;
+  if (!p || reinterpret_cast<uintptr_t>(p) % (uintptr_t)esize) return true;
+  return rows > 1 && (stride < min_stride || stride > ((int64_t)1 << 60) / rows);
+}
+
+using f16_t = _Float16;
+using bf16_t = __bf16;
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(f16_t x) { return (float)x; }
+__device__ __forceinline__ float to_float(bf16_t x) {
+  return __uint_as_float((uint32_t)__builtin_bit_cast(uint16_t, x) << 16);
+}
+// rounded to nearest, ties to even
+template <class T>
+__device__ __forceinline__ T from_float(float x) { return (T)x; }
+// The empty statement keeps a product that is converted in two roundings (to
+// fp32, then to f16): the compiler would merge both into one mixed-precision
+// instruction, and the result would not be the one of fp32 arithmetic.
+template <>
+__device__ __forceinline__ f16_t from_float<f16_t>(float x) {
+  asm("" : "+v"(x));
+  return (f16_t)x;
+}
+
+// 16 bytes of elements, at any alignment that suits one element.
+template <class T>
+struct alignas(16) Vec {
+  static constexpr int N = 16 / (int)sizeof(T);
+  T v[N];
+};
+template <class T>
+__device__ __forceinline__ Vec<T> load_vec(const T *p) {
+  Vec<T> x;
+  __builtin_memcpy(&x, p, sizeof x);
+  return x;
+}
+template <class T>
+__device__ __forceinline__ void store_vec(T *p, const Vec<T> &x) {
+  __builtin_memcpy(p, &x, sizeof x);
+}
+
+}  // namespace bgmfk
