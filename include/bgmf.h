@@ -496,7 +496,7 @@ int bgmf_log_probs_grad(const void *scores, int32_t type, int64_t rows, int64_t 
  *   nearest integer, ties to even, within [-127, 127]
  * with both quotients rounded to fp32 first.  scale 0 (a row of zeros, or of
  * values below 8e-44): q = 0.  A NaN or an infinity in a row: scale = NaN, q =
- * 0.  k >= 1; q's row stride at least k. */
+ * 0.  1 <= k < 2^30; q's row stride at least k. */
 int bgmf_quantize_rows(const void *x, int32_t type, int64_t rows, int64_t k, int64_t row_stride,
                        int8_t *q, int64_t q_stride, float *scale, void *hip_stream);
 
