@@ -9,8 +9,8 @@
 namespace bgmfk {
 namespace {
 
+// Threads of a workgroup: 256, or one wave for short rows (TH below).
 constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / 64;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr double kLn2 = 0.69314718055994530942;
 
@@ -66,10 +66,7 @@ struct Soft {
     s *= f;
   }
   template <int COUNT>
-  __device__ __forceinline__ void add(const float (&x)[COUNT], float c) {
-    float gm = x[0];
-#pragma unroll
-    for (int i = 1; i < COUNT; ++i) gm = fmaxf(gm, x[i]);
+  __device__ __forceinline__ void add(const float (&x)[COUNT], float gm, float c) {  // gm: max x
     if (gm > m) {
       rescale(gm, c);
       m = gm;
@@ -88,52 +85,64 @@ struct Soft {
 };
 
 // Sums over the workgroup in a fixed order; every thread has the result.
+template <int TH>
 struct SoftLds {
-  float m[kWaves];
-  double s[kWaves], w[kWaves];
+  float m[TH / 64];
+  double s[TH / 64], w[TH / 64];
 };
-__device__ __forceinline__ Soft block_soft(Soft a, float c, SoftLds &lds) {
+template <int TH>
+__device__ __forceinline__ Soft block_soft(Soft a, float c, SoftLds<TH> &lds) {
+  constexpr int W = TH / 64;
   const int wave = threadIdx.x / 64;
-  const float wm = wave_max(a.m);
-  if (threadIdx.x % 64 == 0) lds.m[wave] = wm;
-  __syncthreads();
-  float M = lds.m[0];
-#pragma unroll
-  for (int i = 1; i < kWaves; ++i) M = fmaxf(M, lds.m[i]);
-  a.rescale(M, c);
-  const double s = wave_sum(a.s), w = wave_sum(a.w);
-  if (threadIdx.x % 64 == 0) lds.s[wave] = s, lds.w[wave] = w;
-  __syncthreads();
   Soft r;
-  r.m = M;
+  r.m = wave_max(a.m);
+  if constexpr (W > 1) {
+    if (threadIdx.x % 64 == 0) lds.m[wave] = r.m;
+    __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) r.s += lds.s[i], r.w += lds.w[i];
+    for (int i = 0; i < W; ++i) r.m = fmaxf(r.m, lds.m[i]);
+  }
+  a.rescale(r.m, c);
+  a.s = wave_sum(a.s), a.w = wave_sum(a.w);
+  if constexpr (W == 1) {
+    r.s = a.s, r.w = a.w;
+  } else {
+    if (threadIdx.x % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < W; ++i) r.s += lds.s[i], r.w += lds.w[i];
+  }
   return r;
 }
 
 // ---------------------------------------------------------------------------
 // The n best of the scores that a workgroup has just gone through, larger
-// first, ties to the lower item.  A thread kept the largest of its scores, tm.
-// The n-th largest of the 256 tm is a score that the n best are not below, and
-// only the threads with tm at or above it ("hot", about n) can hold any of
-// them: their scores, n / 256 of the row, are read once more (from the cache),
-// and those at or above the bound, few more than n, are put in order by
-// counting how many precede each.  If more than kCandidates qualify (equal
-// scores, or the best ones all with few threads), the scores are gone through
-// in order of items instead, merging each tile's candidates into a list.
+// first, ties to the lower item.  A thread has kCols columns of the scores and
+// kept the largest score of each.  The n-th largest of 256 maxima (of threads,
+// or of columns where a workgroup is one wave) is a score that the n best are
+// not below, and only columns with their maximum at or above it ("hot", a few
+// more than n) can hold any of them: their scores, about n / 1024 of the row,
+// are read once more (from the cache), and those at or above the bound, few
+// more than n, are put in order by counting how many precede each.  If more
+// than CAND qualify (equal scores, or the best ones all in few columns), the
+// scores are gone through in order of items instead, merging each tile's
+// candidates into a list.
 //
-// SRC: per_thread() items of a thread; visit(thread, i, f): f(score, item) for
-// each score of its i-th; size() and at(p, item): all scores in the order of
-// items.  emit(rank, score, item), for every rank below n (item -1: none).
+// SRC: Piece, PIECES: what one load brings, and how many are in flight;
+// per_column() pieces of a column; load(column, i), column % TH is the thread;
+// each(piece, column, i, f): f(score, item) for each score of the piece; size()
+// and at(p, item): all scores in the order of items.
+// emit(rank, score, item), for every rank below n (item -1: none).
 // ---------------------------------------------------------------------------
-constexpr int kCandidates = 1024;
+constexpr int kCols = 4;
+constexpr int64_t kMostParts = kCols * kThreads;  // of a row, see split_of
+template <int TH>
 struct TopLds {
-  float tm[kThreads];
-  uint8_t hot[kThreads];
-  float v[kCandidates];
-  int32_t j[kCandidates];
-  float lv[2][BGMF_TOP_MAX];
-  int32_t lj[2][BGMF_TOP_MAX];
+  static constexpr int CAND = TH == 64 ? 256 : 1024;
+  float tm[TH == 64 ? 1 : TH];
+  uint64_t k[CAND];
+  uint64_t list[2][BGMF_TOP_MAX];
+  uint16_t hot[kCols * TH];
   float bound;
   int hots, count;
 };
@@ -146,16 +155,24 @@ __device__ __forceinline__ int32_t key_of(float x) {
 __device__ __forceinline__ float of_key(int32_t k) {
   return __int_as_float(k < 0 ? k ^ 0x7FFFFFFF : k);
 }
+// A score and its item as one number, larger for what comes first.
+__device__ __forceinline__ uint64_t rank_key(float v, int32_t j) {
+  return (uint64_t)((uint32_t)key_of(v) ^ 0x80000000u) << 32 | (uint32_t)~j;
+}
+__device__ __forceinline__ float key_score(uint64_t k) {
+  return of_key((int32_t)((uint32_t)(k >> 32) ^ 0x80000000u));
+}
+__device__ __forceinline__ int32_t key_item(uint64_t k) { return (int32_t)~(uint32_t)k; }
 
-// By one wave: a score that at least n of the 256 tm are not below, and few
-// more than n; -inf if fewer than n are above -inf.
-__device__ __forceinline__ float top_bound(const float *tm, int n) {
+// By one wave: a score that at least n of 256 maxima (four in each lane) are
+// not below, and few more than n; -inf if fewer than n are above -inf.
+__device__ __forceinline__ float top_bound(const float (&tm)[4], int n) {
   const int32_t none = key_of(-INFINITY);
-  int32_t k[kWaves], lo = 0x7FFFFFFF, hi = none;
+  int32_t k[4], lo = 0x7FFFFFFF, hi = none;
   int some = 0;
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) {
-    k[i] = key_of(tm[threadIdx.x % 64 + 64 * i]);
+  for (int i = 0; i < 4; ++i) {
+    k[i] = key_of(tm[i]);
     if (k[i] > none) lo = min(lo, k[i]);
     hi = max(hi, k[i]);
     some += __popcll(__ballot(k[i] > none));
@@ -172,7 +189,7 @@ __device__ __forceinline__ float top_bound(const float *tm, int n) {
     const int32_t mid = (int32_t)((uint32_t)lo + ((uint32_t)hi - (uint32_t)lo + 1) / 2);
     int c = 0;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) c += __popcll(__ballot(k[i] >= mid));
+    for (int i = 0; i < 4; ++i) c += __popcll(__ballot(k[i] >= mid));
     if (c >= n) {
       lo = mid;
       if (c <= n + 2 + n / 8) break;
@@ -183,115 +200,175 @@ __device__ __forceinline__ float top_bound(const float *tm, int n) {
   return of_key(lo);
 }
 
-__device__ __forceinline__ bool precedes(float v, int32_t j, float w, int32_t l) {
-  return v > w || (v == w && j < l);
+// How many of k[0..c) are larger, c at most CAND, zeros from c on; by G lanes
+// for one number (all of them get the count).
+template <int G>
+__device__ __forceinline__ int count_larger(const uint64_t *k, int c, uint64_t mine) {
+  int r = 0;
+  for (int o = (int)(threadIdx.x % G) * 8; o < c; o += G * 8) {
+    uint64_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = k[o + i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r += x[i] > mine;
+  }
+#pragma unroll
+  for (int o = 1; o < G; o *= 2) r += __shfl_xor(r, o);
+  return r;
 }
 
-template <class SRC, class EMIT>
-__device__ void top_in_order(const SRC &src, int n, TopLds &lds, float bound, const EMIT &emit) {
+template <int TH, class SRC, class EMIT>
+__device__ void top_in_order(const SRC &src, int n, TopLds<TH> &lds, float bound,
+                             const EMIT &emit) {
+  constexpr int CAND = TopLds<TH>::CAND;
   const int tid = threadIdx.x;
   int have = 0, now = 0;
-  constexpr int kPer = kCandidates / kThreads;
-  for (int64_t p0 = 0; p0 < src.size(); p0 += kCandidates) {
+  for (int64_t p0 = 0; p0 < src.size(); p0 += CAND) {
     if (tid == 0) lds.count = 0;
     __syncthreads();
-    const float worst = have == n ? lds.lv[now][n - 1] : -INFINITY;
+    const uint64_t worst = have == n ? lds.list[now][n - 1] : 0;
 #pragma unroll
-    for (int q = 0; q < kPer; ++q) {
-      const int64_t p = p0 + q * kThreads + tid;
+    for (int q = 0; q < CAND / TH; ++q) {
+      const int64_t p = p0 + q * TH + tid;
       if (p < src.size()) {
         int32_t j;
         const float v = src.at(p, j);
-        if (v > worst && v >= bound) {  // a later item loses a tie
-          const int at = atomicAdd(&lds.count, 1);
-          lds.v[at] = v, lds.j[at] = j;
+        if (v > -INFINITY && v >= bound) {
+          const uint64_t k = rank_key(v, j);
+          if (k > worst) lds.k[atomicAdd(&lds.count, 1)] = k;
         }
       }
     }
     __syncthreads();
     const int c = lds.count;
     if (c) {
-      for (int i = tid; i < c + have; i += kThreads) {
-        const bool old = i >= c;
-        const float v = old ? lds.lv[now][i - c] : lds.v[i];
-        const int32_t j = old ? lds.lj[now][i - c] : lds.j[i];
+      for (int i = tid; i < c + have; i += TH) {
+        const uint64_t k = i >= c ? lds.list[now][i - c] : lds.k[i];
         int rank = 0;
-        for (int o = 0; o < c; ++o) rank += precedes(lds.v[o], lds.j[o], v, j);
-        for (int o = 0; o < have; ++o) rank += precedes(lds.lv[now][o], lds.lj[now][o], v, j);
-        if (rank < n) lds.lv[now ^ 1][rank] = v, lds.lj[now ^ 1][rank] = j;
+        for (int o = 0; o < c; ++o) rank += lds.k[o] > k;
+        for (int o = 0; o < have; ++o) rank += lds.list[now][o] > k;
+        if (rank < n) lds.list[now ^ 1][rank] = k;
       }
       have = min(n, have + c);
       now ^= 1;
       __syncthreads();
     }
   }
-  for (int i = tid; i < n; i += kThreads)
-    emit(i, i < have ? lds.lv[now][i] : -INFINITY, i < have ? lds.lj[now][i] : -1);
+  for (int i = tid; i < n; i += TH) {
+    const uint64_t k = lds.list[now][i];
+    if (i < have) emit(i, key_score(k), key_item(k));
+    else emit(i, -INFINITY, -1);
+  }
 }
 
 // Called by the whole workgroup; lds is free for other use after the next
-// barrier.
-template <class SRC, class EMIT>
-__device__ __forceinline__ void top_select(const SRC &src, float tm, int n, TopLds &lds,
-                                           const EMIT &emit) {
+// barrier.  tm: the maxima of the thread's columns.
+template <int TH, class SRC, class EMIT>
+__device__ __forceinline__ void top_select(const SRC &src, const float (&tm)[kCols], int n,
+                                           TopLds<TH> &lds, const EMIT &emit) {
+  constexpr int CAND = TopLds<TH>::CAND;
   const int tid = threadIdx.x;
-  lds.tm[tid] = tm;
+  float most = tm[0];
+#pragma unroll
+  for (int q = 1; q < kCols; ++q) most = fmaxf(most, tm[q]);
+#pragma unroll
+  for (int q = 0; q < CAND / TH; ++q) lds.k[tid + q * TH] = 0;
   if (tid == 0) lds.hots = lds.count = 0;
-  __syncthreads();
-  if (tid < 64) {
-    const float b = top_bound(lds.tm, n);
-    if (tid == 0) lds.bound = b;
+  float bound;
+  if constexpr (TH == 64) {
+    bound = top_bound(tm, n);
+    __syncthreads();
+  } else {
+    lds.tm[tid] = most;
+    __syncthreads();
+    if (tid < 64) {
+      float four[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) four[i] = lds.tm[tid + 64 * i];
+      bound = top_bound(four, n);
+      if (tid == 0) lds.bound = bound;
+    }
+    __syncthreads();
+    bound = lds.bound;
+  }
+  if (most > -INFINITY && most >= bound) {
+#pragma unroll
+    for (int q = 0; q < kCols; ++q)
+      if (tm[q] > -INFINITY && tm[q] >= bound)
+        lds.hot[atomicAdd(&lds.hots, 1)] = (uint16_t)(tid + q * TH);
   }
   __syncthreads();
-  const float bound = lds.bound;
-  if (tm > -INFINITY && tm >= bound) lds.hot[atomicAdd(&lds.hots, 1)] = (uint8_t)tid;
-  __syncthreads();
-  const uint32_t per = (uint32_t)src.per_thread(), items = (uint32_t)lds.hots * per;
-  for (uint32_t i = tid; i < items; i += kThreads)
-    src.visit(lds.hot[i / per], (int32_t)(i % per), [&](float v, int32_t j) {
-      if (v > -INFINITY && v >= bound) {
-        const int at = atomicAdd(&lds.count, 1);
-        if (at < kCandidates) lds.v[at] = v, lds.j[at] = j;
-      }
-    });
+  const uint32_t per = (uint32_t)src.per_column(), items = (uint32_t)lds.hots * per;
+  constexpr int K = SRC::PIECES;
+  for (uint32_t i0 = tid; i0 < items; i0 += TH * K) {
+    typename SRC::Piece piece[K];
+    int col[K], at[K];
+#pragma unroll
+    for (int q = 0; q < K; ++q) {
+      const uint32_t i = i0 + q * TH, h = i / per;
+      col[q] = i < items ? lds.hot[h] : -1;
+      at[q] = (int)(i - h * per);
+      if (col[q] >= 0) piece[q] = src.load(col[q], at[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < K; ++q)
+      if (col[q] >= 0)
+        src.each(piece[q], col[q], at[q], [&](float v, auto item) {
+          if (v > -INFINITY && v >= bound) {
+            const int to = atomicAdd(&lds.count, 1);
+            if (to < CAND) lds.k[to] = rank_key(v, item());
+          }
+        });
+  }
   __syncthreads();
   const int c = lds.count;
-  if (c > kCandidates) {
+  if (c > CAND) {
     __syncthreads();
-    top_in_order(src, n, lds, bound, emit);
+    top_in_order<TH>(src, n, lds, bound, emit);
     return;
   }
-  for (int i = tid; i < c; i += kThreads) {
-    const float v = lds.v[i];
-    const int32_t j = lds.j[i];
-    int rank = 0;
-    for (int o = 0; o < c; ++o) rank += precedes(lds.v[o], lds.j[o], v, j);
-    if (rank < n) emit(rank, v, j);
-  }
-  for (int i = c + tid; i < n; i += kThreads) emit(i, -INFINITY, -1);
+  const auto order = [&](auto lanes) {
+    constexpr int G = decltype(lanes)::value;
+    for (int i = tid / G; i < c; i += TH / G) {
+      const uint64_t k = lds.k[i];
+      const int rank = count_larger<G>(lds.k, c, k);
+      if (rank < n && tid % G == 0) emit(rank, key_score(k), key_item(k));
+    }
+  };
+  if (c <= TH / 4) order(std::integral_constant<int, 4>{});
+  else order(std::integral_constant<int, 1>{});
+  for (int i = c + tid; i < n; i += TH) emit(i, -INFINITY, -1);
 }
 
-template <class T, bool EX>
-struct RowSource {  // thread t has vectors t, t + 256, ... and element t of the tail
+template <class T, bool EX, int TH>
+struct RowSource {  // column q has vectors q, q + 4 TH, ..., and column q < TH tail element q
+  static constexpr int N = Row<T, EX>::N;
+  struct Piece {
+    float x[N];
+  };
+  static constexpr int PIECES = 1;
   Row<T, EX> row;
   int32_t first;  // item of the row's first element
-  __device__ __forceinline__ int32_t per_thread() const {
-    return (row.vecs() + kThreads - 1) / kThreads + 1;
+  __device__ __forceinline__ int32_t per_column() const {
+    return (row.vecs() + kCols * TH - 1) / (kCols * TH) + 1;
+  }
+  __device__ __forceinline__ Piece load(int col, int32_t i) const {
+    Piece p;
+#pragma unroll
+    for (int e = 0; e < N; ++e) p.x[e] = -INFINITY;
+    const int32_t vecs = row.vecs(), v = col + (i - 1) * (kCols * TH);
+    if (i == 0) {
+      if (col < row.len - vecs * N) p.x[0] = row.one(vecs * N + col);
+    } else if (v < vecs) {
+      row.load(v, p.x);
+    }
+    return p;
   }
   template <class F>
-  __device__ __forceinline__ void visit(int t, int32_t i, const F &f) const {
-    constexpr int N = Row<T, EX>::N;
-    const int32_t vecs = row.vecs();
-    if (i == 0) {
-      if (t < row.len - vecs * N) f(row.one(vecs * N + t), first + vecs * N + t);
-      return;
-    }
-    const int32_t v = t + (i - 1) * kThreads;
-    if (v >= vecs) return;
-    float x[N];
-    row.load(v, x);
+  __device__ __forceinline__ void each(const Piece &p, int col, int32_t i, const F &f) const {
+    const int32_t at = i == 0 ? row.vecs() * N + col : (col + (i - 1) * (kCols * TH)) * N;
 #pragma unroll
-    for (int e = 0; e < N; ++e) f(x[e], first + v * N + e);
+    for (int e = 0; e < N; ++e) f(p.x[e], [&] { return first + at + e; });
   }
   __device__ __forceinline__ int64_t size() const { return row.len; }
   __device__ __forceinline__ float at(int64_t p, int32_t &j) const {
@@ -347,11 +424,11 @@ __device__ __forceinline__ void write_row(const LogProbs &P, int64_t r, const So
 // One workgroup per row, or per part of a row.  Bound: HBM; the scores are
 // read once.  A thread takes kGroup vectors at a time (64 bytes in flight),
 // their maximum first, so that the running sums are rescaled once per group.
-constexpr int kGroup = 4;
-template <class T, bool EX, bool TOP>
-__global__ void __launch_bounds__(kThreads) k_log_probs(LogProbs P) {
-  __shared__ SoftLds soft_lds;
-  __shared__ typename std::conditional<TOP, TopLds, int>::type top_lds;
+constexpr int kGroup = kCols;
+template <class T, bool EX, bool TOP, int TH>
+__global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
+  __shared__ SoftLds<TH> soft_lds;
+  __shared__ typename std::conditional<TOP, TopLds<TH>, int>::type top_lds;
   constexpr int N = Vec<T>::N;
   const int tid = threadIdx.x;
   const float c = kLog2e / P.temperature;
@@ -364,24 +441,36 @@ __global__ void __launch_bounds__(kThreads) k_log_probs(LogProbs P) {
                          EX ? P.ex + (r * P.ex_stride + first) : nullptr,
                          (int32_t)(left < P.part_len ? left : P.part_len)};
     Soft a;
+    float tm[kCols];  // the largest score of the g-th vectors of all groups
+#pragma unroll
+    for (int g = 0; g < kCols; ++g) tm[g] = -INFINITY;
     const int32_t vecs = row.vecs();
-    for (int32_t v = tid; v < vecs; v += kThreads * kGroup) {
+    for (int32_t v = tid; v < vecs; v += TH * kGroup) {
       float x[kGroup][N];
 #pragma unroll
       for (int g = 0; g < kGroup; ++g) {
-        if (v + g * kThreads < vecs) row.load(v + g * kThreads, x[g]);
+        if (v + g * TH < vecs) row.load(v + g * TH, x[g]);
         else
 #pragma unroll
           for (int i = 0; i < N; ++i) x[g][i] = -INFINITY;
       }
-      a.add(reinterpret_cast<float(&)[kGroup * N]>(x), c);
+      float gm = -INFINITY;
+#pragma unroll
+      for (int g = 0; g < kGroup; ++g) {
+        float vm = x[g][0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) vm = fmaxf(vm, x[g][i]);
+        if constexpr (TOP) tm[g] = fmaxf(tm[g], vm);
+        gm = fmaxf(gm, vm);
+      }
+      a.add(reinterpret_cast<float(&)[kGroup * N]>(x), gm, c);
     }
     if (tid < row.len - vecs * N) {
       const float x[1] = {row.one(vecs * N + tid)};
-      a.add(x, c);
+      tm[0] = fmaxf(tm[0], x[0]);
+      a.add(x, x[0], c);
     }
-    const float tm = a.m;
-    const Soft all = block_soft(a, c, soft_lds);
+    const Soft all = block_soft<TH>(a, c, soft_lds);
     const float log_s = logf((float)all.s);
     if (tid == 0) {
       if (P.parts == 1) write_row<T>(P, r, all, log_s);
@@ -389,14 +478,14 @@ __global__ void __launch_bounds__(kThreads) k_log_probs(LogProbs P) {
     }
     if constexpr (TOP) {
       const int n = P.top;
-      const RowSource<T, EX> src{row, (int32_t)first};
+      const RowSource<T, EX, TH> src{row, (int32_t)first};
       if (P.parts == 1)
-        top_select(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
+        top_select<TH>(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
           P.top_item[r * n + rank] = j;
           P.top_log_prob[r * n + rank] = j < 0 ? v : (v - all.m) / P.temperature - log_s;
         });
       else
-        top_select(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
+        top_select<TH>(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
           P.part_v[u * n + rank] = v;
           P.part_j[u * n + rank] = j;
         });
@@ -405,18 +494,20 @@ __global__ void __launch_bounds__(kThreads) k_log_probs(LogProbs P) {
   }
 }
 
-struct PartSource {  // thread t has the lists of parts t, t + 256, ...
+struct PartSource {  // column q has the list of part q
+  struct Piece {
+    float v;
+  };
+  static constexpr int PIECES = 4;
   const float *v;
   const int32_t *j;
   int64_t parts;
   int n;
-  __device__ __forceinline__ int32_t per_thread() const {
-    return (int32_t)((parts + kThreads - 1) / kThreads) * n;
-  }
+  __device__ __forceinline__ int32_t per_column() const { return n; }
+  __device__ __forceinline__ Piece load(int col, int32_t i) const { return {v[col * n + i]}; }
   template <class F>
-  __device__ __forceinline__ void visit(int t, int32_t i, const F &f) const {
-    const int64_t part = t + (int64_t)(i / n) * kThreads;
-    if (part < parts) f(v[part * n + i % n], j[part * n + i % n]);
+  __device__ __forceinline__ void each(const Piece &p, int col, int32_t i, const F &f) const {
+    f(p.v, [&] { return j[col * n + i]; });
   }
   __device__ __forceinline__ int64_t size() const { return parts * n; }
   __device__ __forceinline__ float at(int64_t p, int32_t &item) const {
@@ -428,28 +519,32 @@ struct PartSource {  // thread t has the lists of parts t, t + 256, ...
 // Joins the parts of a row: one workgroup per row.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_log_probs_join(LogProbs P) {
-  __shared__ SoftLds soft_lds;
-  __shared__ TopLds top_lds;
+  __shared__ SoftLds<kThreads> soft_lds;
+  __shared__ TopLds<kThreads> top_lds;
   const int tid = threadIdx.x, n = P.top;
   const float c = kLog2e / P.temperature;
   for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x) {
     const PartSum *sums = P.part_sum + r * P.parts;
     Soft a;
-    for (int64_t i = tid; i < P.parts; i += kThreads) {
+    float tm[kCols];
+    static_assert(kMostParts == kCols * kThreads, "a part is a column");
+#pragma unroll
+    for (int q = 0; q < kCols; ++q) {
+      const int64_t i = tid + q * kThreads;
       Soft b;
-      b.m = sums[i].m, b.s = sums[i].s, b.w = sums[i].w;
+      if (i < P.parts) b.m = sums[i].m, b.s = sums[i].s, b.w = sums[i].w;
+      tm[q] = b.m;
       const float M = fmaxf(a.m, b.m);
       a.rescale(M, c);
       b.rescale(M, c);
       a.m = M, a.s += b.s, a.w += b.w;
     }
-    const float tm = a.m;
-    const Soft all = block_soft(a, c, soft_lds);
+    const Soft all = block_soft<kThreads>(a, c, soft_lds);
     const float log_s = logf((float)all.s);
     if (tid == 0) write_row<T>(P, r, all, log_s);
     if (n) {
       const PartSource src{P.part_v + r * P.parts * n, P.part_j + r * P.parts * n, P.parts, n};
-      top_select(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
+      top_select<kThreads>(src, tm, n, top_lds, [&](int rank, float v, int32_t j) {
         P.top_item[r * n + rank] = j;
         P.top_log_prob[r * n + rank] = j < 0 ? v : (v - all.m) / P.temperature - log_s;
       });
@@ -474,10 +569,10 @@ struct LogProbsGrad {
 };
 constexpr int kGradGroup = 4;
 
-template <class T, bool EX, bool ENT>
-__global__ void __launch_bounds__(kThreads) k_log_probs_grad(LogProbsGrad P) {
+template <class T, bool EX, bool ENT, int TH>
+__global__ void __launch_bounds__(TH) k_log_probs_grad(LogProbsGrad P) {
   constexpr int N = Vec<T>::N;
-  constexpr int64_t kGradTile = (int64_t)kThreads * kGradGroup * N;
+  constexpr int64_t kGradTile = (int64_t)TH * kGradGroup * N;
   const int tid = threadIdx.x;
   const float c = kLog2e / P.temperature;
   for (int64_t u = blockIdx.x; u < P.rows * P.tiles; u += gridDim.x) {
@@ -509,7 +604,7 @@ __global__ void __launch_bounds__(kThreads) k_log_probs_grad(LogProbsGrad P) {
     uint8_t b[kGradGroup][N];
 #pragma unroll
     for (int q = 0; q < kGradGroup; ++q) {
-      const int32_t i = (tid + q * kThreads) * N;
+      const int32_t i = (tid + q * TH) * N;
       if (i + N <= len) {
         a[q] = load_vec(x + i);
         if constexpr (EX) __builtin_memcpy(b[q], ex + i, N);
@@ -517,7 +612,7 @@ __global__ void __launch_bounds__(kThreads) k_log_probs_grad(LogProbsGrad P) {
     }
 #pragma unroll
     for (int q = 0; q < kGradGroup; ++q) {
-      const int32_t i = (tid + q * kThreads) * N;
+      const int32_t i = (tid + q * TH) * N;
       if (i + N <= len) {
         Vec<T> y;
 #pragma unroll
@@ -536,7 +631,7 @@ constexpr int64_t kMostGroups = 1 << 20;
 // How a row is split: enough workgroups to fill the GPU (eight for each of
 // 256 CUs) while a part keeps 64 KB or so of scores, and a row at most 1024
 // parts.
-constexpr int64_t kFullGpu = 2048, kLeastPart = 16384, kMostParts = 1024;
+constexpr int64_t kFullGpu = 2048, kLeastPart = 16384;
 struct Split {
   int64_t parts, len;
 };
@@ -549,36 +644,51 @@ Split split_of(int64_t rows, int64_t cols) {
 }
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
 
+// Rows of at most this many scores go to workgroups of one wave.
+constexpr int64_t kShortRow = 2048;
+
+template <bool V>
+using Flag = std::integral_constant<bool, V>;
+template <class F>
+void with_flags(bool a, bool b, const F &f) {
+  if (a && b) f(Flag<true>{}, Flag<true>{});
+  else if (a) f(Flag<true>{}, Flag<false>{});
+  else if (b) f(Flag<false>{}, Flag<true>{});
+  else f(Flag<false>{}, Flag<false>{});
+}
+
 template <class T>
 hipError_t log_probs(const LogProbs &p, hipStream_t stream) {
-  const dim3 groups((unsigned)std::min(p.rows * p.parts, kMostGroups)), threads(kThreads);
-  if (p.ex) {
-    if (p.top) hipLaunchKernelGGL((k_log_probs<T, true, true>), groups, threads, 0, stream, p);
-    else hipLaunchKernelGGL((k_log_probs<T, true, false>), groups, threads, 0, stream, p);
-  } else {
-    if (p.top) hipLaunchKernelGGL((k_log_probs<T, false, true>), groups, threads, 0, stream, p);
-    else hipLaunchKernelGGL((k_log_probs<T, false, false>), groups, threads, 0, stream, p);
-  }
+  const dim3 groups((unsigned)std::min(p.rows * p.parts, kMostGroups));
+  with_flags(p.ex, p.top, [&](auto ex, auto top) {
+    constexpr bool EX = decltype(ex)::value, TOP = decltype(top)::value;
+    if (p.cols <= kShortRow)
+      hipLaunchKernelGGL((k_log_probs<T, EX, TOP, 64>), groups, dim3(64), 0, stream, p);
+    else
+      hipLaunchKernelGGL((k_log_probs<T, EX, TOP, kThreads>), groups, dim3(kThreads), 0, stream,
+                         p);
+  });
   if (p.parts > 1)
-    hipLaunchKernelGGL(k_log_probs_join<T>, dim3((unsigned)std::min(p.rows, kMostGroups)), threads,
-                       0, stream, p);
+    hipLaunchKernelGGL(k_log_probs_join<T>, dim3((unsigned)std::min(p.rows, kMostGroups)),
+                       dim3(kThreads), 0, stream, p);
   return hipGetLastError();
 }
 
 template <class T>
 hipError_t log_probs_grad(LogProbsGrad p, hipStream_t stream) {
-  constexpr int64_t kTile = (int64_t)kThreads * kGradGroup * Vec<T>::N;
-  p.tiles = (p.cols + kTile - 1) / kTile;
-  const dim3 groups((unsigned)std::min(p.rows * p.tiles, kMostGroups)), threads(kThreads);
-  if (p.ex) {
-    if (p.g_entropy)
-      hipLaunchKernelGGL((k_log_probs_grad<T, true, true>), groups, threads, 0, stream, p);
-    else hipLaunchKernelGGL((k_log_probs_grad<T, true, false>), groups, threads, 0, stream, p);
-  } else {
-    if (p.g_entropy)
-      hipLaunchKernelGGL((k_log_probs_grad<T, false, true>), groups, threads, 0, stream, p);
-    else hipLaunchKernelGGL((k_log_probs_grad<T, false, false>), groups, threads, 0, stream, p);
-  }
+  with_flags(p.ex, p.g_entropy, [&](auto ex, auto ent) {
+    constexpr bool EX = decltype(ex)::value, ENT = decltype(ent)::value;
+    const auto go = [&](auto threads) {
+      constexpr int TH = decltype(threads)::value;
+      constexpr int64_t kTile = (int64_t)TH * kGradGroup * Vec<T>::N;
+      p.tiles = (p.cols + kTile - 1) / kTile;
+      hipLaunchKernelGGL((k_log_probs_grad<T, EX, ENT, TH>),
+                         dim3((unsigned)std::min(p.rows * p.tiles, kMostGroups)), dim3(TH), 0,
+                         stream, p);
+    };
+    if (p.cols <= kShortRow) go(std::integral_constant<int, 64>{});
+    else go(std::integral_constant<int, kThreads>{});
+  });
   return hipGetLastError();
 }
 
