@@ -393,7 +393,7 @@ def bgmf_clip_grad_norm_workspace(count: int) -> int:
 
 
 def bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream) -> None:
-    """``grads``: a ctypes array of ``Grad``."""
+    """``grads``: a ctypes array of ``Grad``, or the address of one."""
     _check(None, _lib.bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream))
 
 

@@ -8,11 +8,12 @@ namespace bgmfk {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPartials = 1024;  // workgroups of the norm's first pass, at most
-constexpr int kTable = 60;       // gradients that travel in one kernel's arguments (under 4 KB)
+constexpr int kGroups = 2048;  // workgroups of the norm's pass, at most
+constexpr int kTable = 60;     // gradients that travel in a kernel's arguments (under 4 KB)
 
-// A workgroup works on whole chunks of kChunk elements of one gradient;
-// gradient i has chunks [first_chunk of i, first_chunk of i + 1).
+// Gradients are worked on in chunks of kChunk elements; gradient i has chunks
+// [first_chunk of i, first_chunk of i + 1).  A gradient whose rows are adjacent
+// counts as one row.
 constexpr int64_t kChunk = 8192;
 struct Entry {
   const void *in;
@@ -25,36 +26,29 @@ struct Batch {
   Entry e[kTable];
 };
 
-__global__ void __launch_bounds__(kTable) k_table(Batch b, int count, Entry *table) {
+__global__ void __launch_bounds__(64) k_table(Batch b, int count, Entry *table) {
   if ((int)threadIdx.x < count) table[threadIdx.x] = b.e[threadIdx.x];
 }
 
 // The gradient of chunk c: the last entry whose first chunk is at most c.
-__device__ __forceinline__ Entry find(const Entry *table, int64_t count, int64_t c) {
-  int64_t lo = 0, hi = count - 1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) / 2;
-    if (table[mid].first_chunk <= c) lo = mid;
-    else hi = mid - 1;
+// Every wave looks at 64 entries at a time.
+__device__ __forceinline__ int32_t find(const Entry *table, int32_t count, int64_t c) {
+  int32_t below = 0;
+  for (int32_t i0 = 0; i0 < count; i0 += 64) {
+    const int32_t i = i0 + (int32_t)(threadIdx.x % 64);
+    below += __popcll(__ballot(i < count && table[i].first_chunk <= c));
   }
-  return table[lo];
+  return __builtin_amdgcn_readfirstlane(below - 1);
 }
 
-__device__ __forceinline__ float load(const Entry &e, int64_t i) {
-  const int64_t at = i / e.cols * e.in_stride + i % e.cols;
-  if (e.type == BGMF_TYPE_F32) return static_cast<const float *>(e.in)[at];
-  if (e.type == BGMF_TYPE_BF16) return to_float(static_cast<const bf16_t *>(e.in)[at]);
-  return to_float(static_cast<const f16_t *>(e.in)[at]);
-}
-__device__ __forceinline__ void store(const Entry &e, int64_t i, float v) {
-  const int64_t at = i / e.cols * e.out_stride + i % e.cols;
-  if (e.type == BGMF_TYPE_F32) static_cast<float *>(e.out)[at] = v;
-  else if (e.type == BGMF_TYPE_BF16) static_cast<bf16_t *>(e.out)[at] = from_float<bf16_t>(v);
-  else static_cast<f16_t *>(e.out)[at] = from_float<f16_t>(v);
+template <class T>
+__device__ __forceinline__ double square(T x) {
+  const double v = to_float(x);
+  return v * v;
 }
 
 // Sum over the workgroup, the same order at every call.
-__device__ double block_sum(double v) {
+__device__ __forceinline__ double block_sum(double v) {
   __shared__ double lds[kThreads / 64];
 #pragma unroll
   for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
@@ -66,38 +60,129 @@ __device__ double block_sum(double v) {
   return s;
 }
 
-__global__ void __launch_bounds__(kThreads) k_norm(const Entry *table, int64_t count,
-                                                   int64_t chunks, double *partial) {
-  double s = 0.0;
+// Calls f(entry, type, lo, hi) for the elements [lo, hi) of each chunk that
+// the workgroup has: every gridDim.x-th, so that the chunks worked on at one
+// time lie next to each other.
+template <class F>
+__device__ __forceinline__ void for_chunks(const Entry *table, int32_t count, int64_t chunks,
+                                           const F &f) {
+  Entry e;
+  int64_t stop = -1;  // the first chunk past e's
   for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Entry e = find(table, count, c);
-    const int64_t lo = (c - e.first_chunk) * kChunk, end = e.rows * e.cols;
-    const int64_t hi = lo + kChunk < end ? lo + kChunk : end;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-      const double v = load(e, i);
-      s += v * v;
+    if (c >= stop) {
+      const int32_t at = find(table, count, c);
+      e = table[at];
+      stop = at + 1 < count ? table[at + 1].first_chunk : chunks;
     }
+    const int64_t lo = (c - e.first_chunk) * kChunk, size = e.rows * e.cols;
+    const int64_t hi = lo + kChunk < size ? lo + kChunk : size;
+    if (e.type == BGMF_TYPE_F32) f(e, float{}, lo, hi);
+    else if (e.type == BGMF_TYPE_BF16) f(e, bf16_t{}, lo, hi);
+    else f(e, f16_t{}, lo, hi);
   }
+}
+
+// Squares in fp64: no gradient overflows or vanishes in them, and their sum is
+// better than fp32 whatever its order.  Bound: HBM, one read.
+__device__ __forceinline__ void norm_part(const Entry *table, int32_t count, int64_t chunks,
+                                          double *partial) {
+  double s = 0.0;
+  for_chunks(table, count, chunks, [&](const Entry &e, auto type, int64_t lo, int64_t hi) {
+    using T = decltype(type);
+    constexpr int N = Vec<T>::N, K = (int)(kChunk / (kThreads * N));
+    const T *x = static_cast<const T *>(e.in);
+    const int tid = threadIdx.x;
+    if (e.rows == 1 && hi - lo == kChunk) {
+      Vec<T> a[K];
+#pragma unroll
+      for (int q = 0; q < K; ++q) a[q] = load_vec(x + lo + (tid + q * kThreads) * N);
+#pragma unroll
+      for (int q = 0; q < K; ++q)
+#pragma unroll
+        for (int i = 0; i < N; ++i) s += square(a[q].v[i]);
+    } else if (e.rows == 1) {
+      int64_t i = lo + tid * N;
+      for (; i + N <= hi; i += kThreads * N) {
+        const Vec<T> a = load_vec(x + i);
+#pragma unroll
+        for (int k = 0; k < N; ++k) s += square(a.v[k]);
+      }
+      for (; i < hi; ++i) s += square(x[i]);
+    } else {
+      for (int64_t i = lo + tid; i < hi; i += kThreads)
+        s += square(x[i / e.cols * e.in_stride + i % e.cols]);
+    }
+  });
   s = block_sum(s);
   if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-__global__ void __launch_bounds__(kThreads) k_clip(const Entry *table, int64_t count,
-                                                   int64_t chunks, const double *partial,
-                                                   int partials, float max_norm, float *norm) {
+// The norm from the partial sums, by every workgroup, and the gradients times
+// the factor.  Bound: HBM, one read (from the Infinity Cache where the
+// gradients fit it) and one write.
+__device__ __forceinline__ void clip_part(const Entry *table, int32_t count, int64_t chunks,
+                                          const double *partial, int partials, float max_norm,
+                                          float *norm) {
   double s = 0.0;
   for (int i = threadIdx.x; i < partials; i += kThreads) s += partial[i];
   const float n = (float)sqrt(block_sum(s));
   if (blockIdx.x == 0 && threadIdx.x == 0) *norm = n;
   const bool clips = n > max_norm && n < INFINITY;
   const float factor = clips ? max_norm / n : 1.0f;
-  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
-    const Entry e = find(table, count, c);
-    if (!clips && e.in == e.out) continue;
-    const int64_t lo = (c - e.first_chunk) * kChunk, end = e.rows * e.cols;
-    const int64_t hi = lo + kChunk < end ? lo + kChunk : end;
-    for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) store(e, i, load(e, i) * factor);
-  }
+  for_chunks(table, count, chunks, [&](const Entry &e, auto type, int64_t lo, int64_t hi) {
+    using T = decltype(type);
+    constexpr int N = Vec<T>::N, K = (int)(kChunk / (kThreads * N));
+    if (!clips && e.in == e.out) return;
+    const T *x = static_cast<const T *>(e.in);
+    T *y = static_cast<T *>(e.out);
+    const int tid = threadIdx.x;
+    const auto scaled = [&](T v) { return from_float<T>(to_float(v) * factor); };
+    if (e.rows == 1 && hi - lo == kChunk) {
+      Vec<T> a[K];
+#pragma unroll
+      for (int q = 0; q < K; ++q) a[q] = load_vec(x + lo + (tid + q * kThreads) * N);
+#pragma unroll
+      for (int q = 0; q < K; ++q) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) a[q].v[i] = scaled(a[q].v[i]);
+        store_vec_stream(y + lo + (tid + q * kThreads) * N, a[q]);
+      }
+    } else if (e.rows == 1) {
+      int64_t i = lo + tid * N;
+      for (; i + N <= hi; i += kThreads * N) {
+        Vec<T> a = load_vec(x + i);
+#pragma unroll
+        for (int k = 0; k < N; ++k) a.v[k] = scaled(a.v[k]);
+        store_vec_stream(y + i, a);
+      }
+      for (; i < hi; ++i) y[i] = scaled(x[i]);
+    } else {
+      for (int64_t i = lo + tid; i < hi; i += kThreads) {
+        const int64_t r = i / e.cols, k = i % e.cols;
+        y[r * e.out_stride + k] = scaled(x[r * e.in_stride + k]);
+      }
+    }
+  });
+}
+
+// The table in the kernel's arguments, or in the workspace.
+__global__ void __launch_bounds__(kThreads) k_norm_few(Batch b, int32_t count, int64_t chunks,
+                                                       double *partial) {
+  norm_part(b.e, count, chunks, partial);
+}
+__global__ void __launch_bounds__(kThreads) k_norm(const Entry *table, int32_t count,
+                                                   int64_t chunks, double *partial) {
+  norm_part(table, count, chunks, partial);
+}
+__global__ void __launch_bounds__(kThreads) k_clip_few(Batch b, int32_t count, int64_t chunks,
+                                                       const double *partial, int partials,
+                                                       float max_norm, float *norm) {
+  clip_part(b.e, count, chunks, partial, partials, max_norm, norm);
+}
+__global__ void __launch_bounds__(kThreads) k_clip(const Entry *table, int32_t count,
+                                                   int64_t chunks, const double *partial,
+                                                   int partials, float max_norm, float *norm) {
+  clip_part(table, count, chunks, partial, partials, max_norm, norm);
 }
 
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
@@ -111,7 +196,7 @@ extern "C" {
 
 int64_t bgmf_clip_grad_norm_workspace(int64_t count) {
   if (count < 0 || count >= (1ll << 31)) return 0;
-  return padded(kPartials * 8) + padded(count * (int64_t)sizeof(Entry));
+  return padded(kGroups * 8) + padded(count * (int64_t)sizeof(Entry));
 }
 
 int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm, float *norm,
@@ -146,31 +231,40 @@ int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm,
   }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   double *partial = static_cast<double *>(ws);
-  Entry *table = reinterpret_cast<Entry *>(static_cast<char *>(ws) + padded(kPartials * 8));
-  int64_t chunks = 0, entries = 0;
+  Entry *table = reinterpret_cast<Entry *>(static_cast<char *>(ws) + padded(kGroups * 8));
+  int64_t chunks = 0;
+  int32_t entries = 0, held = 0;
   Batch b;
-  int held = 0;
   const auto send = [&] {
     if (held)
-      hipLaunchKernelGGL(k_table, dim3(1), dim3(kTable), 0, stream, b, held,
-                         table + entries - held);
+      hipLaunchKernelGGL(k_table, dim3(1), dim3(64), 0, stream, b, held, table + entries - held);
     held = 0;
   };
   for (int64_t i = 0; i < count; ++i) {
     const bgmf_grad_t &g = grads[i];
     if (g.rows == 0 || g.cols == 0) continue;
-    b.e[held++] = Entry{g.in, g.out, g.rows, g.cols, g.in_stride, g.out_stride, chunks, g.type};
+    if (held == kTable) send();
+    const bool dense = g.rows == 1 || (g.in_stride == g.cols && g.out_stride == g.cols);
+    b.e[held++] = Entry{g.in,        g.out,        dense ? 1 : g.rows, dense ? g.rows * g.cols : g.cols,
+                        g.in_stride, g.out_stride, chunks,             g.type};
     ++entries;
     chunks += (g.rows * g.cols + kChunk - 1) / kChunk;
-    if (held == kTable) send();
   }
-  send();
-  const unsigned groups = (unsigned)std::min<int64_t>(chunks, kPartials);
-  if (groups)
+  const unsigned groups = (unsigned)std::min<int64_t>(chunks, kGroups);
+  const unsigned clip_groups = (unsigned)std::max<int64_t>(std::min<int64_t>(chunks, kGroups), 1);
+  if (entries <= kTable) {
+    if (groups)
+      hipLaunchKernelGGL(k_norm_few, dim3(groups), dim3(kThreads), 0, stream, b, entries, chunks,
+                         partial);
+    hipLaunchKernelGGL(k_clip_few, dim3(clip_groups), dim3(kThreads), 0, stream, b, entries,
+                       chunks, partial, (int)groups, max_norm, norm);
+  } else {
+    send();
     hipLaunchKernelGGL(k_norm, dim3(groups), dim3(kThreads), 0, stream, table, entries, chunks,
                        partial);
-  hipLaunchKernelGGL(k_clip, dim3(groups ? groups : 1), dim3(kThreads), 0, stream, table, entries,
-                     chunks, partial, (int)groups, max_norm, norm);
+    hipLaunchKernelGGL(k_clip, dim3(clip_groups), dim3(kThreads), 0, stream, table, entries,
+                       chunks, partial, (int)groups, max_norm, norm);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return fail_call(BGMF_E_HIP, "%s: %s", call, hipGetErrorString(e));
   return BGMF_OK;

@@ -65,5 +65,13 @@ template <class T>
 __device__ __forceinline__ void store_vec(T *p, const Vec<T> &x) {
   __builtin_memcpy(p, &x, sizeof x);
 }
+// The same for what is not read again soon.
+template <class T>
+__device__ __forceinline__ void store_vec_stream(T *p, const Vec<T> &x) {
+  typedef uint32_t quad __attribute__((ext_vector_type(4), aligned(2)));
+  quad q;
+  __builtin_memcpy(&q, &x, sizeof q);
+  __builtin_nontemporal_store(q, reinterpret_cast<quad *>(p));
+}
 
 }  // namespace bgmfk

@@ -16,6 +16,7 @@ from typing import NamedTuple, Optional, Sequence, Tuple
 
 from . import bgmf  # before torch: one HIP runtime in the process
 
+import numpy as np
 import torch
 
 TOP_MAX = bgmf.BGMF_TOP_MAX
@@ -271,13 +272,13 @@ class Catalogue:
 
 # --- clipping -------------------------------------------------------------------
 
-def _layout(t: torch.Tensor) -> Optional[Tuple[int, int, int]]:
-    """(rows, cols, row stride) that cover t's elements, None if none do."""
+def _layout(t: torch.Tensor) -> Tuple[int, int, int]:
+    """(rows, cols, row stride) that cover a gradient's elements."""
     if t.is_contiguous():
         return 1, t.numel(), t.numel()
     if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
         return t.shape[0], t.shape[1], t.stride(0)
-    return None
+    raise ValueError("a gradient is neither contiguous nor 2-D with adjacent row elements")
 
 
 def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
@@ -290,30 +291,41 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
     grads = list(grads)
     if not grads:
         raise ValueError("clip_grad_norm needs at least one gradient")
-    dev = grads[0].device
+    dev = grads[0].get_device()
     out = grads if out is None else list(out)
     if len(out) != len(grads):
         raise ValueError("out must have a tensor for each gradient")
-    table = (bgmf.Grad * len(grads))()
-    for e, g, o in zip(table, grads, out):
-        code = _TYPES.get(g.dtype)
-        if code is None or not g.is_cuda or g.device != dev:
-            raise ValueError("gradients must be float32, bfloat16 or float16 on one GPU")
-        at = _layout(g)
-        to = at if o is g else _layout(o)
-        if o.shape != g.shape or o.dtype != g.dtype or o.device != dev:
-            raise ValueError("out must have the gradients' shapes, types and device")
-        if at is None or to is None:
-            raise ValueError("a gradient is neither contiguous nor 2-D with adjacent row elements")
-        if at[0] != to[0]:  # one side is a matrix with a row stride: both are taken as one
-            at, to = ((t.shape[0], t.shape[1], t.stride(0)) for t in (g, o))
-        e.in_, e.out, e.type = g.data_ptr(), o.data_ptr(), code
-        e.rows, e.cols, e.in_stride = at
-        e.out_stride = to[2]
-    norm = torch.empty((), device=dev)
+    sides = (grads,) if out is grads else (grads, out)
+    types = [g.dtype for g in grads]
+    # whole columns of the table at a time: a model has hundreds of gradients
+    for side in sides:
+        if dev < 0 or any(d != dev for d in map(torch.Tensor.get_device, side)):
+            raise ValueError("gradients and out must be on one GPU")
+    if any(t not in _TYPES for t in set(types)):
+        raise ValueError("gradients must be float32, bfloat16 or float16")
+    if out is not grads:
+        if types != [o.dtype for o in out]:
+            raise ValueError("out must have the gradients' types")
+        if any(g.shape != o.shape for g, o in zip(grads, out)):
+            raise ValueError("out must have the gradients' shapes")
+    table = np.zeros((len(grads), 7), dtype=np.int64)  # rows of bgmf_grad_t
+    table[:, 0] = [g.data_ptr() for g in grads]
+    table[:, 1] = table[:, 0] if out is grads else [o.data_ptr() for o in out]
+    table[:, 6] = [_TYPES[t] for t in types]
+    if all(all(map(torch.Tensor.is_contiguous, side)) for side in sides):
+        table[:, 2] = 1
+        table[:, 3] = list(map(torch.Tensor.numel, grads))
+        table[:, 4] = table[:, 5] = table[:, 3]
+    else:
+        for row, g, o in zip(table, grads, out):
+            at, to = _layout(g), _layout(o)
+            if at[0] != to[0]:  # one side has a row stride: both are taken as matrices
+                at, to = ((t.shape[0], t.shape[1], t.stride(0)) for t in (g, o))
+            row[2:6] = (*at, to[2])
+    norm = torch.empty((), device=grads[0].device)
     nbytes = bgmf.bgmf_clip_grad_norm_workspace(len(grads))
     ws = _workspace(nbytes, grads[0])
     with _on(grads[0]):
-        bgmf.bgmf_clip_grad_norm(table, len(grads), float(max_norm), norm.data_ptr(),
+        bgmf.bgmf_clip_grad_norm(table.ctypes.data, len(grads), float(max_norm), norm.data_ptr(),
                                  ws.data_ptr(), nbytes, _stream(grads[0]))
     return norm
