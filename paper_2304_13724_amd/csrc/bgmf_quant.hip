@@ -17,11 +17,32 @@ using i32x16 = __attribute__((ext_vector_type(16))) int32_t;
 
 // ---------------------------------------------------------------------------
 // Rows to bytes.  One pass over global memory: LANES threads hold a row
-// (HELD vectors of 16 bytes each), reduce its largest magnitude, and write
+// (kHeld vectors of 16 bytes each), reduce its largest magnitude, and write
 // the quotients; what a longer row has beyond that is read a second time.
 // Bound: HBM.
 // ---------------------------------------------------------------------------
 constexpr int kHeld = 4;
+
+// Largest magnitude, +infinity where a value is NaN or infinite.
+struct Largest {
+  float most = 0.0f;
+  bool bad = false;
+  __device__ __forceinline__ void look(float x) {
+    const float v = fabsf(x);
+    bad |= !(v < INFINITY);
+    most = fmaxf(most, v);
+  }
+  __device__ __forceinline__ float get() const { return bad ? INFINITY : most; }
+};
+// The scale of a row with that magnitude, and a value's byte; NaN and 0 bytes
+// where it is infinite.
+__device__ __forceinline__ float scale_of(float most) {
+  return most == INFINITY ? NAN : most / 127.0f;
+}
+__device__ __forceinline__ int8_t byte_of(float x, float scale) {
+  const float y = scale > 0.0f ? rintf(x / scale) : 0.0f;
+  return (int8_t)fminf(fmaxf(y, -127.0f), 127.0f);
+}
 
 template <class T, int LANES>
 __global__ void __launch_bounds__(kThreads) k_quantize(const T *x, int64_t rows, int32_t k,
@@ -29,38 +50,29 @@ __global__ void __launch_bounds__(kThreads) k_quantize(const T *x, int64_t rows,
                                                        int32_t fill, float *scale) {
   constexpr int N = Vec<T>::N;
   const int lane = threadIdx.x % LANES;
-  const int32_t vecs = (k + N - 1) / N;
+  const int32_t vecs = k / N, tail = vecs * N + lane;
   __shared__ float lds[kWaves];
   for (int64_t r = (int64_t)blockIdx.x * (kThreads / LANES) + threadIdx.x / LANES; r < rows;
        r += (int64_t)gridDim.x * (kThreads / LANES)) {
     const T *row = x + r * stride;
-    const auto load = [&](int32_t v) {  // vector v of the row, zeros past its end
-      Vec<T> a = {};
-      const int32_t at = v * N;
-      if (at + N <= k) a = load_vec(row + at);
-      else
-        for (int i = 0; i < N; ++i)
-          if (at + i < k) a.v[i] = row[at + i];
-      return a;
-    };
-    float most = 0.0f;
-    bool bad = false;
-    const auto look = [&](const Vec<T> &a) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float v = fabsf(to_float(a.v[i]));
-        bad |= !(v < INFINITY);
-        most = fmaxf(most, v);
-      }
-    };
+    Largest a;
     Vec<T> held[kHeld];
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h) held[h] = load(lane + h * LANES);
+    for (int h = 0; h < kHeld; ++h)
+      if (lane + h * LANES < vecs) held[h] = load_vec(row + (lane + h * LANES) * N);
+      else held[h] = {};
+    for (int32_t i = tail; i < k; i += LANES) a.look(to_float(row[i]));
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h) look(held[h]);
+    for (int h = 0; h < kHeld; ++h)
+#pragma unroll
+      for (int i = 0; i < N; ++i) a.look(to_float(held[h].v[i]));
 #pragma unroll 4
-    for (int32_t v = lane + kHeld * LANES; v < vecs; v += LANES) look(load(v));
-    if (bad) most = INFINITY;
+    for (int32_t v = lane + kHeld * LANES; v < vecs; v += LANES) {
+      const Vec<T> more = load_vec(row + v * N);
+#pragma unroll
+      for (int i = 0; i < N; ++i) a.look(to_float(more.v[i]));
+    }
+    float most = a.get();
 #pragma unroll
     for (int o = LANES < 64 ? LANES / 2 : 32; o; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
     if constexpr (LANES > 64) {
@@ -70,25 +82,20 @@ __global__ void __launch_bounds__(kThreads) k_quantize(const T *x, int64_t rows,
       for (int w = 0; w < kWaves; ++w) most = fmaxf(most, lds[w]);
       __syncthreads();
     }
-    const float s = most == INFINITY ? NAN : most / 127.0f;
+    const float s = scale_of(most);
     if (lane == 0) scale[r] = s;
     int8_t *to = q + r * q_stride;
     const auto put = [&](int32_t v, const Vec<T> &a) {
       int8_t b[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const float y = s > 0.0f ? rintf(to_float(a.v[i]) / s) : 0.0f;
-        b[i] = (int8_t)fminf(fmaxf(y, -127.0f), 127.0f);
-      }
-      const int32_t at = v * N;
-      if (at + N <= fill) __builtin_memcpy(to + at, b, N);
-      else
-        for (int i = 0; i < N; ++i)
-          if (at + i < fill) to[at + i] = b[i];
+      for (int i = 0; i < N; ++i) b[i] = byte_of(to_float(a.v[i]), s);
+      __builtin_memcpy(to + v * N, b, N);
     };
 #pragma unroll
-    for (int h = 0; h < kHeld; ++h) put(lane + h * LANES, held[h]);
-    for (int32_t v = lane + kHeld * LANES; v * N < fill; v += LANES) put(v, load(v));
+    for (int h = 0; h < kHeld; ++h)
+      if (lane + h * LANES < vecs) put(lane + h * LANES, held[h]);
+    for (int32_t v = lane + kHeld * LANES; v < vecs; v += LANES) put(v, load_vec(row + v * N));
+    for (int32_t i = tail; i < fill; i += LANES) to[i] = i < k ? byte_of(to_float(row[i]), s) : 0;
   }
 }
 
@@ -131,6 +138,8 @@ constexpr int kUnit = 64;
 inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; }
 
 struct Product {
+  const void *x;    // users' values (own_bytes)
+  int64_t x_stride;
   const int8_t *a;  // users: rows x kp
   const float *a_scale;
   int64_t rows;
@@ -168,16 +177,24 @@ __device__ __forceinline__ i32x4 item_bytes(const int8_t *row, int32_t c) {
   return x;
 }
 // The same where c may be at or past the row's end: nothing is read past the
-// end of the matrix.
+// end of the matrix (of at least 16 bytes), whose last bytes are shifted into
+// their place.
 __device__ __forceinline__ i32x4 item_bytes_tail(const int8_t *row, int32_t c, int32_t k,
                                                  const int8_t *end) {
   i32x4 x = {0, 0, 0, 0};
-  if (c >= k) return x;
-  if (row + c + 16 <= end) return item_bytes(row, c);
-  int8_t b[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) b[i] = c + i < k ? row[c + i] : (int8_t)0;
-  __builtin_memcpy(&x, b, 16);
+  if (c < k) {
+    const int64_t past = row + c + 16 - end;
+    x = item_bytes(row, (int32_t)(past > 0 ? c - past : c));
+    if (past > 0) {
+      uint64_t w[2];
+      __builtin_memcpy(w, &x, 16);
+      const int bits = (int)past * 8;  // 8 to 120
+      const uint64_t carried = bits < 64 ? w[1] << (64 - bits) : 0;
+      w[0] = bits < 64 ? w[0] >> bits | carried : w[1] >> (bits - 64);
+      w[1] = bits < 64 ? w[1] >> bits : 0;
+      __builtin_memcpy(&x, w, 16);
+    }
+  }
   return x;
 }
 
@@ -186,93 +203,190 @@ __device__ __forceinline__ O score_of(int32_t sum, float a, float b) {
   return from_float<O>((float)sum * a * b);
 }
 
+// Items of less than 16 bytes altogether: one thread per score.
+template <class O>
+__global__ void __launch_bounds__(kThreads) k_product_tiny(Product P) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < P.rows * P.items;
+       i += (int64_t)gridDim.x * kThreads) {
+    const int64_t r = i / P.items, j = i % P.items;
+    int32_t sum = 0;
+    for (int32_t c = 0; c < P.k; ++c)
+      sum += (int32_t)P.a[r * P.kp + c] * P.b[j * P.b_stride + c];
+    static_cast<O *>(P.out)[r * P.out_stride + j] =
+        score_of<O>(sum, P.a_scale[r], P.b_scale[j]);
+  }
+}
+
 // Few users (rows <= 16 USERS): every item's bytes go from global memory into
 // a matrix instruction once (v_mfma_i32_16x16x64_i8: 16 items x 16 users, 64
 // columns of k; lane l holds 16 bytes of item l % 16 and of user l % 16).  A
-// wave takes ITEMS tiles of 16 items, so that many loads are in flight.  With
-// SPLIT, the workgroup's waves share the tiles and take a quarter of k each.
-// Bound: HBM (the items' bytes).
-template <class O, int USERS, int ITEMS, bool SPLIT>
-__global__ void __launch_bounds__(kThreads) k_product_few(Product P) {
+// wave takes ITEMS tiles of 16 items at a time, and while it forms their
+// products the bytes and scales of its next step or tiles are on their way.
+// With SPLIT, the waves of a workgroup share the tiles and take a quarter of k
+// each.  Bound: HBM (the items' bytes).
+//
+// X: int8_t, users' bytes in P.a; or the type of their values in P.x, which
+// every wave then turns into bytes itself (one launch less; k <= 64 kOwn).
+constexpr int kOwn = 4;
+
+template <class X>
+__device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part, i32x4 (&y)[kOwn]) {
+  const X *x = static_cast<const X *>(P.x) + r * P.x_stride;
+  float v[kOwn][16];
+  Largest a;
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s) {
+    const int32_t c = s * 64 + part * 16;
+    if (c + 16 <= P.k) {
+      constexpr int N = Vec<X>::N;
+#pragma unroll
+      for (int h = 0; h < 16 / N; ++h) {
+        const Vec<X> w = load_vec(x + c + h * N);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[s][h * N + i] = to_float(w.v[i]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[s][i] = c + i < P.k ? to_float(x[c + i]) : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a.look(v[s][i]);
+  }
+  float most = a.get();
+  most = fmaxf(most, __shfl_xor(most, 16));
+  most = fmaxf(most, __shfl_xor(most, 32));
+  const float scale = scale_of(most);
+#pragma unroll
+  for (int s = 0; s < kOwn; ++s) {
+    int8_t b[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) b[i] = byte_of(v[s][i], scale);
+    __builtin_memcpy(&y[s], b, 16);
+  }
+  return scale;
+}
+
+template <class O, class X, int USERS, int ITEMS, bool SPLIT>
+__global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
+  constexpr bool OWN = !std::is_same<X, int8_t>::value;
+  static_assert(!OWN || (USERS == 1 && !SPLIT), "own bytes: one tile of users");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int l16 = lane % 16, part = lane / 16;
-  const int64_t first = SPLIT ? (int64_t)blockIdx.x * (16 * ITEMS)
-                              : ((int64_t)blockIdx.x * kWaves + wave) * (16 * ITEMS);
-  if (!SPLIT && first >= P.items) return;
-  const int8_t *item[ITEMS], *user[USERS];
+  const int64_t tiles = (P.items + 16 * ITEMS - 1) / (16 * ITEMS);
+  int64_t tile = SPLIT ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
+  const int64_t stride = SPLIT ? gridDim.x : (int64_t)gridDim.x * kWaves;
+  if (tile >= tiles) return;  // with SPLIT, all waves or none
+
+  const int64_t own_row = l16 < P.rows ? l16 : P.rows - 1;
+  i32x4 own[OWN ? kOwn : 1];
+  float a_scale[USERS];
+  const int8_t *user[USERS];
+  if constexpr (OWN) {
+    a_scale[0] = own_bytes<X>(P, own_row, part, own);
+  } else {
 #pragma unroll
-  for (int t = 0; t < ITEMS; ++t) {
-    const int64_t j = first + t * 16 + l16;
-    item[t] = P.b + (j < P.items ? j : P.items - 1) * P.b_stride;
+    for (int u = 0; u < USERS; ++u) {
+      const int64_t r = u * 16 + l16 < P.rows ? u * 16 + l16 : P.rows - 1;
+      a_scale[u] = P.a_scale[r];
+      user[u] = P.a + r * P.kp + part * 16;
+    }
   }
-#pragma unroll
-  for (int u = 0; u < USERS; ++u) {
-    const int64_t r = u * 16 + l16;
-    user[u] = P.a + (r < P.rows ? r : P.rows - 1) * P.kp + part * 16;
-  }
-  i32x4 acc[ITEMS][USERS] = {};
   const int steps = P.kp / 64, full = P.k / 64;
   const int begin = SPLIT ? steps * wave / kWaves : 0;
   const int end = SPLIT ? steps * (wave + 1) / kWaves : steps;
-  const auto step = [&](int s, auto tail) {
-    const int32_t c = s * 64 + part * 16;
-    i32x4 x[ITEMS], y[USERS];
-#pragma unroll
-    for (int t = 0; t < ITEMS; ++t) {
-      if constexpr (decltype(tail)::value) x[t] = item_bytes_tail(item[t], c, P.k, P.b_end);
-      else x[t] = item_bytes(item[t], c);
-    }
-#pragma unroll
-    for (int u = 0; u < USERS; ++u) y[u] = *reinterpret_cast<const i32x4 *>(user[u] + s * 64);
-#pragma unroll
-    for (int t = 0; t < ITEMS; ++t)
-#pragma unroll
-      for (int u = 0; u < USERS; ++u)
-        acc[t][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[t], y[u], acc[t][u], 0, 0, 0);
-  };
-#pragma unroll(SPLIT ? 4 : 1)
-  for (int s = begin; s < (end < full ? end : full); ++s) step(s, std::false_type{});
-  if (full < end && end == steps) step(full, std::true_type{});
 
-  if constexpr (SPLIT) {
-    __shared__ i32x4 lds[kWaves - 1][ITEMS * USERS][64];
-    if (wave) {
+  // on its way: the bytes of the next step, and the scales of the next tiles
+  // (lane l holds that of item l % 16)
+  i32x4 x[ITEMS], y[USERS];
+  float scale[ITEMS];
+  const auto load = [&](int64_t t, int s) {
+    const int32_t c = s * 64 + part * 16;
+    const int8_t *row[ITEMS];
 #pragma unroll
-      for (int t = 0; t < ITEMS; ++t)
-#pragma unroll
-        for (int u = 0; u < USERS; ++u) lds[wave - 1][t * USERS + u][lane] = acc[t][u];
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t j = t * (16 * ITEMS) + i * 16 + l16, at = j < P.items ? j : P.items - 1;
+      row[i] = P.b + at * P.b_stride;
+      if (s == begin) scale[i] = P.b_scale[at];
     }
-    __syncthreads();
-    if (wave) return;
+    if (s < full) {
 #pragma unroll
-    for (int t = 0; t < ITEMS; ++t)
+      for (int i = 0; i < ITEMS; ++i) x[i] = item_bytes(row[i], c);
+    } else {
 #pragma unroll
-      for (int u = 0; u < USERS; ++u)
+      for (int i = 0; i < ITEMS; ++i) x[i] = item_bytes_tail(row[i], c, P.k, P.b_end);
+    }
+    if constexpr (!OWN) {
 #pragma unroll
-        for (int w = 0; w < kWaves - 1; ++w) acc[t][u] += lds[w][t * USERS + u][lane];
-  }
-  // lane l holds the sums of items 4 (l / 16) .. + 3 and user l % 16
+      for (int u = 0; u < USERS; ++u) y[u] = *reinterpret_cast<const i32x4 *>(user[u] + s * 64);
+    }
+  };
+  load(tile, begin);
+  for (; tile < tiles; tile += stride) {
+    i32x4 acc[ITEMS][USERS] = {};
+    float b[ITEMS];
+    const auto step = [&](int s, const i32x4 *mine) {
 #pragma unroll
-  for (int t = 0; t < ITEMS; ++t) {
-    const int64_t j = first + t * 16 + part * 4;
-    if (j >= P.items) continue;
-    const int left = P.items - j < 4 ? (int)(P.items - j) : 4;
-    float b[4] = {};
-    if (left == 4) __builtin_memcpy(b, P.b_scale + j, 16);
-    else
-      for (int i = 0; i < left; ++i) b[i] = P.b_scale[j + i];
+      for (int i = 0; i < ITEMS; ++i)
 #pragma unroll
-    for (int u = 0; u < USERS; ++u) {
-      const int64_t r = u * 16 + l16;
-      if (r >= P.rows) continue;
-      const float a = P.a_scale[r];
-      O v[4];
+        for (int u = 0; u < USERS; ++u) {
+          const i32x4 other = OWN ? *mine : y[u];
+          acc[i][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i], other, acc[i][u], 0, 0, 0);
+        }
+      const bool last = s + 1 == end;
+      const int64_t next = last ? tile + stride : tile;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = score_of<O>(acc[t][u][i], a, b[i]);
-      O *to = static_cast<O *>(P.out) + r * P.out_stride + j;
-      if (left == 4) __builtin_memcpy(to, v, 4 * sizeof(O));
-      else
-        for (int i = 0; i < left; ++i) to[i] = v[i];
+      for (int i = 0; i < ITEMS; ++i) b[i] = scale[i];
+      if (next < tiles) load(next, last ? begin : s + 1);
+    };
+    if constexpr (OWN) {  // the steps are counted out, so that the bytes stay in registers
+#pragma unroll
+      for (int s = 0; s < kOwn; ++s)
+        if (s < end) step(s, &own[s]);
+    } else {
+      for (int s = begin; s < end; ++s) step(s, nullptr);
+    }
+
+    if constexpr (SPLIT) {
+      __shared__ i32x4 lds[kWaves - 1][ITEMS * USERS][64];
+      __syncthreads();  // the last tile's sums have been read
+      if (wave) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+          for (int u = 0; u < USERS; ++u) lds[wave - 1][i * USERS + u][lane] = acc[i][u];
+      }
+      __syncthreads();
+      if (wave) continue;
+#pragma unroll
+      for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+        for (int u = 0; u < USERS; ++u)
+#pragma unroll
+          for (int w = 0; w < kWaves - 1; ++w) acc[i][u] += lds[w][i * USERS + u][lane];
+    }
+    // lane l holds the sums of items 4 (l / 16) .. + 3 and user l % 16
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      const int64_t j = tile * (16 * ITEMS) + i * 16 + part * 4;
+      float bs[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) bs[e] = __shfl(b[i], part * 4 + e);
+      if (j >= P.items) continue;
+      const int left = P.items - j < 4 ? (int)(P.items - j) : 4;
+#pragma unroll
+      for (int u = 0; u < USERS; ++u) {
+        const int64_t r = u * 16 + l16;
+        if (r >= P.rows) continue;
+        O v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = score_of<O>(acc[i][u][e], a_scale[u], bs[e]);
+        O *to = static_cast<O *>(P.out) + r * P.out_stride + j;
+        if (left == 4) __builtin_memcpy(to, v, 4 * sizeof(O));
+        else
+#pragma unroll
+          for (int e = 0; e < 3; ++e)
+            if (e < left) to[e] = v[e];
+      }
     }
   }
 }
@@ -293,7 +407,10 @@ __device__ __forceinline__ int lds_chunk(int row, int c) {
 template <class O>
 __global__ void __launch_bounds__(kThreads, 2) k_product_many(Product P, int64_t item_tiles,
                                                               int64_t user_tiles) {
-  __shared__ i32x4 lds_items[kTile * kStep / 16], lds_users[kTile * kStep / 16];
+  // a step's bytes, and afterwards the scores on their way out
+  constexpr int kStage = 2 * kTile * kStep, kScores = kWaves * 32 * (64 * (int)sizeof(O) + 16);
+  __shared__ i32x4 lds[(kStage > kScores ? kStage : kScores) / 16];
+  i32x4 *lds_items = lds, *lds_users = lds + kTile * kStep / 16;
   __shared__ float s_item[kTile], s_user[kTile];
   const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
   const int wi = wave % 2, wu = wave / 2, l32 = lane % 32, half = lane / 32;
@@ -346,56 +463,90 @@ __global__ void __launch_bounds__(kThreads, 2) k_product_many(Product P, int64_t
           acc[i][u] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fi[i], fu[u], acc[i][u], 0, 0, 0);
     }
   }
-  // register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and user l % 32
+  // Register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and
+  // user l % 32.  The scores of 32 users at a time pass through LDS, so that a
+  // user's 64 scores are stored in a row.
+  constexpr int kPitch = 64 + 16 / (int)sizeof(O);  // elements
+  __syncthreads();
+  O *mine = reinterpret_cast<O *>(lds) + wave * (32 * kPitch);
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int u = 0; u < 2; ++u) {
+    const float a = s_user[wu * 64 + u * 32 + l32];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int ru = wu * 64 + u * 32 + l32;
-      const int64_t r = r0 + ru;
-      if (r >= P.rows) continue;
-      const float a = s_user[ru];
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const int ji = wi * 64 + i * 32 + g * 8 + half * 4;
-        const int64_t j = j0 + ji;
+        const int ji = i * 32 + g * 8 + half * 4;
         O v[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[ji + e]);
-        O *to = static_cast<O *>(P.out) + r * P.out_stride + j;
-        if (j + 4 <= P.items) __builtin_memcpy(to, v, 4 * sizeof(O));
+        for (int e = 0; e < 4; ++e)
+          v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[wi * 64 + ji + e]);
+        __builtin_memcpy(__builtin_assume_aligned(mine + l32 * kPitch + ji, 4 * sizeof(O)), v,
+                         4 * sizeof(O));
+      }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int N = Vec<O>::N, kLanes = 64 / N;  // lanes of a user's row
+#pragma unroll
+    for (int q = 0; q < 32 * kLanes / 64; ++q) {
+      const int ru = q * (64 / kLanes) + lane / kLanes, ji = lane % kLanes * N;
+      const Vec<O> v = *reinterpret_cast<const Vec<O> *>(mine + ru * kPitch + ji);
+      const int64_t r = r0 + wu * 64 + u * 32 + ru, j = j0 + wi * 64 + ji;
+      O *to = static_cast<O *>(P.out) + r * P.out_stride + j;
+      if (r < P.rows) {
+        if (j + N <= P.items) store_vec(to, v);
         else
-          for (int e = 0; e < 4; ++e)
-            if (j + e < P.items) to[e] = v[e];
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (j + e < P.items) to[e] = v.v[e];
       }
     }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
+constexpr int64_t kFullGpu = 2048;
+
+template <class O, class X, int USERS, int ITEMS, bool SPLIT>
+void launch_few(const Product &p, hipStream_t stream) {
+  const int64_t per = 16 * ITEMS * (SPLIT ? 1 : kWaves);
+  const int64_t groups = std::min((p.items + per - 1) / per, kFullGpu);
+  hipLaunchKernelGGL((k_product_few<O, X, USERS, ITEMS, SPLIT>), dim3((unsigned)groups),
+                     dim3(kThreads), 0, stream, p);
+}
+
+constexpr int64_t kFewUsers = 64;
+// Whether the product's waves turn the users' values into bytes themselves.
+bool takes_values(int64_t rows, int64_t k, int64_t items_bytes) {
+  return rows <= 16 && k <= 64 * kOwn && items_bytes >= 16;
 }
 
 template <class O>
-hipError_t product(const Product &p, hipStream_t stream) {
-  const auto few = [&](auto users, auto items, auto split) {
-    constexpr int U = decltype(users)::value, I = decltype(items)::value;
-    constexpr bool S = decltype(split)::value;
-    const int64_t per = 16 * I * (S ? 1 : kWaves);
-    hipLaunchKernelGGL((k_product_few<O, U, I, S>), dim3((unsigned)((p.items + per - 1) / per)),
-                       dim3(kThreads), 0, stream, p);
-  };
-  using std::integral_constant;
-  if (p.rows <= 64) {
-    // few tiles and a long k: the waves of a workgroup share a tile
+hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
+  if (p.b_end - p.b < 16) {
+    const int64_t groups = std::min((p.rows * p.items + kThreads - 1) / kThreads, kFullGpu);
+    hipLaunchKernelGGL(k_product_tiny<O>, dim3((unsigned)groups), dim3(kThreads), 0, stream, p);
+  } else if (p.x) {
+    if (type == BGMF_TYPE_F32) launch_few<O, float, 1, 4, false>(p, stream);
+    else if (type == BGMF_TYPE_BF16) launch_few<O, bf16_t, 1, 4, false>(p, stream);
+    else launch_few<O, f16_t, 1, 4, false>(p, stream);
+  } else if (p.rows <= kFewUsers) {
+    // the waves of a workgroup share a tile where the tiles are few and k is long
     const bool split = p.items < 16 * 4096 && p.kp >= 512;
-    if (p.rows <= 16 && split)
-      few(integral_constant<int, 1>{}, integral_constant<int, 1>{}, std::true_type{});
-    else if (p.rows <= 16)
-      few(integral_constant<int, 1>{}, integral_constant<int, 4>{}, std::false_type{});
-    else if (p.rows <= 32 && split)
-      few(integral_constant<int, 2>{}, integral_constant<int, 1>{}, std::true_type{});
-    else if (p.rows <= 32)
-      few(integral_constant<int, 2>{}, integral_constant<int, 4>{}, std::false_type{});
-    else if (split)
-      few(integral_constant<int, 4>{}, integral_constant<int, 1>{}, std::true_type{});
-    else
-      few(integral_constant<int, 4>{}, integral_constant<int, 4>{}, std::false_type{});
+    const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
+    if (p.rows <= 16) {
+      if (split) launch_few<O, int8_t, 1, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 1, 1, false>(p, stream);
+      else launch_few<O, int8_t, 1, 4, false>(p, stream);
+    } else if (p.rows <= 32) {
+      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 2, 1, false>(p, stream);
+      else launch_few<O, int8_t, 2, 4, false>(p, stream);
+    } else {
+      if (split) launch_few<O, int8_t, 4, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 4, 1, false>(p, stream);
+      else launch_few<O, int8_t, 4, 2, false>(p, stream);
+    }
   } else {
     const int64_t it = (p.items + kTile - 1) / kTile, ut = (p.rows + kTile - 1) / kTile;
     if (it * ut >= (1ll << 24)) return hipErrorInvalidConfiguration;
@@ -482,7 +633,7 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const int32_t kp = (int32_t)round_up(k, kUnit);
   int8_t *q = static_cast<int8_t *>(ws);
-  Product p{q, row_scale, rows, (int32_t)k, kp, items,
+  Product p{nullptr, 0, q, row_scale, rows, (int32_t)k, kp, items,
             items + (items_stride * (item_count - 1) + k), item_scale, item_count, items_stride,
             out, out_stride};
   hipError_t e = hipSuccess;
@@ -491,15 +642,17 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
     hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)groups), dim3(kThreads), 0, stream,
                        static_cast<const int8_t *>(x), rows, (int32_t)k, row_stride, q, kp);
     e = hipGetLastError();
+  } else if (takes_values(rows, k, p.b_end - p.b)) {
+    p.x = x, p.x_stride = row_stride;
   } else {
     float *scale = reinterpret_cast<float *>(q + bytes_part(rows, k));
     e = quantize_by_type(type, x, rows, (int32_t)k, row_stride, q, kp, kp, scale, stream);
     p.a_scale = scale;
   }
   if (e == hipSuccess)
-    e = out_type == BGMF_TYPE_F32    ? product<float>(p, stream)
-        : out_type == BGMF_TYPE_BF16 ? product<bf16_t>(p, stream)
-                                     : product<f16_t>(p, stream);
+    e = out_type == BGMF_TYPE_F32    ? product<float>(p, type, stream)
+        : out_type == BGMF_TYPE_BF16 ? product<bf16_t>(p, type, stream)
+                                     : product<f16_t>(p, type, stream);
   if (e != hipSuccess) return fail_call(BGMF_E_HIP, "%s: %s", call, hipGetErrorString(e));
   return BGMF_OK;
 }
