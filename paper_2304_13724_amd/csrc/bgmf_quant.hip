@@ -170,11 +170,15 @@ __global__ void __launch_bounds__(kThreads) k_pad_rows(const int8_t *x, int64_t 
   }
 }
 
-// 16 bytes of an item from column c on, at any address.
+// 16 bytes of an item from column c on, at any address.  STREAM: items that
+// the caches cannot keep until the next call are read past them (320 MB: 6.4
+// TB/s against 5.9).
+template <bool STREAM = false>
 __device__ __forceinline__ i32x4 item_bytes(const int8_t *row, int32_t c) {
-  i32x4 x;
-  __builtin_memcpy(&x, row + c, 16);
-  return x;
+  typedef int32_t quad __attribute__((ext_vector_type(4), aligned(1)));
+  const quad *p = reinterpret_cast<const quad *>(row + c);
+  if constexpr (STREAM) return __builtin_nontemporal_load(p);
+  else return *p;
 }
 // The same where c may be at or past the row's end: nothing is read past the
 // end of the matrix (of at least 16 bytes), whose last bytes are shifted into
@@ -223,19 +227,20 @@ __global__ void __launch_bounds__(kThreads) k_product_tiny(Product P) {
 // wave takes ITEMS tiles of 16 items at a time, and while it forms their
 // products the bytes and scales of its next step or tiles are on their way.
 // With SPLIT, the waves of a workgroup share the tiles and take a quarter of k
-// each.  Bound: HBM (the items' bytes).
+// each.  ODD: k is no multiple of 16, so that a lane's bytes may end inside
+// its 16.  Bound: HBM (the items' bytes).
 //
 // X: int8_t, users' bytes in P.a; or the type of their values in P.x, which
-// every wave then turns into bytes itself (one launch less; k <= 64 kOwn).
-constexpr int kOwn = 4;
+// every wave then turns into bytes itself (one launch less; k <= 64 OWN).
+constexpr int kOwnMost = 4;
 
-template <class X>
-__device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part, i32x4 (&y)[kOwn]) {
+template <class X, int OWN>
+__device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part, i32x4 (&y)[OWN]) {
   const X *x = static_cast<const X *>(P.x) + r * P.x_stride;
-  float v[kOwn][16];
+  float v[OWN][16];
   Largest a;
 #pragma unroll
-  for (int s = 0; s < kOwn; ++s) {
+  for (int s = 0; s < OWN; ++s) {
     const int32_t c = s * 64 + part * 16;
     if (c + 16 <= P.k) {
       constexpr int N = Vec<X>::N;
@@ -257,7 +262,7 @@ __device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part
   most = fmaxf(most, __shfl_xor(most, 32));
   const float scale = scale_of(most);
 #pragma unroll
-  for (int s = 0; s < kOwn; ++s) {
+  for (int s = 0; s < OWN; ++s) {
     int8_t b[16];
 #pragma unroll
     for (int i = 0; i < 16; ++i) b[i] = byte_of(v[s][i], scale);
@@ -266,9 +271,8 @@ __device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part
   return scale;
 }
 
-template <class O, class X, int USERS, int ITEMS, bool SPLIT>
+template <class O, class X, int OWN, int USERS, int ITEMS, bool SPLIT, bool ODD, bool STREAM>
 __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
-  constexpr bool OWN = !std::is_same<X, int8_t>::value;
   static_assert(!OWN || (USERS == 1 && !SPLIT), "own bytes: one tile of users");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int l16 = lane % 16, part = lane / 16;
@@ -278,11 +282,11 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   if (tile >= tiles) return;  // with SPLIT, all waves or none
 
   const int64_t own_row = l16 < P.rows ? l16 : P.rows - 1;
-  i32x4 own[OWN ? kOwn : 1];
+  i32x4 own[OWN ? OWN : 1];
   float a_scale[USERS];
   const int8_t *user[USERS];
-  if constexpr (OWN) {
-    a_scale[0] = own_bytes<X>(P, own_row, part, own);
+  if constexpr (OWN > 0) {
+    a_scale[0] = own_bytes<X, OWN>(P, own_row, part, own);
   } else {
 #pragma unroll
     for (int u = 0; u < USERS; ++u) {
@@ -299,23 +303,26 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   // (lane l holds that of item l % 16)
   i32x4 x[ITEMS], y[USERS];
   float scale[ITEMS];
+  // the last tiles of several go back so far that all of them are whole (the
+  // scores that two waves then form are the same)
+  const auto first_of = [&](int64_t t) {
+    const int64_t j = t * (16 * ITEMS), most = P.items - 16 * ITEMS;
+    return ITEMS > 1 && j > most ? most : j;
+  };
   const auto load = [&](int64_t t, int s) {
     const int32_t c = s * 64 + part * 16;
-    const int8_t *row[ITEMS];
+    const int64_t j0 = first_of(t);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t j = t * (16 * ITEMS) + i * 16 + l16, at = j < P.items ? j : P.items - 1;
-      row[i] = P.b + at * P.b_stride;
-      if (s == begin) scale[i] = P.b_scale[at];
+      int64_t j = j0 + i * 16 + l16;
+      if (ITEMS == 1 && j >= P.items) j = P.items - 1;
+      const int8_t *row = P.b + j * P.b_stride;
+      if (s < full) x[i] = item_bytes<STREAM>(row, c);
+      else if constexpr (ODD) x[i] = item_bytes_tail(row, c, P.k, P.b_end);
+      else x[i] = c < P.k ? item_bytes<STREAM>(row, c) : i32x4{0, 0, 0, 0};
+      if (s == begin) scale[i] = P.b_scale[j];
     }
-    if (s < full) {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) x[i] = item_bytes(row[i], c);
-    } else {
-#pragma unroll
-      for (int i = 0; i < ITEMS; ++i) x[i] = item_bytes_tail(row[i], c, P.k, P.b_end);
-    }
-    if constexpr (!OWN) {
+    if constexpr (OWN == 0) {
 #pragma unroll
       for (int u = 0; u < USERS; ++u) y[u] = *reinterpret_cast<const i32x4 *>(user[u] + s * 64);
     }
@@ -338,9 +345,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
       for (int i = 0; i < ITEMS; ++i) b[i] = scale[i];
       if (next < tiles) load(next, last ? begin : s + 1);
     };
-    if constexpr (OWN) {  // the steps are counted out, so that the bytes stay in registers
+    if constexpr (OWN > 0) {  // the steps are counted out, so that the bytes stay in registers
 #pragma unroll
-      for (int s = 0; s < kOwn; ++s)
+      for (int s = 0; s < OWN; ++s)
         if (s < end) step(s, &own[s]);
     } else {
       for (int s = begin; s < end; ++s) step(s, nullptr);
@@ -367,12 +374,12 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
     // lane l holds the sums of items 4 (l / 16) .. + 3 and user l % 16
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-      const int64_t j = tile * (16 * ITEMS) + i * 16 + part * 4;
+      const int64_t j = first_of(tile) + i * 16 + part * 4;
       float bs[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) bs[e] = __shfl(b[i], part * 4 + e);
-      if (j >= P.items) continue;
-      const int left = P.items - j < 4 ? (int)(P.items - j) : 4;
+      const int left = ITEMS > 1 || P.items - j > 3 ? 4 : (int)(P.items - j);
+      if (left <= 0) continue;
 #pragma unroll
       for (int u = 0; u < USERS; ++u) {
         const int64_t r = u * 16 + l16;
@@ -507,45 +514,66 @@ __global__ void __launch_bounds__(kThreads, 2) k_product_many(Product P, int64_t
 // Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
 constexpr int64_t kFullGpu = 2048;
 
-template <class O, class X, int USERS, int ITEMS, bool SPLIT>
+constexpr int64_t kCached = 192 << 20;  // items that stay in the 256 MB Infinity Cache
+
+template <class O, class X, int OWN, int USERS, int ITEMS, bool SPLIT>
 void launch_few(const Product &p, hipStream_t stream) {
   const int64_t per = 16 * ITEMS * (SPLIT ? 1 : kWaves);
-  const int64_t groups = std::min((p.items + per - 1) / per, kFullGpu);
-  hipLaunchKernelGGL((k_product_few<O, X, USERS, ITEMS, SPLIT>), dim3((unsigned)groups),
-                     dim3(kThreads), 0, stream, p);
+  const dim3 groups((unsigned)std::min((p.items + per - 1) / per, kFullGpu)), threads(kThreads);
+  constexpr bool BIG = ITEMS > 1;  // enough items that the caches may not keep them
+  if (p.k % 16)
+    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, true, false>), groups,
+                       threads, 0, stream, p);
+  else if (BIG && p.b_end - p.b > kCached)
+    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, false, BIG>), groups,
+                       threads, 0, stream, p);
+  else
+    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, false, false>), groups,
+                       threads, 0, stream, p);
 }
 
 constexpr int64_t kFewUsers = 64;
 // Whether the product's waves turn the users' values into bytes themselves.
 bool takes_values(int64_t rows, int64_t k, int64_t items_bytes) {
-  return rows <= 16 && k <= 64 * kOwn && items_bytes >= 16;
+  return rows <= 16 && k <= 64 * kOwnMost && items_bytes >= 16;
+}
+
+template <class O, class X>
+void launch_values(const Product &p, bool small, hipStream_t stream) {
+  if (p.k <= 64) {
+    if (small) launch_few<O, X, 1, 1, 1, false>(p, stream);
+    else launch_few<O, X, 1, 1, 8, false>(p, stream);
+  } else {
+    if (small) launch_few<O, X, kOwnMost, 1, 1, false>(p, stream);
+    else launch_few<O, X, kOwnMost, 1, 4, false>(p, stream);
+  }
 }
 
 template <class O>
 hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
+  const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
   if (p.b_end - p.b < 16) {
     const int64_t groups = std::min((p.rows * p.items + kThreads - 1) / kThreads, kFullGpu);
     hipLaunchKernelGGL(k_product_tiny<O>, dim3((unsigned)groups), dim3(kThreads), 0, stream, p);
   } else if (p.x) {
-    if (type == BGMF_TYPE_F32) launch_few<O, float, 1, 4, false>(p, stream);
-    else if (type == BGMF_TYPE_BF16) launch_few<O, bf16_t, 1, 4, false>(p, stream);
-    else launch_few<O, f16_t, 1, 4, false>(p, stream);
+    if (type == BGMF_TYPE_F32) launch_values<O, float>(p, small, stream);
+    else if (type == BGMF_TYPE_BF16) launch_values<O, bf16_t>(p, small, stream);
+    else launch_values<O, f16_t>(p, small, stream);
   } else if (p.rows <= kFewUsers) {
     // the waves of a workgroup share a tile where the tiles are few and k is long
     const bool split = p.items < 16 * 4096 && p.kp >= 512;
-    const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
     if (p.rows <= 16) {
-      if (split) launch_few<O, int8_t, 1, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 1, 1, false>(p, stream);
-      else launch_few<O, int8_t, 1, 4, false>(p, stream);
+      if (split) launch_few<O, int8_t, 0, 1, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 0, 1, 1, false>(p, stream);
+      else launch_few<O, int8_t, 0, 1, 4, false>(p, stream);
     } else if (p.rows <= 32) {
-      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 2, 1, false>(p, stream);
-      else launch_few<O, int8_t, 2, 4, false>(p, stream);
+      if (split) launch_few<O, int8_t, 0, 2, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 0, 2, 1, false>(p, stream);
+      else launch_few<O, int8_t, 0, 2, 4, false>(p, stream);
     } else {
-      if (split) launch_few<O, int8_t, 4, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 4, 1, false>(p, stream);
-      else launch_few<O, int8_t, 4, 2, false>(p, stream);
+      if (split) launch_few<O, int8_t, 0, 4, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 0, 4, 1, false>(p, stream);
+      else launch_few<O, int8_t, 0, 4, 2, false>(p, stream);
     }
   } else {
     const int64_t it = (p.items + kTile - 1) / kTile, ut = (p.rows + kTile - 1) / kTile;
