@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) k_product_tiny(Product P) {
   }
 }
 
-// Few users (rows <= 16 USERS): every item's bytes go from global memory into
+// Few users (16 USERS for each blockIdx.y): every item's bytes go from global memory into
 // a matrix instruction once (v_mfma_i32_16x16x64_i8: 16 items x 16 users, 64
 // columns of k; lane l holds 16 bytes of item l % 16 and of user l % 16).  A
 // wave takes ITEMS tiles of 16 items at a time, and while it forms their
@@ -231,48 +231,44 @@ __global__ void __launch_bounds__(kThreads) k_product_tiny(Product P) {
 // its 16.  Bound: HBM (the items' bytes).
 //
 // X: int8_t, users' bytes in P.a; or the type of their values in P.x, which
-// every wave then turns into bytes itself (one launch less; k <= 64 OWN).
-constexpr int kOwnMost = 4;
+// every wave then turns into bytes itself (k <= 64: one launch less, 16
+// quotients a lane; with four times as many the waves spend more on them than
+// the launch costs: 16 x 100,003 x 200 23 us, 15 with 32 users and a launch).
 
-template <class X, int OWN>
-__device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part, i32x4 (&y)[OWN]) {
+template <class X>
+__device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part, i32x4 &y) {
   const X *x = static_cast<const X *>(P.x) + r * P.x_stride;
-  float v[OWN][16];
+  float v[16];
   Largest a;
+  const int32_t c = part * 16;
+  if (c + 16 <= P.k) {
+    constexpr int N = Vec<X>::N;
 #pragma unroll
-  for (int s = 0; s < OWN; ++s) {
-    const int32_t c = s * 64 + part * 16;
-    if (c + 16 <= P.k) {
-      constexpr int N = Vec<X>::N;
+    for (int h = 0; h < 16 / N; ++h) {
+      const Vec<X> w = load_vec(x + c + h * N);
 #pragma unroll
-      for (int h = 0; h < 16 / N; ++h) {
-        const Vec<X> w = load_vec(x + c + h * N);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[s][h * N + i] = to_float(w.v[i]);
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) v[s][i] = c + i < P.k ? to_float(x[c + i]) : 0.0f;
+      for (int i = 0; i < N; ++i) v[h * N + i] = to_float(w.v[i]);
     }
+  } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) a.look(v[s][i]);
+    for (int i = 0; i < 16; ++i) v[i] = c + i < P.k ? to_float(x[c + i]) : 0.0f;
   }
+#pragma unroll
+  for (int i = 0; i < 16; ++i) a.look(v[i]);
   float most = a.get();
   most = fmaxf(most, __shfl_xor(most, 16));
   most = fmaxf(most, __shfl_xor(most, 32));
   const float scale = scale_of(most);
+  int8_t b[16];
 #pragma unroll
-  for (int s = 0; s < OWN; ++s) {
-    int8_t b[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) b[i] = byte_of(v[s][i], scale);
-    __builtin_memcpy(&y[s], b, 16);
-  }
+  for (int i = 0; i < 16; ++i) b[i] = byte_of(v[i], scale);
+  __builtin_memcpy(&y, b, 16);
   return scale;
 }
 
-template <class O, class X, int OWN, int USERS, int ITEMS, bool SPLIT, bool ODD, bool STREAM>
+template <class O, class X, int USERS, int ITEMS, bool SPLIT, bool ODD, bool STREAM>
 __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
+  constexpr bool OWN = !std::is_same<X, int8_t>::value;
   static_assert(!OWN || (USERS == 1 && !SPLIT), "own bytes: one tile of users");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int l16 = lane % 16, part = lane / 16;
@@ -281,16 +277,17 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   const int64_t stride = SPLIT ? gridDim.x : (int64_t)gridDim.x * kWaves;
   if (tile >= tiles) return;  // with SPLIT, all waves or none
 
+  const int64_t r0 = (int64_t)blockIdx.y * (16 * USERS);
   const int64_t own_row = l16 < P.rows ? l16 : P.rows - 1;
-  i32x4 own[OWN ? OWN : 1];
+  i32x4 own;
   float a_scale[USERS];
   const int8_t *user[USERS];
-  if constexpr (OWN > 0) {
-    a_scale[0] = own_bytes<X, OWN>(P, own_row, part, own);
+  if constexpr (OWN) {
+    a_scale[0] = own_bytes<X>(P, own_row, part, own);
   } else {
 #pragma unroll
     for (int u = 0; u < USERS; ++u) {
-      const int64_t r = u * 16 + l16 < P.rows ? u * 16 + l16 : P.rows - 1;
+      const int64_t j = r0 + u * 16 + l16, r = j < P.rows ? j : P.rows - 1;
       a_scale[u] = P.a_scale[r];
       user[u] = P.a + r * P.kp + part * 16;
     }
@@ -299,9 +296,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   const int begin = SPLIT ? steps * wave / kWaves : 0;
   const int end = SPLIT ? steps * (wave + 1) / kWaves : steps;
 
-  // on its way: the bytes of the next step, and the scales of the next tiles
-  // (lane l holds that of item l % 16)
-  i32x4 x[ITEMS], y[USERS];
+  // on its way: the bytes of the next AHEAD steps, and the scales of the next
+  // tiles (lane l holds that of item l % 16)
+  constexpr int AHEAD = ITEMS > 1 || OWN ? 1 : USERS > 2 ? 2 : 4;
+  i32x4 x[AHEAD][ITEMS], y[AHEAD][USERS];
   float scale[ITEMS];
   // the last tiles of several go back so far that all of them are whole (the
   // scores that two waves then form are the same)
@@ -309,48 +307,56 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
     const int64_t j = t * (16 * ITEMS), most = P.items - 16 * ITEMS;
     return ITEMS > 1 && j > most ? most : j;
   };
-  const auto load = [&](int64_t t, int s) {
-    const int32_t c = s * 64 + part * 16;
+  const auto load = [&](int64_t t, int s0) {
     const int64_t j0 = first_of(t);
+    const int8_t *row[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
       int64_t j = j0 + i * 16 + l16;
       if (ITEMS == 1 && j >= P.items) j = P.items - 1;
-      const int8_t *row = P.b + j * P.b_stride;
-      if (s < full) x[i] = item_bytes<STREAM>(row, c);
-      else if constexpr (ODD) x[i] = item_bytes_tail(row, c, P.k, P.b_end);
-      else x[i] = c < P.k ? item_bytes<STREAM>(row, c) : i32x4{0, 0, 0, 0};
-      if (s == begin) scale[i] = P.b_scale[j];
+      row[i] = P.b + j * P.b_stride;
+      if (s0 == begin) scale[i] = P.b_scale[j];
     }
-    if constexpr (OWN == 0) {
 #pragma unroll
-      for (int u = 0; u < USERS; ++u) y[u] = *reinterpret_cast<const i32x4 *>(user[u] + s * 64);
+    for (int p = 0; p < AHEAD; ++p) {
+      const int s = s0 + p;
+      const int32_t c = s * 64 + part * 16;
+      if (s < full && s < end) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) x[p][i] = item_bytes<STREAM>(row[i], c);
+      } else {  // the end of k, and steps past it
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+          if constexpr (ODD) x[p][i] = item_bytes_tail(row[i], c, s < end ? P.k : 0, P.b_end);
+          else x[p][i] = s < end && c < P.k ? item_bytes<STREAM>(row[i], c) : i32x4{0, 0, 0, 0};
+        }
+      }
+      if constexpr (!OWN) {
+#pragma unroll
+        for (int u = 0; u < USERS; ++u)
+          y[p][u] = *reinterpret_cast<const i32x4 *>(user[u] + (s < end ? s : s0) * 64);
+      }
     }
   };
   load(tile, begin);
   for (; tile < tiles; tile += stride) {
     i32x4 acc[ITEMS][USERS] = {};
     float b[ITEMS];
-    const auto step = [&](int s, const i32x4 *mine) {
+    for (int s0 = begin; s0 < end; s0 += AHEAD) {
 #pragma unroll
-      for (int i = 0; i < ITEMS; ++i)
+      for (int p = 0; p < AHEAD; ++p)
 #pragma unroll
-        for (int u = 0; u < USERS; ++u) {
-          const i32x4 other = OWN ? *mine : y[u];
-          acc[i][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[i], other, acc[i][u], 0, 0, 0);
-        }
-      const bool last = s + 1 == end;
+        for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+          for (int u = 0; u < USERS; ++u) {
+            const i32x4 other = OWN ? own : y[p][u];
+            acc[i][u] = __builtin_amdgcn_mfma_i32_16x16x64_i8(x[p][i], other, acc[i][u], 0, 0, 0);
+          }
+      const bool last = s0 + AHEAD >= end;
       const int64_t next = last ? tile + stride : tile;
 #pragma unroll
       for (int i = 0; i < ITEMS; ++i) b[i] = scale[i];
-      if (next < tiles) load(next, last ? begin : s + 1);
-    };
-    if constexpr (OWN > 0) {  // the steps are counted out, so that the bytes stay in registers
-#pragma unroll
-      for (int s = 0; s < OWN; ++s)
-        if (s < end) step(s, &own[s]);
-    } else {
-      for (int s = begin; s < end; ++s) step(s, nullptr);
+      if (next < tiles) load(next, last ? begin : s0 + AHEAD);
     }
 
     if constexpr (SPLIT) {
@@ -382,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
       if (left <= 0) continue;
 #pragma unroll
       for (int u = 0; u < USERS; ++u) {
-        const int64_t r = u * 16 + l16;
+        const int64_t r = r0 + u * 16 + l16;
         if (r >= P.rows) continue;
         O v[4];
 #pragma unroll
@@ -398,117 +404,247 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   }
 }
 
-// Many users: a workgroup of 2 x 2 waves takes a tile of kTile items x kTile
-// users, each wave 64 x 64 of it in v_mfma_i32_32x32x32_i8 (lane l holds 16
-// bytes of item or user l % 32).  64 columns of k at a time pass through LDS,
-// in 16-byte chunks whose place in a row is swizzled so that eight lanes
-// reading eight rows meet all banks.  While a step's products are formed the
-// next step's bytes are loaded into registers.
-constexpr int kTile = 128;
-constexpr int kStep = 64;  // bytes of k per step, 4 chunks
+// Many users: a workgroup of 2 x 2 waves takes tiles of 64 B items x 64 B
+// users, each wave a quarter of it in B x B blocks of v_mfma_i32_32x32x32_i8
+// (lane l holds 16 bytes of item or user l % 32).  STEP bytes of k at a time
+// pass through LDS, in 16-byte chunks whose place in a row is swizzled so that
+// eight lanes that read eight rows meet all banks.  items >= 64 B; the users'
+// bytes are allocated up to a multiple of kUserPad rows.
+constexpr int64_t kUserPad = 256;
 
-__device__ __forceinline__ int lds_chunk(int row, int c) {
-  return row * 4 + (c ^ ((row >> 1) & 3));
-}
+template <class O, int B, int STEP>
+struct Many {
+  static constexpr int kSide = 64 * B, kChunks = STEP / 16;
+  static constexpr int kPass = kThreads / kChunks;  // rows that the workgroup loads at a time
+  static constexpr int kLoads = kSide / kPass;      // 16-byte loads of a thread, each side
+  static constexpr int kBuffer = 2 * kSide * kChunks;  // i32x4 of a step
+  static constexpr int kPitch = 32 * B + 16 / (int)sizeof(O);  // of the scores on their way out
+  static constexpr int kScores = kWaves * 32 * kPitch * (int)sizeof(O) / 16;  // i32x4
+  static constexpr int kScales = 2 * kSide * 4 / 16;
 
-template <class O>
-__global__ void __launch_bounds__(kThreads, 2) k_product_many(Product P, int64_t item_tiles,
-                                                              int64_t user_tiles) {
-  // a step's bytes, and afterwards the scores on their way out
-  constexpr int kStage = 2 * kTile * kStep, kScores = kWaves * 32 * (64 * (int)sizeof(O) + 16);
-  __shared__ i32x4 lds[(kStage > kScores ? kStage : kScores) / 16];
-  i32x4 *lds_items = lds, *lds_users = lds + kTile * kStep / 16;
-  __shared__ float s_item[kTile], s_user[kTile];
-  const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-  const int wi = wave % 2, wu = wave / 2, l32 = lane % 32, half = lane / 32;
-  const int64_t tile = blockIdx.x;
-  const int64_t j0 = tile % item_tiles * kTile, r0 = tile / item_tiles * kTile;
-  // staging: thread t moves chunk t % 4 of rows t / 4 and t / 4 + 64
-  const int chunk = tid % 4, row = tid / 4;
-  const int8_t *item[2], *user[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int64_t j = j0 + row + 64 * h, r = r0 + row + 64 * h;
-    item[h] = P.b + (j < P.items ? j : P.items - 1) * P.b_stride;
-    user[h] = P.a + (r < P.rows ? r : P.rows - 1) * P.kp + chunk * 16;
+  static __device__ __forceinline__ int at(int row, int c) {
+    if constexpr (STEP == 64) return row * 4 + (c ^ ((row >> 1) & 3));
+    else return row * 8 + (c ^ (row & 7));
   }
-  if (tid < kTile) s_item[tid] = j0 + tid < P.items ? P.b_scale[j0 + tid] : 0.0f;
-  else s_user[tid - kTile] = r0 + tid - kTile < P.rows ? P.a_scale[r0 + tid - kTile] : 0.0f;
-  i32x16 acc[2][2] = {};
-  const int steps = P.kp / kStep, full = P.k / kStep;
-  i32x4 x[2], y[2];
-  const auto load = [&](int s) {
+
+  // Tile t in the order in which workgroups take them: these go to the eight
+  // XCDs in turn, and each XCD gets a part of the tiles of its own, four users'
+  // tiles by one items' after another, so that its L2 serves many of them.  The
+  // last items' tile goes back so far that it is whole.
+  static __device__ __forceinline__ void place(const Product &P, int64_t t, int64_t &j0,
+                                               int64_t &r0) {
+    const int64_t item_tiles = (P.items + kSide - 1) / kSide;
+    const int64_t user_tiles = (P.rows + kSide - 1) / kSide, tiles = item_tiles * user_tiles;
+    const int64_t xcd = t % 8, per = tiles / 8, more = tiles % 8;
+    const int64_t i = xcd * per + (xcd < more ? xcd : more) + t / 8;
+    constexpr int64_t kGroup = 4;
+    const int64_t group = i / (kGroup * item_tiles), in = i % (kGroup * item_tiles);
+    const int64_t left = user_tiles - group * kGroup, size = left < kGroup ? left : kGroup;
+    j0 = in / size * kSide;
+    if (j0 > P.items - kSide) j0 = P.items - kSide;
+    r0 = (group * kGroup + in % size) * kSide;
+  }
+
+  // A thread's 16-byte chunks of step s of the tile at (j0, r0).
+  template <bool ODD>
+  static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
+                                              i32x4 (&x)[kLoads], i32x4 (&y)[kLoads]) {
+    const int row = threadIdx.x / kChunks;
+    const int32_t c = s * STEP + threadIdx.x % kChunks * 16;
+    const int8_t *b = P.b + (j0 + row) * P.b_stride;
+    const int8_t *a = P.a + (r0 + row) * P.kp + c;
+    if ((s + 1) * STEP <= P.k) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      x[h] = s < full ? item_bytes(item[h], s * kStep + chunk * 16)
-                      : item_bytes_tail(item[h], s * kStep + chunk * 16, P.k, P.b_end);
-      y[h] = *reinterpret_cast<const i32x4 *>(user[h] + s * kStep);
-    }
-  };
-  load(0);
-  for (int s = 0; s < steps; ++s) {
-    __syncthreads();
+      for (int h = 0; h < kLoads; ++h) x[h] = item_bytes(b + h * kPass * P.b_stride, c);
+    } else {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      lds_items[lds_chunk(row + 64 * h, chunk)] = x[h];
-      lds_users[lds_chunk(row + 64 * h, chunk)] = y[h];
-    }
-    __syncthreads();
-    if (s + 1 < steps) load(s + 1);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      i32x4 fi[2], fu[2];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        fi[h] = lds_items[lds_chunk(wi * 64 + h * 32 + l32, c * 2 + half)];
-        fu[h] = lds_users[lds_chunk(wu * 64 + h * 32 + l32, c * 2 + half)];
+      for (int h = 0; h < kLoads; ++h) {
+        if constexpr (ODD) x[h] = item_bytes_tail(b + h * kPass * P.b_stride, c, P.k, P.b_end);
+        else x[h] = c < P.k ? item_bytes(b + h * kPass * P.b_stride, c) : i32x4{0, 0, 0, 0};
       }
+    }
+    if (STEP <= kUnit || c < P.kp) {
+#pragma unroll
+      for (int h = 0; h < kLoads; ++h)
+        y[h] = *reinterpret_cast<const i32x4 *>(a + (int64_t)h * kPass * P.kp);
+    }
+  }
+  static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kLoads],
+                                               const i32x4 (&y)[kLoads]) {
+    const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+#pragma unroll
+    for (int h = 0; h < kLoads; ++h) buffer[at(row + kPass * h, chunk)] = x[h];
+#pragma unroll
+    for (int h = 0; h < kLoads; ++h)
+      buffer[kSide * kChunks + at(row + kPass * h, chunk)] = y[h];
+  }
+  // A wave's bytes of 32 columns of k.
+  static __device__ __forceinline__ void read(const i32x4 *buffer, int sub, i32x4 (&fi)[B],
+                                              i32x4 (&fu)[B]) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int c = sub * 2 + lane / 32;
+#pragma unroll
+    for (int h = 0; h < B; ++h) {
+      fi[h] = buffer[at((wave % 2 * B + h) * 32 + lane % 32, c)];
+      fu[h] = buffer[kSide * kChunks + at((wave / 2 * B + h) * 32 + lane % 32, c)];
+    }
+  }
+  static __device__ __forceinline__ void multiply(i32x16 (&acc)[B][B], const i32x4 (&fi)[B],
+                                                  const i32x4 (&fu)[B]) {
+#pragma unroll
+    for (int i = 0; i < B; ++i)
+#pragma unroll
+      for (int u = 0; u < B; ++u)
+        acc[i][u] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fi[i], fu[u], acc[i][u], 0, 0, 0);
+  }
+  // The scales of the tile's items, then of its users (those past the last
+  // user's are not used).
+  static constexpr int kScaleLoads = 2 * kSide / kThreads;
+  static __device__ __forceinline__ void load_scales(const Product &P, int64_t j0, int64_t r0,
+                                                     float (&scale)[kScaleLoads]) {
+#pragma unroll
+    for (int h = 0; h < kScaleLoads; ++h) {
+      const int i = threadIdx.x + h * kThreads;
+      const int64_t r = r0 + i - kSide;
+      scale[h] = i < kSide ? P.b_scale[j0 + i] : P.a_scale[r < P.rows ? r : P.rows - 1];
+    }
+  }
+
+  // Register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and
+  // user l % 32.  The scores of 32 users at a time pass through LDS (lds: the
+  // whole workgroup's), so that a user's 32 B scores are stored in a row.
+  static __device__ __forceinline__ void store_scores(const Product &P, int64_t j0, int64_t r0,
+                                                      const i32x16 (&acc)[B][B], i32x4 *lds,
+                                                      const float *s_item) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int wi = wave % 2, wu = wave / 2, l32 = lane % 32, half = lane / 32;
+    const float *s_user = s_item + kSide;
+    O *mine = reinterpret_cast<O *>(lds) + wave * (32 * kPitch);
+    constexpr int N = Vec<O>::N, kLanes = 32 * B / N;  // lanes of a user's row
+#pragma unroll
+    for (int u = 0; u < B; ++u) {
+      const float a = s_user[(wu * B + u) * 32 + l32];
+#pragma unroll
+      for (int i = 0; i < B; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int ji = i * 32 + g * 8 + half * 4;
+          O v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[wi * B * 32 + ji + e]);
+          __builtin_memcpy(__builtin_assume_aligned(mine + l32 * kPitch + ji, 4 * sizeof(O)), v,
+                           4 * sizeof(O));
+        }
+      __builtin_amdgcn_wave_barrier();
+      const int64_t r1 = r0 + (wu * B + u) * 32 + lane / kLanes;
+      const int ji = lane % kLanes * N;
+      O *to = static_cast<O *>(P.out) + r1 * P.out_stride + (j0 + wi * B * 32 + ji);
+#pragma unroll
+      for (int q = 0; q < 32 * kLanes / 64; ++q) {
+        const int ru = q * (64 / kLanes);
+        const Vec<O> v =
+            *reinterpret_cast<const Vec<O> *>(mine + (ru + lane / kLanes) * kPitch + ji);
+        if (r1 + ru < P.rows) store_vec(to + ru * P.out_stride, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+};
+
+// Tiles of 128 x 128, 64 bytes of k at a time: four workgroups on a CU overlap
+// their loads, products and stores.  A workgroup's bytes of the next step, or
+// of its next tile, are on their way into registers meanwhile.
+template <class O, bool ODD>
+__global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t tiles) {
+  using M = Many<O, 2, 64>;
+  __shared__ i32x4 lds[M::kBuffer > M::kScores ? M::kBuffer : M::kScores];
+  __shared__ float s_item[2 * M::kSide];
+  const int steps = P.kp / 64;
+  i32x4 x[M::kLoads], y[M::kLoads];
+  float scale[M::kScaleLoads];
+  i32x16 acc[2][2] = {};
+  int64_t tile = blockIdx.x, j0, r0;
+  M::place(P, tile, j0, r0);
+  M::template load<ODD>(P, j0, r0, 0, x, y);
+  M::load_scales(P, j0, r0, scale);
+  for (int s = 0; tile < tiles;) {
+    __syncthreads();
+    M::store(lds, x, y);
+    if (s == 0) s_item[threadIdx.x] = scale[0];
+    __syncthreads();
+    const bool last = s + 1 == steps;
+    int64_t jn = j0, rn = r0;
+    const int64_t next = last ? tile + gridDim.x : tile;
+    if (next < tiles) {
+      if (last) M::place(P, next, jn, rn);
+      M::template load<ODD>(P, jn, rn, last ? 0 : s + 1, x, y);
+      if (last) M::load_scales(P, jn, rn, scale);
+    }
+#pragma unroll
+    for (int sub = 0; sub < 2; ++sub) {
+      i32x4 fi[2], fu[2];
+      M::read(lds, sub, fi, fu);
+      M::multiply(acc, fi, fu);
+    }
+    ++s;
+    if (last) {
+      __syncthreads();
+      M::store_scores(P, j0, r0, acc, lds, s_item);
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-          acc[i][u] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fi[i], fu[u], acc[i][u], 0, 0, 0);
+        for (int u = 0; u < 2; ++u) acc[i][u] = i32x16{};
+      tile = next, j0 = jn, r0 = rn, s = 0;
     }
   }
-  // Register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and
-  // user l % 32.  The scores of 32 users at a time pass through LDS, so that a
-  // user's 64 scores are stored in a row.
-  constexpr int kPitch = 64 + 16 / (int)sizeof(O);  // elements
+}
+
+// Long k: tiles of 256 x 256, 128 bytes of k at a time, which halves the LDS
+// traffic per product (LDS would bound the smaller tile before the matrix units
+// do).  One workgroup fills a CU, so a wave itself reads its next 32 columns
+// from LDS while the matrix unit works, and a step's bytes are loaded a whole
+// step before they go to the other LDS buffer.
+template <class O, bool ODD>
+__global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
+  using M = Many<O, 4, 128>;
+  __shared__ i32x4 lds[2 * M::kBuffer > M::kScores ? 2 * M::kBuffer : M::kScores];
+  __shared__ float s_item[2 * M::kSide];
+  const int steps = (P.k + 127) / 128;
+  int64_t j0, r0;
+  M::place(P, blockIdx.x, j0, r0);
+  i32x4 x[M::kLoads], y[M::kLoads];
+  M::template load<ODD>(P, j0, r0, 0, x, y);
+  {
+    float scale[M::kScaleLoads];
+    M::load_scales(P, j0, r0, scale);
+#pragma unroll
+    for (int h = 0; h < M::kScaleLoads; ++h) s_item[threadIdx.x + h * kThreads] = scale[h];
+  }
+  M::store(lds, x, y);
+  if (steps > 1) M::template load<ODD>(P, j0, r0, 1, x, y);
   __syncthreads();
-  O *mine = reinterpret_cast<O *>(lds) + wave * (32 * kPitch);
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const float a = s_user[wu * 64 + u * 32 + l32];
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int ji = i * 32 + g * 8 + half * 4;
-        O v[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[wi * 64 + ji + e]);
-        __builtin_memcpy(__builtin_assume_aligned(mine + l32 * kPitch + ji, 4 * sizeof(O)), v,
-                         4 * sizeof(O));
-      }
-    __builtin_amdgcn_wave_barrier();
-    constexpr int N = Vec<O>::N, kLanes = 64 / N;  // lanes of a user's row
-#pragma unroll
-    for (int q = 0; q < 32 * kLanes / 64; ++q) {
-      const int ru = q * (64 / kLanes) + lane / kLanes, ji = lane % kLanes * N;
-      const Vec<O> v = *reinterpret_cast<const Vec<O> *>(mine + ru * kPitch + ji);
-      const int64_t r = r0 + wu * 64 + u * 32 + ru, j = j0 + wi * 64 + ji;
-      O *to = static_cast<O *>(P.out) + r * P.out_stride + j;
-      if (r < P.rows) {
-        if (j + N <= P.items) store_vec(to, v);
-        else
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (j + e < P.items) to[e] = v.v[e];
-      }
+  i32x16 acc[4][4] = {};
+  i32x4 fi[2][4], fu[2][4];
+  M::read(lds, 0, fi[0], fu[0]);
+  for (int s = 0; s < steps; ++s) {
+    i32x4 *now = lds + s % 2 * M::kBuffer, *other = lds + (s + 1) % 2 * M::kBuffer;
+    M::read(now, 1, fi[1], fu[1]);
+    M::multiply(acc, fi[0], fu[0]);
+    M::read(now, 2, fi[0], fu[0]);
+    M::multiply(acc, fi[1], fu[1]);
+    M::read(now, 3, fi[1], fu[1]);
+    M::multiply(acc, fi[0], fu[0]);
+    if (s + 1 < steps) {
+      M::store(other, x, y);
+      if (s + 2 < steps) M::template load<ODD>(P, j0, r0, s + 2, x, y);
     }
-    __builtin_amdgcn_wave_barrier();
+    __syncthreads();
+    if (s + 1 < steps) M::read(other, 0, fi[0], fu[0]);
+    M::multiply(acc, fi[1], fu[1]);
   }
+  __syncthreads();
+  M::store_scores(P, j0, r0, acc, lds, s_item);
 }
 
 // Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
@@ -516,37 +652,40 @@ constexpr int64_t kFullGpu = 2048;
 
 constexpr int64_t kCached = 192 << 20;  // items that stay in the 256 MB Infinity Cache
 
-template <class O, class X, int OWN, int USERS, int ITEMS, bool SPLIT>
-void launch_few(const Product &p, hipStream_t stream) {
-  const int64_t per = 16 * ITEMS * (SPLIT ? 1 : kWaves);
-  const dim3 groups((unsigned)std::min((p.items + per - 1) / per, kFullGpu)), threads(kThreads);
+template <class O, class X, int USERS, int ITEMS, bool SPLIT>
+void launch_few(Product p, hipStream_t stream) {
+  const int64_t per = 16 * ITEMS * (SPLIT ? 1 : kWaves), all = (p.items + per - 1) / per;
+  // equally many tiles for each
+  const int64_t rounds = (all + kFullGpu - 1) / kFullGpu, groups = (all + rounds - 1) / rounds;
   constexpr bool BIG = ITEMS > 1;  // enough items that the caches may not keep them
-  if (p.k % 16)
-    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, true, false>), groups,
-                       threads, 0, stream, p);
-  else if (BIG && p.b_end - p.b > kCached)
-    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, false, BIG>), groups,
-                       threads, 0, stream, p);
-  else
-    hipLaunchKernelGGL((k_product_few<O, X, OWN, USERS, ITEMS, SPLIT, false, false>), groups,
-                       threads, 0, stream, p);
+  constexpr int64_t kMost = 65535ll * 16 * USERS;  // users of a launch
+  for (int64_t left = p.rows; left > 0; left -= kMost) {
+    p.rows = std::min(left, kMost);
+    const dim3 grid((unsigned)groups, (unsigned)((p.rows + 16 * USERS - 1) / (16 * USERS)));
+    if (p.k % 16)
+      hipLaunchKernelGGL((k_product_few<O, X, USERS, ITEMS, SPLIT, true, false>), grid,
+                         dim3(kThreads), 0, stream, p);
+    else if (BIG && p.b_end - p.b > kCached)
+      hipLaunchKernelGGL((k_product_few<O, X, USERS, ITEMS, SPLIT, false, BIG>), grid,
+                         dim3(kThreads), 0, stream, p);
+    else
+      hipLaunchKernelGGL((k_product_few<O, X, USERS, ITEMS, SPLIT, false, false>), grid,
+                         dim3(kThreads), 0, stream, p);
+    p.a += kMost * p.kp, p.a_scale += kMost;
+    p.out = static_cast<O *>(p.out) + kMost * p.out_stride;
+  }
 }
 
 constexpr int64_t kFewUsers = 64;
 // Whether the product's waves turn the users' values into bytes themselves.
 bool takes_values(int64_t rows, int64_t k, int64_t items_bytes) {
-  return rows <= 16 && k <= 64 * kOwnMost && items_bytes >= 16;
+  return rows <= 16 && k <= 64 && items_bytes >= 16;
 }
 
 template <class O, class X>
 void launch_values(const Product &p, bool small, hipStream_t stream) {
-  if (p.k <= 64) {
-    if (small) launch_few<O, X, 1, 1, 1, false>(p, stream);
-    else launch_few<O, X, 1, 1, 8, false>(p, stream);
-  } else {
-    if (small) launch_few<O, X, kOwnMost, 1, 1, false>(p, stream);
-    else launch_few<O, X, kOwnMost, 1, 4, false>(p, stream);
-  }
+  if (small) launch_few<O, X, 1, 1, false>(p, stream);
+  else launch_few<O, X, 1, 8, false>(p, stream);
 }
 
 template <class O>
@@ -559,33 +698,44 @@ hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
     if (type == BGMF_TYPE_F32) launch_values<O, float>(p, small, stream);
     else if (type == BGMF_TYPE_BF16) launch_values<O, bf16_t>(p, small, stream);
     else launch_values<O, f16_t>(p, small, stream);
-  } else if (p.rows <= kFewUsers) {
+  } else if (p.rows <= kFewUsers || p.items < 128) {
     // the waves of a workgroup share a tile where the tiles are few and k is long
     const bool split = p.items < 16 * 4096 && p.kp >= 512;
     if (p.rows <= 16) {
-      if (split) launch_few<O, int8_t, 0, 1, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 0, 1, 1, false>(p, stream);
-      else launch_few<O, int8_t, 0, 1, 4, false>(p, stream);
+      if (split) launch_few<O, int8_t, 1, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 1, 1, false>(p, stream);
+      else launch_few<O, int8_t, 1, 4, false>(p, stream);
     } else if (p.rows <= 32) {
-      if (split) launch_few<O, int8_t, 0, 2, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 0, 2, 1, false>(p, stream);
-      else launch_few<O, int8_t, 0, 2, 4, false>(p, stream);
+      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 2, 1, false>(p, stream);
+      else launch_few<O, int8_t, 2, 4, false>(p, stream);
     } else {
-      if (split) launch_few<O, int8_t, 0, 4, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 0, 4, 1, false>(p, stream);
-      else launch_few<O, int8_t, 0, 4, 2, false>(p, stream);
+      if (split) launch_few<O, int8_t, 4, 1, true>(p, stream);
+      else if (small) launch_few<O, int8_t, 4, 1, false>(p, stream);
+      else launch_few<O, int8_t, 4, 2, false>(p, stream);
     }
   } else {
-    const int64_t it = (p.items + kTile - 1) / kTile, ut = (p.rows + kTile - 1) / kTile;
-    if (it * ut >= (1ll << 24)) return hipErrorInvalidConfiguration;
-    hipLaunchKernelGGL(k_product_many<O>, dim3((unsigned)(it * ut)), dim3(kThreads), 0, stream, p,
-                       it, ut);
+    const int64_t large = (p.items + 255) / 256 * ((p.rows + 255) / 256);
+    const int64_t many = (p.items + 127) / 128 * ((p.rows + 127) / 128);
+    const bool odd = p.k % 16;
+    if (p.k >= 512 && large >= 256 && p.items >= 256) {
+      const dim3 groups((unsigned)large), threads(kThreads);
+      if (odd) hipLaunchKernelGGL((k_product_large<O, true>), groups, threads, 0, stream, p);
+      else hipLaunchKernelGGL((k_product_large<O, false>), groups, threads, 0, stream, p);
+    } else {
+      const dim3 groups((unsigned)std::min<int64_t>(many, 1024)), threads(kThreads);
+      if (odd) hipLaunchKernelGGL((k_product_many<O, true>), groups, threads, 0, stream, p, many);
+      else hipLaunchKernelGGL((k_product_many<O, false>), groups, threads, 0, stream, p, many);
+    }
   }
   return hipGetLastError();
 }
 
 // Workspace: the users' bytes in the product's layout, then their scales.
-int64_t bytes_part(int64_t rows, int64_t k) { return round_up(rows * round_up(k, kUnit), 256); }
+int64_t bytes_part(int64_t rows, int64_t k) {
+  if (rows > kFewUsers) rows = round_up(rows, kUserPad);
+  return round_up(rows * round_up(k, kUnit), 256);
+}
 
 }  // namespace
 }  // namespace bgmfk
