@@ -404,23 +404,22 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
   }
 }
 
-// Many users: a workgroup of 2 x 2 waves takes tiles of 64 B items x 64 B
-// users, each wave a quarter of it in B x B blocks of v_mfma_i32_32x32x32_i8
+// Many users: a workgroup of 2 x 2 waves takes tiles of 64 BI items x 64 BU
+// users, each wave a quarter of it in BI x BU blocks of v_mfma_i32_32x32x32_i8
 // (lane l holds 16 bytes of item or user l % 32).  STEP bytes of k at a time
 // pass through LDS, in 16-byte chunks whose place in a row is swizzled so that
-// eight lanes that read eight rows meet all banks.  items >= 64 B; the users'
+// eight lanes that read eight rows meet all banks.  items >= 64 BI; the users'
 // bytes are allocated up to a multiple of kUserPad rows.
 constexpr int64_t kUserPad = 256;
 
-template <class O, int B, int STEP>
+template <class O, int BI, int BU, int STEP>
 struct Many {
-  static constexpr int kSide = 64 * B, kChunks = STEP / 16;
+  static constexpr int kItems = 64 * BI, kUsers = 64 * BU, kChunks = STEP / 16;
   static constexpr int kPass = kThreads / kChunks;  // rows that the workgroup loads at a time
-  static constexpr int kLoads = kSide / kPass;      // 16-byte loads of a thread, each side
-  static constexpr int kBuffer = 2 * kSide * kChunks;  // i32x4 of a step
-  static constexpr int kPitch = 32 * B + 16 / (int)sizeof(O);  // of the scores on their way out
+  static constexpr int kItemLoads = kItems / kPass, kUserLoads = kUsers / kPass;  // of a thread
+  static constexpr int kBuffer = (kItems + kUsers) * kChunks;  // i32x4 of a step
+  static constexpr int kPitch = 32 * BI + 16 / (int)sizeof(O);  // of the scores on their way out
   static constexpr int kScores = kWaves * 32 * kPitch * (int)sizeof(O) / 16;  // i32x4
-  static constexpr int kScales = 2 * kSide * 4 / 16;
 
   static __device__ __forceinline__ int at(int row, int c) {
     if constexpr (STEP == 64) return row * 4 + (c ^ ((row >> 1) & 3));
@@ -433,113 +432,115 @@ struct Many {
   // last items' tile goes back so far that it is whole.
   static __device__ __forceinline__ void place(const Product &P, int64_t t, int64_t &j0,
                                                int64_t &r0) {
-    const int64_t item_tiles = (P.items + kSide - 1) / kSide;
-    const int64_t user_tiles = (P.rows + kSide - 1) / kSide, tiles = item_tiles * user_tiles;
+    const int64_t item_tiles = (P.items + kItems - 1) / kItems;
+    const int64_t user_tiles = (P.rows + kUsers - 1) / kUsers, tiles = item_tiles * user_tiles;
     const int64_t xcd = t % 8, per = tiles / 8, more = tiles % 8;
     const int64_t i = xcd * per + (xcd < more ? xcd : more) + t / 8;
     constexpr int64_t kGroup = 4;
     const int64_t group = i / (kGroup * item_tiles), in = i % (kGroup * item_tiles);
     const int64_t left = user_tiles - group * kGroup, size = left < kGroup ? left : kGroup;
-    j0 = in / size * kSide;
-    if (j0 > P.items - kSide) j0 = P.items - kSide;
-    r0 = (group * kGroup + in % size) * kSide;
+    j0 = in / size * kItems;
+    if (j0 > P.items - kItems) j0 = P.items - kItems;
+    r0 = (group * kGroup + in % size) * kUsers;
   }
 
-  // A thread's 16-byte chunks of step s of the tile at (j0, r0).
-  template <bool ODD>
+  // A thread's 16-byte chunks of step s of the tile at (j0, r0).  FULL: the step
+  // lies within k.
+  template <bool ODD, bool FULL = false>
   static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
-                                              i32x4 (&x)[kLoads], i32x4 (&y)[kLoads]) {
+                                              i32x4 (&x)[kItemLoads],
+                                              i32x4 (&y)[kUserLoads]) {
     const int row = threadIdx.x / kChunks;
     const int32_t c = s * STEP + threadIdx.x % kChunks * 16;
     const int8_t *b = P.b + (j0 + row) * P.b_stride;
     const int8_t *a = P.a + (r0 + row) * P.kp + c;
-    if ((s + 1) * STEP <= P.k) {
+    if (FULL || (s + 1) * STEP <= P.k) {
 #pragma unroll
-      for (int h = 0; h < kLoads; ++h) x[h] = item_bytes(b + h * kPass * P.b_stride, c);
+      for (int h = 0; h < kItemLoads; ++h) x[h] = item_bytes(b + h * kPass * P.b_stride, c);
     } else {
 #pragma unroll
-      for (int h = 0; h < kLoads; ++h) {
+      for (int h = 0; h < kItemLoads; ++h) {
         if constexpr (ODD) x[h] = item_bytes_tail(b + h * kPass * P.b_stride, c, P.k, P.b_end);
         else x[h] = c < P.k ? item_bytes(b + h * kPass * P.b_stride, c) : i32x4{0, 0, 0, 0};
       }
     }
-    if (STEP <= kUnit || c < P.kp) {
+    if (FULL || STEP <= kUnit || c < P.kp) {
 #pragma unroll
-      for (int h = 0; h < kLoads; ++h)
+      for (int h = 0; h < kUserLoads; ++h)
         y[h] = *reinterpret_cast<const i32x4 *>(a + (int64_t)h * kPass * P.kp);
     }
   }
-  static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kLoads],
-                                               const i32x4 (&y)[kLoads]) {
+  static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kItemLoads],
+                                               const i32x4 (&y)[kUserLoads]) {
     const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
 #pragma unroll
-    for (int h = 0; h < kLoads; ++h) buffer[at(row + kPass * h, chunk)] = x[h];
+    for (int h = 0; h < kItemLoads; ++h) buffer[at(row + kPass * h, chunk)] = x[h];
 #pragma unroll
-    for (int h = 0; h < kLoads; ++h)
-      buffer[kSide * kChunks + at(row + kPass * h, chunk)] = y[h];
+    for (int h = 0; h < kUserLoads; ++h)
+      buffer[kItems * kChunks + at(row + kPass * h, chunk)] = y[h];
   }
   // A wave's bytes of 32 columns of k.
-  static __device__ __forceinline__ void read(const i32x4 *buffer, int sub, i32x4 (&fi)[B],
-                                              i32x4 (&fu)[B]) {
+  static __device__ __forceinline__ void read(const i32x4 *buffer, int sub, i32x4 (&fi)[BI],
+                                              i32x4 (&fu)[BU]) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int c = sub * 2 + lane / 32;
 #pragma unroll
-    for (int h = 0; h < B; ++h) {
-      fi[h] = buffer[at((wave % 2 * B + h) * 32 + lane % 32, c)];
-      fu[h] = buffer[kSide * kChunks + at((wave / 2 * B + h) * 32 + lane % 32, c)];
-    }
+    for (int h = 0; h < BI; ++h) fi[h] = buffer[at((wave % 2 * BI + h) * 32 + lane % 32, c)];
+#pragma unroll
+    for (int h = 0; h < BU; ++h)
+      fu[h] = buffer[kItems * kChunks + at((wave / 2 * BU + h) * 32 + lane % 32, c)];
   }
-  static __device__ __forceinline__ void multiply(i32x16 (&acc)[B][B], const i32x4 (&fi)[B],
-                                                  const i32x4 (&fu)[B]) {
+  static __device__ __forceinline__ void multiply(i32x16 (&acc)[BI][BU], const i32x4 (&fi)[BI],
+                                                  const i32x4 (&fu)[BU]) {
 #pragma unroll
-    for (int i = 0; i < B; ++i)
+    for (int i = 0; i < BI; ++i)
 #pragma unroll
-      for (int u = 0; u < B; ++u)
+      for (int u = 0; u < BU; ++u)
         acc[i][u] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fi[i], fu[u], acc[i][u], 0, 0, 0);
   }
   // The scales of the tile's items, then of its users (those past the last
   // user's are not used).
-  static constexpr int kScaleLoads = 2 * kSide / kThreads;
+  static constexpr int kScaleLoads = (kItems + kUsers + kThreads - 1) / kThreads;
   static __device__ __forceinline__ void load_scales(const Product &P, int64_t j0, int64_t r0,
                                                      float (&scale)[kScaleLoads]) {
 #pragma unroll
     for (int h = 0; h < kScaleLoads; ++h) {
       const int i = threadIdx.x + h * kThreads;
-      const int64_t r = r0 + i - kSide;
-      scale[h] = i < kSide ? P.b_scale[j0 + i] : P.a_scale[r < P.rows ? r : P.rows - 1];
+      const int64_t r = r0 + i - kItems;
+      scale[h] = i < kItems ? P.b_scale[j0 + i] : P.a_scale[r < P.rows ? r : P.rows - 1];
     }
   }
 
   // Register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and
   // user l % 32.  The scores of 32 users at a time pass through LDS (lds: the
-  // whole workgroup's), so that a user's 32 B scores are stored in a row.
+  // whole workgroup's), so that a user's 32 BI scores are stored in a row.
   static __device__ __forceinline__ void store_scores(const Product &P, int64_t j0, int64_t r0,
-                                                      const i32x16 (&acc)[B][B], i32x4 *lds,
+                                                      const i32x16 (&acc)[BI][BU], i32x4 *lds,
                                                       const float *s_item) {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wi = wave % 2, wu = wave / 2, l32 = lane % 32, half = lane / 32;
-    const float *s_user = s_item + kSide;
+    const float *s_user = s_item + kItems;
     O *mine = reinterpret_cast<O *>(lds) + wave * (32 * kPitch);
-    constexpr int N = Vec<O>::N, kLanes = 32 * B / N;  // lanes of a user's row
+    constexpr int N = Vec<O>::N, kLanes = 32 * BI / N;  // lanes of a user's row
 #pragma unroll
-    for (int u = 0; u < B; ++u) {
-      const float a = s_user[(wu * B + u) * 32 + l32];
+    for (int u = 0; u < BU; ++u) {
+      const float a = s_user[(wu * BU + u) * 32 + l32];
 #pragma unroll
-      for (int i = 0; i < B; ++i)
+      for (int i = 0; i < BI; ++i)
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int ji = i * 32 + g * 8 + half * 4;
           O v[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[wi * B * 32 + ji + e]);
+            v[e] = score_of<O>(acc[i][u][g * 4 + e], a, s_item[wi * BI * 32 + ji + e]);
           __builtin_memcpy(__builtin_assume_aligned(mine + l32 * kPitch + ji, 4 * sizeof(O)), v,
                            4 * sizeof(O));
         }
       __builtin_amdgcn_wave_barrier();
-      const int64_t r1 = r0 + (wu * B + u) * 32 + lane / kLanes;
+      const int64_t r1 = r0 + (wu * BU + u) * 32 + lane / kLanes;
       const int ji = lane % kLanes * N;
-      O *to = static_cast<O *>(P.out) + r1 * P.out_stride + (j0 + wi * B * 32 + ji);
+      O *to = static_cast<O *>(P.out) + r1 * P.out_stride + (j0 + wi * BI * 32 + ji);
 #pragma unroll
       for (int q = 0; q < 32 * kLanes / 64; ++q) {
         const int ru = q * (64 / kLanes);
@@ -552,18 +553,17 @@ struct Many {
   }
 };
 
-// Tiles of 128 x 128, 64 bytes of k at a time: four workgroups on a CU overlap
-// their loads, products and stores.  A workgroup's bytes of the next step, or
+// Tiles of 128 or 64 items x 128 or 64 users, 64 bytes of k at a time: four workgroups on a CU overlap their loads, products and stores.  A workgroup's bytes of the next step, or
 // of its next tile, are on their way into registers meanwhile.
-template <class O, bool ODD>
+template <class O, int BI, int BU, bool ODD>
 __global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t tiles) {
-  using M = Many<O, 2, 64>;
+  using M = Many<O, BI, BU, 64>;
   __shared__ i32x4 lds[M::kBuffer > M::kScores ? M::kBuffer : M::kScores];
-  __shared__ float s_item[2 * M::kSide];
+  __shared__ float s_item[M::kScaleLoads * kThreads];
   const int steps = P.kp / 64;
-  i32x4 x[M::kLoads], y[M::kLoads];
+  i32x4 x[M::kItemLoads], y[M::kUserLoads];
   float scale[M::kScaleLoads];
-  i32x16 acc[2][2] = {};
+  i32x16 acc[BI][BU] = {};
   int64_t tile = blockIdx.x, j0, r0;
   M::place(P, tile, j0, r0);
   M::template load<ODD>(P, j0, r0, 0, x, y);
@@ -583,7 +583,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t
     }
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
-      i32x4 fi[2], fu[2];
+      i32x4 fi[BI], fu[BU];
       M::read(lds, sub, fi, fu);
       M::multiply(acc, fi, fu);
     }
@@ -592,9 +592,9 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t
       __syncthreads();
       M::store_scores(P, j0, r0, acc, lds, s_item);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int i = 0; i < BI; ++i)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) acc[i][u] = i32x16{};
+        for (int u = 0; u < BU; ++u) acc[i][u] = i32x16{};
       tile = next, j0 = jn, r0 = rn, s = 0;
     }
   }
@@ -605,15 +605,18 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t
 // do).  One workgroup fills a CU, so a wave itself reads its next 32 columns
 // from LDS while the matrix unit works, and a step's bytes are loaded a whole
 // step before they go to the other LDS buffer.
+// Kinds of instructions that the scheduler is told to place.
+constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
+
 template <class O, bool ODD>
 __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
-  using M = Many<O, 4, 128>;
+  using M = Many<O, 4, 4, 128>;
   __shared__ i32x4 lds[2 * M::kBuffer > M::kScores ? 2 * M::kBuffer : M::kScores];
-  __shared__ float s_item[2 * M::kSide];
+  __shared__ float s_item[M::kScaleLoads * kThreads];
   const int steps = (P.k + 127) / 128;
   int64_t j0, r0;
   M::place(P, blockIdx.x, j0, r0);
-  i32x4 x[M::kLoads], y[M::kLoads];
+  i32x4 x[M::kItemLoads], y[M::kUserLoads];
   M::template load<ODD>(P, j0, r0, 0, x, y);
   {
     float scale[M::kScaleLoads];
@@ -627,7 +630,38 @@ __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
   i32x16 acc[4][4] = {};
   i32x4 fi[2][4], fu[2][4];
   M::read(lds, 0, fi[0], fu[0]);
-  for (int s = 0; s < steps; ++s) {
+  // Between two barriers: 48 products with the reads of the next columns, the
+  // writes of the next step and the loads of the one after it spread over them.
+  const int full = P.k / 128;
+  int s = 0;
+  for (; s + 2 < full; ++s) {
+    i32x4 *now = lds + s % 2 * M::kBuffer, *other = lds + (s + 1) % 2 * M::kBuffer;
+    M::read(now, 1, fi[1], fu[1]);
+    M::multiply(acc, fi[0], fu[0]);
+    M::read(now, 2, fi[0], fu[0]);
+    M::multiply(acc, fi[1], fu[1]);
+    M::read(now, 3, fi[1], fu[1]);
+    M::multiply(acc, fi[0], fu[0]);
+    M::store(other, x, y);
+    M::template load<ODD, true>(P, j0, r0, s + 2, x, y);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    }
+    __syncthreads();
+    M::read(other, 0, fi[0], fu[0]);
+    M::multiply(acc, fi[1], fu[1]);
+  }
+  for (; s < steps; ++s) {  // the last steps, where nothing or less follows
     i32x4 *now = lds + s % 2 * M::kBuffer, *other = lds + (s + 1) % 2 * M::kBuffer;
     M::read(now, 1, fi[1], fu[1]);
     M::multiply(acc, fi[0], fu[0]);
@@ -676,7 +710,7 @@ void launch_few(Product p, hipStream_t stream) {
   }
 }
 
-constexpr int64_t kFewUsers = 64;
+constexpr int64_t kFewUsers = 16;
 // Whether the product's waves turn the users' values into bytes themselves.
 bool takes_values(int64_t rows, int64_t k, int64_t items_bytes) {
   return rows <= 16 && k <= 64 && items_bytes >= 16;
@@ -691,6 +725,8 @@ void launch_values(const Product &p, bool small, hipStream_t stream) {
 template <class O>
 hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
   const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
+  // few tiles and a long k: the waves of a workgroup share a tile
+  const bool split = p.items < (p.rows <= 16 ? 32768 : 8193) && p.kp >= 512;
   if (p.b_end - p.b < 16) {
     const int64_t groups = std::min((p.rows * p.items + kThreads - 1) / kThreads, kFullGpu);
     hipLaunchKernelGGL(k_product_tiny<O>, dim3((unsigned)groups), dim3(kThreads), 0, stream, p);
@@ -698,34 +734,42 @@ hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
     if (type == BGMF_TYPE_F32) launch_values<O, float>(p, small, stream);
     else if (type == BGMF_TYPE_BF16) launch_values<O, bf16_t>(p, small, stream);
     else launch_values<O, f16_t>(p, small, stream);
-  } else if (p.rows <= kFewUsers || p.items < 128) {
-    // the waves of a workgroup share a tile where the tiles are few and k is long
-    const bool split = p.items < 16 * 4096 && p.kp >= 512;
+  } else if (p.rows <= kFewUsers || p.items < 128 || (p.rows <= 64 && split)) {
     if (p.rows <= 16) {
       if (split) launch_few<O, int8_t, 1, 1, true>(p, stream);
       else if (small) launch_few<O, int8_t, 1, 1, false>(p, stream);
       else launch_few<O, int8_t, 1, 4, false>(p, stream);
-    } else if (p.rows <= 32) {
-      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 2, 1, false>(p, stream);
-      else launch_few<O, int8_t, 2, 4, false>(p, stream);
     } else {
-      if (split) launch_few<O, int8_t, 4, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 4, 1, false>(p, stream);
-      else launch_few<O, int8_t, 4, 2, false>(p, stream);
+      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
+      else launch_few<O, int8_t, 2, 1, false>(p, stream);
     }
   } else {
-    const int64_t large = (p.items + 255) / 256 * ((p.rows + 255) / 256);
-    const int64_t many = (p.items + 127) / 128 * ((p.rows + 127) / 128);
+    const auto tiles = [&](int64_t items, int64_t users) {
+      return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
+    };
     const bool odd = p.k % 16;
-    if (p.k >= 512 && large >= 256 && p.items >= 256) {
-      const dim3 groups((unsigned)large), threads(kThreads);
+    const dim3 threads(kThreads);
+    if (p.k >= 512 && p.items >= 256 && tiles(256, 256) >= 256) {
+      const dim3 groups((unsigned)tiles(256, 256));
       if (odd) hipLaunchKernelGGL((k_product_large<O, true>), groups, threads, 0, stream, p);
       else hipLaunchKernelGGL((k_product_large<O, false>), groups, threads, 0, stream, p);
     } else {
-      const dim3 groups((unsigned)std::min<int64_t>(many, 1024)), threads(kThreads);
-      if (odd) hipLaunchKernelGGL((k_product_many<O, true>), groups, threads, 0, stream, p, many);
-      else hipLaunchKernelGGL((k_product_many<O, false>), groups, threads, 0, stream, p, many);
+      const auto many = [&](auto bi, auto bu) {
+        constexpr int BI = decltype(bi)::value, BU = decltype(bu)::value;
+        const int64_t all = tiles(64 * BI, 64 * BU);
+        const dim3 groups((unsigned)std::min<int64_t>(all, 1024));
+        if (odd)
+          hipLaunchKernelGGL((k_product_many<O, BI, BU, true>), groups, threads, 0, stream, p, all);
+        else
+          hipLaunchKernelGGL((k_product_many<O, BI, BU, false>), groups, threads, 0, stream, p,
+                             all);
+      };
+      // the largest tiles of which every CU gets one
+      using std::integral_constant;
+      if (p.rows > 64 && tiles(128, 128) >= 256)
+        many(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+      else if (tiles(128, 64) >= 256) many(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+      else many(integral_constant<int, 1>{}, integral_constant<int, 1>{});
     }
   }
   return hipGetLastError();
