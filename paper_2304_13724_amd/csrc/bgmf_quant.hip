@@ -21,8 +21,6 @@ using i32x16 = __attribute__((ext_vector_type(16))) int32_t;
 // the quotients; what a longer row has beyond that is read a second time.
 // Bound: HBM.
 // ---------------------------------------------------------------------------
-constexpr int kHeld = 4;
-
 // Largest magnitude, +infinity where a value is NaN or infinite.
 struct Largest {
   float most = 0.0f;
@@ -34,21 +32,38 @@ struct Largest {
   }
   __device__ __forceinline__ float get() const { return bad ? INFINITY : most; }
 };
-// The scale of a row with that magnitude, and a value's byte; NaN and 0 bytes
-// where it is infinite.
-__device__ __forceinline__ float scale_of(float most) {
-  return most == INFINITY ? NAN : most / 127.0f;
-}
-__device__ __forceinline__ int8_t byte_of(float x, float scale) {
-  const float y = scale > 0.0f ? rintf(x / scale) : 0.0f;
-  return (int8_t)fminf(fmaxf(y, -127.0f), 127.0f);
-}
+// A row's scale, and its values' bytes; NaN and 0 where the magnitude is
+// infinite.  x / scale has to be rounded as by a division.  Where neither it
+// nor its remainder can leave the normal range, the product with the rounded
+// reciprocal, corrected once by its exact remainder, is that quotient (the
+// error left, 2^-24 units, is less than a quotient of fp32 numbers keeps from
+// a rounding boundary; equal to the division in 1.7e10 of them, half of these
+// next to ties) in a third of the instructions.
+struct Scale {
+  float s, r;
+  bool quick;
+  __device__ __forceinline__ explicit Scale(float most) {
+    s = most == INFINITY ? NAN : most / 127.0f;
+    quick = s >= 0x1p-60f && s <= 0x1p60f;
+    r = quick ? 1.0f / s : 0.0f;
+  }
+  __device__ __forceinline__ int8_t byte(float x) const {
+    float y;
+    if (quick) {
+      y = x * r;
+      y = fmaf(fmaf(-y, s, x), r, y);
+    } else {
+      y = s > 0.0f ? x / s : 0.0f;
+    }
+    return (int8_t)fminf(fmaxf(rintf(y), -127.0f), 127.0f);
+  }
+};
 
 template <class T, int LANES>
 __global__ void __launch_bounds__(kThreads) k_quantize(const T *x, int64_t rows, int32_t k,
                                                        int64_t stride, int8_t *q, int64_t q_stride,
                                                        int32_t fill, float *scale) {
-  constexpr int N = Vec<T>::N;
+  constexpr int N = Vec<T>::N, kHeld = LANES < 64 ? 2 : 8;
   const int lane = threadIdx.x % LANES;
   const int32_t vecs = k / N, tail = vecs * N + lane;
   __shared__ float lds[kWaves];
@@ -82,20 +97,20 @@ __global__ void __launch_bounds__(kThreads) k_quantize(const T *x, int64_t rows,
       for (int w = 0; w < kWaves; ++w) most = fmaxf(most, lds[w]);
       __syncthreads();
     }
-    const float s = scale_of(most);
-    if (lane == 0) scale[r] = s;
+    const Scale s(most);
+    if (lane == 0) scale[r] = s.s;
     int8_t *to = q + r * q_stride;
     const auto put = [&](int32_t v, const Vec<T> &a) {
       int8_t b[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) b[i] = byte_of(to_float(a.v[i]), s);
+      for (int i = 0; i < N; ++i) b[i] = s.byte(to_float(a.v[i]));
       __builtin_memcpy(to + v * N, b, N);
     };
 #pragma unroll
     for (int h = 0; h < kHeld; ++h)
       if (lane + h * LANES < vecs) put(lane + h * LANES, held[h]);
     for (int32_t v = lane + kHeld * LANES; v < vecs; v += LANES) put(v, load_vec(row + v * N));
-    for (int32_t i = tail; i < fill; i += LANES) to[i] = i < k ? byte_of(to_float(row[i]), s) : 0;
+    for (int32_t i = tail; i < fill; i += LANES) to[i] = i < k ? s.byte(to_float(row[i])) : 0;
   }
 }
 
@@ -111,10 +126,11 @@ hipError_t quantize(const void *x, int64_t rows, int32_t k, int64_t stride, int8
                        stream, static_cast<const T *>(x), rows, k, stride, q, q_stride, fill,
                        scale);
   };
-  // as few lanes as keep at most two vectors each, so that short rows fill a wave
+  // as few lanes as hold the row: short rows share a wave, and a wave that has a
+  // row needs no barrier
   if (vecs <= 8) go(std::integral_constant<int, 4>{});
   else if (vecs <= 32) go(std::integral_constant<int, 16>{});
-  else if (vecs <= 256) go(std::integral_constant<int, 64>{});
+  else if (vecs <= 512) go(std::integral_constant<int, 64>{});
   else go(std::integral_constant<int, kThreads>{});
   return hipGetLastError();
 }
@@ -258,12 +274,12 @@ __device__ __forceinline__ float own_bytes(const Product &P, int64_t r, int part
   float most = a.get();
   most = fmaxf(most, __shfl_xor(most, 16));
   most = fmaxf(most, __shfl_xor(most, 32));
-  const float scale = scale_of(most);
+  const Scale s(most);
   int8_t b[16];
 #pragma unroll
-  for (int i = 0; i < 16; ++i) b[i] = byte_of(v[i], scale);
+  for (int i = 0; i < 16; ++i) b[i] = s.byte(v[i]);
   __builtin_memcpy(&y, b, 16);
-  return scale;
+  return s.s;
 }
 
 template <class O, class X, int USERS, int ITEMS, bool SPLIT, bool ODD, bool STREAM>
