@@ -23,6 +23,8 @@ TOP_MAX = bgmf.BGMF_TOP_MAX
 
 _TYPES = {torch.float32: bgmf.BGMF_TYPE_F32, torch.bfloat16: bgmf.BGMF_TYPE_BF16,
           torch.float16: bgmf.BGMF_TYPE_F16}
+_BYTES = {torch.int8: bgmf.BGMF_TYPE_I8}
+_ROW_TYPES = {**_TYPES, **_BYTES}
 
 
 class LogProbs(NamedTuple):
@@ -55,7 +57,7 @@ def _matrix(t: torch.Tensor, name: str, types) -> int:
 def _vector(t: torch.Tensor, name: str, like: torch.Tensor, count: int, dtype) -> None:
     if not isinstance(t, torch.Tensor) or t.dim() != 1 or t.shape[0] != count:
         raise ValueError(f"{name} must be a 1-D tensor of length {count}")
-    if t.dtype != dtype or t.device != like.device:
+    if t.dtype != dtype or t.get_device() != like.get_device():
         raise ValueError(f"{name} must be {dtype} on {like.device}")
     if count > 1 and t.stride(0) != 1:
         raise ValueError(f"{name} must be contiguous")
@@ -80,14 +82,20 @@ def _excluded(t: Optional[torch.Tensor], like: torch.Tensor) -> Tuple[int, int]:
     return t.data_ptr(), t.stride(0)
 
 
+_HERE = contextlib.nullcontext()
+# the current stream's address without a Stream object, where PyTorch offers it
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _on(t: torch.Tensor):
     """The context in which a launch for t's device is made."""
-    if t.device.index == torch.cuda.current_device():
-        return contextlib.nullcontext()
-    return torch.cuda.device(t.device)
+    at = t.get_device()
+    return _HERE if at == torch.cuda.current_device() else torch.cuda.device(at)
 
 
 def _stream(t: torch.Tensor) -> int:
+    if _raw_stream is not None:
+        return _raw_stream(t.get_device())
     return torch.cuda.current_stream(t.device).cuda_stream
 
 
@@ -224,8 +232,8 @@ def quantized_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.
     item_scale, as ``dtype``.  ``rows``: int8 with ``row_scale``, or float32,
     bfloat16 or float16 without it, quantised in the call as by
     ``quantize_rows``.  ``items``: int8 with ``item_scale``."""
-    code = _matrix(rows, "rows", {**_TYPES, torch.int8: bgmf.BGMF_TYPE_I8})
-    _matrix(items, "items", {torch.int8: bgmf.BGMF_TYPE_I8})
+    code = _matrix(rows, "rows", _ROW_TYPES)
+    _matrix(items, "items", _BYTES)
     n, k = rows.shape
     m = items.shape[0]
     if items.shape[1] != k or items.device != rows.device:
@@ -296,28 +304,29 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
     if len(out) != len(grads):
         raise ValueError("out must have a tensor for each gradient")
     sides = (grads,) if out is grads else (grads, out)
-    types = [g.dtype for g in grads]
+    codes = list(map(_TYPES.get, [g.dtype for g in grads]))
     # whole columns of the table at a time: a model has hundreds of gradients
     for side in sides:
-        if dev < 0 or any(d != dev for d in map(torch.Tensor.get_device, side)):
+        if dev < 0 or set(map(torch.Tensor.get_device, side)) != {dev}:
             raise ValueError("gradients and out must be on one GPU")
-    if any(t not in _TYPES for t in set(types)):
+    if None in codes:
         raise ValueError("gradients must be float32, bfloat16 or float16")
-    if out is not grads:
-        if types != [o.dtype for o in out]:
-            raise ValueError("out must have the gradients' types")
-        if any(g.shape != o.shape for g, o in zip(grads, out)):
-            raise ValueError("out must have the gradients' shapes")
+    if out is not grads and codes != list(map(_TYPES.get, [o.dtype for o in out])):
+        raise ValueError("out must have the gradients' types")
     table = np.zeros((len(grads), 7), dtype=np.int64)  # rows of bgmf_grad_t
-    table[:, 0] = [g.data_ptr() for g in grads]
-    table[:, 1] = table[:, 0] if out is grads else [o.data_ptr() for o in out]
-    table[:, 6] = [_TYPES[t] for t in types]
+    table[:, 0] = list(map(torch.Tensor.data_ptr, grads))
+    table[:, 1] = table[:, 0] if out is grads else list(map(torch.Tensor.data_ptr, out))
+    table[:, 6] = codes
     if all(all(map(torch.Tensor.is_contiguous, side)) for side in sides):
+        sizes = list(map(torch.Tensor.numel, grads))
+        if out is not grads and sizes != list(map(torch.Tensor.numel, out)):
+            raise ValueError("out must have the gradients' sizes")
         table[:, 2] = 1
-        table[:, 3] = list(map(torch.Tensor.numel, grads))
-        table[:, 4] = table[:, 5] = table[:, 3]
+        table[:, 3:6] = np.array(sizes, dtype=np.int64)[:, None]
     else:
         for row, g, o in zip(table, grads, out):
+            if g.shape != o.shape:
+                raise ValueError("out must have the gradients' shapes")
             at, to = _layout(g), _layout(o)
             if at[0] != to[0]:  # one side has a row stride: both are taken as matrices
                 at, to = ((t.shape[0], t.shape[1], t.stride(0)) for t in (g, o))
