@@ -1,14 +1,17 @@
-"""Build libbgmf.so (HIP, gfx950) in-tree with hipcc."""
+"""Build libbgmf.so (HIP, gfx950) in-tree with hipcc, and _ranking.so, the
+ranking calls on PyTorch tensors, with g++."""
 from __future__ import annotations
 
 import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 LIB = os.path.join(PKG, "libbgmf.so")
+TENSORS = os.path.join(PKG, "_ranking.so")
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -45,18 +48,39 @@ def _runtime_name_stub() -> str:
     return stub_dir
 
 
-def build(verbose: bool = False) -> str:
-    """Compile every HIP source into paper_2304_13724_amd/libbgmf.so."""
-    tmp = LIB + ".tmp"
-    cmd = [HIPCC, *FLAGS, "-L", _runtime_name_stub(), "-I", os.path.join(ROOT, "include"),
-           *sources(), "-lrocprofiler-sdk-roctx", "-o", tmp]
+def _compile(cmd, out: str, verbose: bool) -> None:
+    tmp = out + ".tmp"
+    cmd = [*cmd, "-o", tmp]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         sys.stderr.write(res.stdout + res.stderr)
-        raise RuntimeError("hipcc failed building libbgmf.so")
-    os.replace(tmp, LIB)
+        raise RuntimeError(f"{os.path.basename(cmd[0])} failed building {os.path.basename(out)}")
+    os.replace(tmp, out)
+
+
+def build_tensors(verbose: bool = False) -> str:
+    """Compile csrc/ranking_tensors.cpp (host code only) against PyTorch's
+    headers and libbgmf.so, which it finds beside itself."""
+    import torch
+    home = os.path.dirname(torch.__file__)
+    _compile(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+              "-isystem", os.path.join(home, "include"),
+              "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"),
+              os.path.join(PKG, "csrc", "ranking_tensors.cpp"), "-L", PKG, "-l:libbgmf.so",
+              "-Wl,-rpath,$ORIGIN", "-L", os.path.join(home, "lib"), "-lc10", "-ltorch_cpu",
+              "-ltorch_python"], TENSORS, verbose)
+    return TENSORS
+
+
+def build(verbose: bool = False) -> str:
+    """Compile every HIP source into paper_2304_13724_amd/libbgmf.so, and
+    paper_2304_13724_amd/_ranking.so."""
+    _compile([HIPCC, *FLAGS, "-L", _runtime_name_stub(), "-I", os.path.join(ROOT, "include"),
+              *sources(), "-lrocprofiler-sdk-roctx"], LIB, verbose)
+    build_tensors(verbose)
     return LIB
 
 
