@@ -9,36 +9,55 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kGroups = 2048;  // workgroups of the norm's pass, at most
-constexpr int kTable = 60;     // gradients that travel in a kernel's arguments (under 4 KB)
+constexpr int kTable = 120;    // table slots that travel in a kernel's arguments (under 4 KB)
 
 // Gradients are worked on in chunks of kChunk elements; gradient i has chunks
-// [first_chunk of i, first_chunk of i + 1).  A gradient whose rows are adjacent
-// counts as one row.
+// [first_chunk of i, first_chunk of the next).  It takes a slot of the table,
+// and a second one if its rows are not adjacent (kMatrix): in, out and size of
+// that hold cols, in_stride and out_stride, and its first_chunk is past all.
 constexpr int64_t kChunk = 8192;
+constexpr int32_t kMatrix = 4, kPast = 0x7FFFFFFF;
+struct Slot {
+  int64_t in, out, size;
+  int32_t first_chunk, type;
+};
+struct Batch {
+  Slot s[kTable];
+};
+
+__global__ void __launch_bounds__(128) k_table(Batch b, int count, Slot *table) {
+  if ((int)threadIdx.x < count) table[threadIdx.x] = b.s[threadIdx.x];
+}
+
+// The gradient of chunk c: the last slot whose first chunk is at most c.
+// Every wave looks at 64 slots at a time.
+__device__ __forceinline__ int32_t find(const Slot *table, int32_t count, int32_t c) {
+  int32_t at = 0;
+  for (int32_t i0 = 0; i0 < count; i0 += 64) {
+    const int32_t i = i0 + (int32_t)(threadIdx.x % 64);
+    const uint64_t below = __ballot(i < count && table[i].first_chunk <= c);
+    if (below) at = i0 + 63 - __builtin_clzll(below);
+  }
+  return __builtin_amdgcn_readfirstlane(at);
+}
+
+// A gradient as the kernels use it.
 struct Entry {
   const void *in;
   void *out;
-  int64_t rows, cols, in_stride, out_stride;
-  int64_t first_chunk;
-  int64_t type;
+  int64_t size, cols, in_stride, out_stride;
+  int32_t first_chunk, type;
+  bool dense;
 };
-struct Batch {
-  Entry e[kTable];
-};
-
-__global__ void __launch_bounds__(64) k_table(Batch b, int count, Entry *table) {
-  if ((int)threadIdx.x < count) table[threadIdx.x] = b.e[threadIdx.x];
-}
-
-// The gradient of chunk c: the last entry whose first chunk is at most c.
-// Every wave looks at 64 entries at a time.
-__device__ __forceinline__ int32_t find(const Entry *table, int32_t count, int64_t c) {
-  int32_t below = 0;
-  for (int32_t i0 = 0; i0 < count; i0 += 64) {
-    const int32_t i = i0 + (int32_t)(threadIdx.x % 64);
-    below += __popcll(__ballot(i < count && table[i].first_chunk <= c));
+__device__ __forceinline__ Entry entry(const Slot *table, int32_t at) {
+  const Slot s = table[at];
+  Entry e{reinterpret_cast<const void *>(s.in), reinterpret_cast<void *>(s.out), s.size, 0, 0, 0,
+          s.first_chunk, s.type & (kMatrix - 1), !(s.type & kMatrix)};
+  if (!e.dense) {
+    const Slot m = table[at + 1];
+    e.cols = m.in, e.in_stride = m.out, e.out_stride = m.size;
   }
-  return __builtin_amdgcn_readfirstlane(below - 1);
+  return e;
 }
 
 template <class T>
@@ -64,18 +83,19 @@ __device__ __forceinline__ double block_sum(double v) {
 // the workgroup has: every gridDim.x-th, so that the chunks worked on at one
 // time lie next to each other.
 template <class F>
-__device__ __forceinline__ void for_chunks(const Entry *table, int32_t count, int64_t chunks,
+__device__ __forceinline__ void for_chunks(const Slot *table, int32_t count, int32_t chunks,
                                            const F &f) {
   Entry e;
-  int64_t stop = -1;  // the first chunk past e's
-  for (int64_t c = blockIdx.x; c < chunks; c += gridDim.x) {
+  int32_t stop = -1;  // the first chunk past e's
+  for (int32_t c = blockIdx.x; c < chunks; c += gridDim.x) {
     if (c >= stop) {
       const int32_t at = find(table, count, c);
-      e = table[at];
-      stop = at + 1 < count ? table[at + 1].first_chunk : chunks;
+      e = entry(table, at);
+      const int32_t next = at + (e.dense ? 1 : 2);
+      stop = next < count ? table[next].first_chunk : chunks;
     }
-    const int64_t lo = (c - e.first_chunk) * kChunk, size = e.rows * e.cols;
-    const int64_t hi = lo + kChunk < size ? lo + kChunk : size;
+    const int64_t lo = (int64_t)(c - e.first_chunk) * kChunk;
+    const int64_t hi = lo + kChunk < e.size ? lo + kChunk : e.size;
     if (e.type == BGMF_TYPE_F32) f(e, float{}, lo, hi);
     else if (e.type == BGMF_TYPE_BF16) f(e, bf16_t{}, lo, hi);
     else f(e, f16_t{}, lo, hi);
@@ -84,7 +104,7 @@ __device__ __forceinline__ void for_chunks(const Entry *table, int32_t count, in
 
 // Squares in fp64: no gradient overflows or vanishes in them, and their sum is
 // better than fp32 whatever its order.  Bound: HBM, one read.
-__device__ __forceinline__ void norm_part(const Entry *table, int32_t count, int64_t chunks,
+__device__ __forceinline__ void norm_part(const Slot *table, int32_t count, int32_t chunks,
                                           double *partial) {
   double s = 0.0;
   for_chunks(table, count, chunks, [&](const Entry &e, auto type, int64_t lo, int64_t hi) {
@@ -92,7 +112,7 @@ __device__ __forceinline__ void norm_part(const Entry *table, int32_t count, int
     constexpr int N = Vec<T>::N, K = (int)(kChunk / (kThreads * N));
     const T *x = static_cast<const T *>(e.in);
     const int tid = threadIdx.x;
-    if (e.rows == 1 && hi - lo == kChunk) {
+    if (e.dense && hi - lo == kChunk) {
       Vec<T> a[K];
 #pragma unroll
       for (int q = 0; q < K; ++q) a[q] = load_vec(x + lo + (tid + q * kThreads) * N);
@@ -100,7 +120,7 @@ __device__ __forceinline__ void norm_part(const Entry *table, int32_t count, int
       for (int q = 0; q < K; ++q)
 #pragma unroll
         for (int i = 0; i < N; ++i) s += square(a[q].v[i]);
-    } else if (e.rows == 1) {
+    } else if (e.dense) {
       int64_t i = lo + tid * N;
       for (; i + N <= hi; i += kThreads * N) {
         const Vec<T> a = load_vec(x + i);
@@ -120,7 +140,7 @@ __device__ __forceinline__ void norm_part(const Entry *table, int32_t count, int
 // The norm from the partial sums, by every workgroup, and the gradients times
 // the factor.  Bound: HBM, one read (from the Infinity Cache where the
 // gradients fit it) and one write.
-__device__ __forceinline__ void clip_part(const Entry *table, int32_t count, int64_t chunks,
+__device__ __forceinline__ void clip_part(const Slot *table, int32_t count, int32_t chunks,
                                           const double *partial, int partials, float max_norm,
                                           float *norm) {
   double s = 0.0;
@@ -137,7 +157,7 @@ __device__ __forceinline__ void clip_part(const Entry *table, int32_t count, int
     T *y = static_cast<T *>(e.out);
     const int tid = threadIdx.x;
     const auto scaled = [&](T v) { return from_float<T>(to_float(v) * factor); };
-    if (e.rows == 1 && hi - lo == kChunk) {
+    if (e.dense && hi - lo == kChunk) {
       Vec<T> a[K];
 #pragma unroll
       for (int q = 0; q < K; ++q) a[q] = load_vec(x + lo + (tid + q * kThreads) * N);
@@ -147,7 +167,7 @@ __device__ __forceinline__ void clip_part(const Entry *table, int32_t count, int
         for (int i = 0; i < N; ++i) a[q].v[i] = scaled(a[q].v[i]);
         store_vec_stream(y + lo + (tid + q * kThreads) * N, a[q]);
       }
-    } else if (e.rows == 1) {
+    } else if (e.dense) {
       int64_t i = lo + tid * N;
       for (; i + N <= hi; i += kThreads * N) {
         Vec<T> a = load_vec(x + i);
@@ -166,21 +186,21 @@ __device__ __forceinline__ void clip_part(const Entry *table, int32_t count, int
 }
 
 // The table in the kernel's arguments, or in the workspace.
-__global__ void __launch_bounds__(kThreads) k_norm_few(Batch b, int32_t count, int64_t chunks,
+__global__ void __launch_bounds__(kThreads) k_norm_few(Batch b, int32_t count, int32_t chunks,
                                                        double *partial) {
-  norm_part(b.e, count, chunks, partial);
+  norm_part(b.s, count, chunks, partial);
 }
-__global__ void __launch_bounds__(kThreads) k_norm(const Entry *table, int32_t count,
-                                                   int64_t chunks, double *partial) {
+__global__ void __launch_bounds__(kThreads) k_norm(const Slot *table, int32_t count,
+                                                   int32_t chunks, double *partial) {
   norm_part(table, count, chunks, partial);
 }
-__global__ void __launch_bounds__(kThreads) k_clip_few(Batch b, int32_t count, int64_t chunks,
+__global__ void __launch_bounds__(kThreads) k_clip_few(Batch b, int32_t count, int32_t chunks,
                                                        const double *partial, int partials,
                                                        float max_norm, float *norm) {
-  clip_part(b.e, count, chunks, partial, partials, max_norm, norm);
+  clip_part(b.s, count, chunks, partial, partials, max_norm, norm);
 }
-__global__ void __launch_bounds__(kThreads) k_clip(const Entry *table, int32_t count,
-                                                   int64_t chunks, const double *partial,
+__global__ void __launch_bounds__(kThreads) k_clip(const Slot *table, int32_t count,
+                                                   int32_t chunks, const double *partial,
                                                    int partials, float max_norm, float *norm) {
   clip_part(table, count, chunks, partial, partials, max_norm, norm);
 }
@@ -196,7 +216,7 @@ extern "C" {
 
 int64_t bgmf_clip_grad_norm_workspace(int64_t count) {
   if (count < 0 || count >= (1ll << 31)) return 0;
-  return padded(kGroups * 8) + padded(count * (int64_t)sizeof(Entry));
+  return padded(kGroups * 8) + padded(2 * count * (int64_t)sizeof(Slot));
 }
 
 int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm, float *norm,
@@ -231,38 +251,45 @@ int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm,
   }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   double *partial = static_cast<double *>(ws);
-  Entry *table = reinterpret_cast<Entry *>(static_cast<char *>(ws) + padded(kGroups * 8));
-  int64_t chunks = 0;
-  int32_t entries = 0, held = 0;
+  Slot *table = reinterpret_cast<Slot *>(static_cast<char *>(ws) + padded(kGroups * 8));
+  int64_t total = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    total += (grads[i].rows * grads[i].cols + kChunk - 1) / kChunk;
+    if (total >= kPast - (1 << 20) || count >= (1 << 30))
+      return fail_call(BGMF_E_UNSUPPORTED, "%s: more than 2^43 elements or 2^30 gradients", call);
+  }
+  int32_t chunks = 0, slots = 0, held = 0;
   Batch b;
   const auto send = [&] {
     if (held)
-      hipLaunchKernelGGL(k_table, dim3(1), dim3(64), 0, stream, b, held, table + entries - held);
+      hipLaunchKernelGGL(k_table, dim3(1), dim3(128), 0, stream, b, held, table + slots - held);
     held = 0;
   };
   for (int64_t i = 0; i < count; ++i) {
     const bgmf_grad_t &g = grads[i];
     if (g.rows == 0 || g.cols == 0) continue;
-    if (held == kTable) send();
     const bool dense = g.rows == 1 || (g.in_stride == g.cols && g.out_stride == g.cols);
-    b.e[held++] = Entry{g.in,        g.out,        dense ? 1 : g.rows, dense ? g.rows * g.cols : g.cols,
-                        g.in_stride, g.out_stride, chunks,             g.type};
-    ++entries;
-    chunks += (g.rows * g.cols + kChunk - 1) / kChunk;
+    const int32_t need = dense ? 1 : 2;
+    if (held + need > kTable) send();
+    b.s[held] = Slot{reinterpret_cast<int64_t>(g.in), reinterpret_cast<int64_t>(g.out),
+                     g.rows * g.cols, chunks, g.type | (dense ? 0 : kMatrix)};
+    if (!dense) b.s[held + 1] = Slot{g.cols, g.in_stride, g.out_stride, kPast, 0};
+    held += need, slots += need;
+    chunks += (int32_t)((g.rows * g.cols + kChunk - 1) / kChunk);
   }
   const unsigned groups = (unsigned)std::min<int64_t>(chunks, kGroups);
   const unsigned clip_groups = (unsigned)std::max<int64_t>(std::min<int64_t>(chunks, kGroups), 1);
-  if (entries <= kTable) {
+  if (slots == held) {
     if (groups)
-      hipLaunchKernelGGL(k_norm_few, dim3(groups), dim3(kThreads), 0, stream, b, entries, chunks,
+      hipLaunchKernelGGL(k_norm_few, dim3(groups), dim3(kThreads), 0, stream, b, slots, chunks,
                          partial);
-    hipLaunchKernelGGL(k_clip_few, dim3(clip_groups), dim3(kThreads), 0, stream, b, entries,
+    hipLaunchKernelGGL(k_clip_few, dim3(clip_groups), dim3(kThreads), 0, stream, b, slots,
                        chunks, partial, (int)groups, max_norm, norm);
   } else {
     send();
-    hipLaunchKernelGGL(k_norm, dim3(groups), dim3(kThreads), 0, stream, table, entries, chunks,
+    hipLaunchKernelGGL(k_norm, dim3(groups), dim3(kThreads), 0, stream, table, slots, chunks,
                        partial);
-    hipLaunchKernelGGL(k_clip, dim3(clip_groups), dim3(kThreads), 0, stream, table, entries,
+    hipLaunchKernelGGL(k_clip, dim3(clip_groups), dim3(kThreads), 0, stream, table, slots,
                        chunks, partial, (int)groups, max_norm, norm);
   }
   const hipError_t e = hipGetLastError();

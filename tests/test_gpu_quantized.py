@@ -100,6 +100,66 @@ def test_product(out, rows, items, k):
     assert torch.equal(c.scores(x.cuda(), TYPES[out]).cpu(), want)
 
 
+# the kernels' other ways: tiles of 128 and 64 items and users, long k shared by
+# the waves of a workgroup, less than 128 items or 16 bytes for many users
+@pytest.mark.parametrize("rows,items,k", [
+    (100, 20000, 72), (100, 20001, 64), (1030, 4100, 96), (1030, 4099, 201), (64, 4097, 64),
+    (20, 300, 777), (64, 2000, 600), (33, 8200, 512), (17, 8193, 640), (200, 100, 64),
+    (70, 127, 130), (5, 3, 5), (300, 2, 7), (40, 15, 1), (16, 33000, 520)])
+def test_product_other_tiles(rows, items, k):
+    x, v = draw(rows, k, "f32", rows + 1), draw(items, k, "f32", items + 1)
+    q, a = quantized(x)
+    w, b = quantized(v)
+    want = product(q, a, w, b, torch.float32)
+    wc, bc = torch.from_numpy(w).cuda(), torch.from_numpy(b).cuda()
+    assert torch.equal(ranking.quantized_scores(x.cuda(), wc, bc).cpu(), want)
+    assert torch.equal(ranking.Catalogue(v.cuda()).scores(x.cuda()).cpu(), want)
+
+
+def on_gpu(rows, items, k, seed, pad=0):
+    """Bytes, scales and the product in doubles, all on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    draw8 = lambda n, wide: torch.randint(-127, 128, (n, wide), generator=g, device="cuda",  # noqa: E731
+                                          dtype=torch.int8)
+    q, w = draw8(rows, k), draw8(items, k + pad)[:, :k]
+    a, b = (torch.rand(n, generator=g, device="cuda") for n in (rows, items))
+    total = q.double() @ w.double().t()
+    return q, a, w, b, total.float() * a[:, None] * b[None]
+
+
+# many items: several tiles for each wave, the last ones overlapping, and items
+# that the caches cannot hold
+@pytest.mark.parametrize("rows,items,k,pad", [
+    (1, 524_293, 64, 0), (1, 600_001, 50, 0), (16, 524_300, 48, 0), (3, 524_301, 128, 0),
+    (2, 530_000, 100, 0), (1, 3_200_001, 64, 0), (2, 1_700_003, 128, 0), (1, 600_001, 50, 14),
+    (40, 524_301, 64, 0)])
+def test_product_many_items(rows, items, k, pad):
+    q, a, w, b, want = on_gpu(rows, items, k, k + rows, pad)
+    assert torch.equal(ranking.quantized_scores(q, w, b, a), want)
+    # values whose bytes are q with scale a: the largest of each row is 127
+    x = q.float()
+    x[:, 0] = 127.0
+    got = ranking.quantized_scores(x * a[:, None], w, b)
+    r, s = ranking.quantize_rows(x * a[:, None])
+    assert torch.equal(got, ranking.quantized_scores(r, w, b, s))
+
+
+@pytest.mark.parametrize("out", list(TYPES))
+@pytest.mark.parametrize("rows,items,k,pad", [
+    (4096, 4096, 512, 0), (4000, 4099, 528, 0), (3841, 4111, 521, 0), (4096, 4352, 640, 0),
+    (4000, 4200, 513, 3), (5000, 4100, 1000, 8), (4097, 4097, 1152, 16)])
+def test_product_large_tiles(out, rows, items, k, pad):
+    q, a, w, b, want = on_gpu(rows, items, k, k, pad)
+    got = ranking.quantized_scores(q, w, b, a, dtype=TYPES[out])
+    assert torch.equal(got, want.to(TYPES[out]))
+
+
+def test_product_of_millions_of_users():
+    """More users than a launch has blocks for."""
+    q, a, w, b, want = on_gpu(65535 * 32 + 37, 20, 16, 1)
+    assert torch.equal(ranking.quantized_scores(q, w, b, a), want)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_product_of_16_bit_rows(dtype):
     for rows, items, k in ((1, 500, 64), (40, 130, 200), (150, 260, 96)):
