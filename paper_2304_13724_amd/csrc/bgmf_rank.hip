@@ -14,15 +14,44 @@ constexpr int kThreads = 256;
 constexpr float kLog2e = 1.44269504088896341f;
 constexpr double kLn2 = 0.69314718055994530942;
 
+// Reductions over a wave in registers (DPP): four steps within rows of 16
+// lanes, two between rows, the total in lane 63.  A lane without a source adds
+// `none`.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t dpp(int32_t none, int32_t x) {
+  return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xF, false);
+}
+template <class F>
+__device__ __forceinline__ int32_t wave_reduce(int32_t v, int32_t none, const F &f) {
+  v = f(v, dpp<0x111, 0xF>(none, v));
+  v = f(v, dpp<0x112, 0xF>(none, v));
+  v = f(v, dpp<0x114, 0xF>(none, v));
+  v = f(v, dpp<0x118, 0xF>(none, v));
+  v = f(v, dpp<0x142, 0xA>(none, v));
+  v = f(v, dpp<0x143, 0xC>(none, v));
+  return __builtin_amdgcn_readlane(v, 63);
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return __int_as_float(wave_reduce(__float_as_int(v), __float_as_int(-INFINITY),
+                                    [](int32_t a, int32_t b) {
+                                      return __float_as_int(
+                                          fmaxf(__int_as_float(a), __int_as_float(b)));
+                                    }));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double dpp_add(double v) {
+  const int32_t lo = dpp<CTRL, ROWS>(0, __double2loint(v)), hi = dpp<CTRL, ROWS>(0, __double2hiint(v));
+  return v + __hiloint2double(hi, lo);
 }
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  v = dpp_add<0x111, 0xF>(v);
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);
+  v = dpp_add<0x143, 0xC>(v);
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 63),
+                          __builtin_amdgcn_readlane(__double2loint(v), 63));
 }
 
 // A row, or a part of one, in 16-byte vectors and up to N - 1 single elements
@@ -121,17 +150,18 @@ __device__ __forceinline__ Soft block_soft(Soft a, float c, SoftLds<TH> &lds) {
 // kept the largest score of each.  The n-th largest of 256 maxima (of threads,
 // or of columns where a workgroup is one wave) is a score that the n best are
 // not below, and only columns with their maximum at or above it ("hot", a few
-// more than n) can hold any of them: their scores, about n / 1024 of the row,
-// are read once more (from the cache), and those at or above the bound, few
-// more than n, are put in order by counting how many precede each.  If more
+// more than n) can hold any of them: these are read once more, about n / 1024
+// of the row and from the cache, and the scores at or above the bound, few more
+// than n, are put in order by counting how many precede each.  If more
 // than CAND qualify (equal scores, or the best ones all in few columns), the
 // scores are gone through in order of items instead, merging each tile's
 // candidates into a list.
 //
-// SRC: Piece, PIECES: what one load brings, and how many are in flight;
-// per_column() pieces of a column; load(column, i), column % TH is the thread;
-// each(piece, column, i, f): f(score, item) for each score of the piece; size()
-// and at(p, item): all scores in the order of items.
+// SRC: either SHARED, per_column() and piece(q, i, f): f(score, item) for
+// each score of piece i of column q (the workgroup shares the hot columns'
+// pieces), or not SHARED and column(q, bound, f): the same for scores of column
+// q, all that are at or above the bound among them (by the column's thread);
+// size() and at(p, item): all scores in the order of items.
 // emit(rank, score, item), for every rank below n (item -1: none).
 // ---------------------------------------------------------------------------
 constexpr int kCols = 4;
@@ -178,13 +208,8 @@ __device__ __forceinline__ float top_bound(const float (&tm)[4], int n) {
     some += __popcll(__ballot(k[i] > none));
   }
   if (some < n) return -INFINITY;
-#pragma unroll
-  for (int o = 32; o; o >>= 1) {
-    lo = min(lo, __shfl_xor(lo, o));
-    hi = max(hi, __shfl_xor(hi, o));
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
+  lo = wave_reduce(lo, 0x7FFFFFFF, [](int32_t a, int32_t b) { return min(a, b); });
+  hi = wave_reduce(hi, none, [](int32_t a, int32_t b) { return max(a, b); });
   while (lo < hi) {  // at least n are at or above lo, fewer than n above hi
     const int32_t mid = (int32_t)((uint32_t)lo + ((uint32_t)hi - (uint32_t)lo + 1) / 2);
     int c = 0;
@@ -291,36 +316,26 @@ __device__ __forceinline__ void top_select(const SRC &src, const float (&tm)[kCo
     __syncthreads();
     bound = lds.bound;
   }
+  const auto candidate = [&](float v, int32_t j) {
+    if (v > -INFINITY && v >= bound) {
+      const int to = atomicAdd(&lds.count, 1);
+      if (to < CAND) lds.k[to] = rank_key(v, j);
+    }
+  };
   if (most > -INFINITY && most >= bound) {
 #pragma unroll
     for (int q = 0; q < kCols; ++q)
-      if (tm[q] > -INFINITY && tm[q] >= bound)
-        lds.hot[atomicAdd(&lds.hots, 1)] = (uint16_t)(tid + q * TH);
+      if (tm[q] > -INFINITY && tm[q] >= bound) {
+        if constexpr (SRC::SHARED) lds.hot[atomicAdd(&lds.hots, 1)] = (uint16_t)(tid + q * TH);
+        else src.column(tid + q * TH, bound, candidate);
+      }
   }
   __syncthreads();
-  const uint32_t per = (uint32_t)src.per_column(), items = (uint32_t)lds.hots * per;
-  constexpr int K = SRC::PIECES;
-  for (uint32_t i0 = tid; i0 < items; i0 += TH * K) {
-    typename SRC::Piece piece[K];
-    int col[K], at[K];
-#pragma unroll
-    for (int q = 0; q < K; ++q) {
-      const uint32_t i = i0 + q * TH, h = i / per;
-      col[q] = i < items ? lds.hot[h] : -1;
-      at[q] = (int)(i - h * per);
-      if (col[q] >= 0) piece[q] = src.load(col[q], at[q]);
-    }
-#pragma unroll
-    for (int q = 0; q < K; ++q)
-      if (col[q] >= 0)
-        src.each(piece[q], col[q], at[q], [&](float v, auto item) {
-          if (v > -INFINITY && v >= bound) {
-            const int to = atomicAdd(&lds.count, 1);
-            if (to < CAND) lds.k[to] = rank_key(v, item());
-          }
-        });
+  if constexpr (SRC::SHARED) {
+    const uint32_t per = (uint32_t)src.per_column(), pieces = (uint32_t)lds.hots * per;
+    for (uint32_t i = tid; i < pieces; i += TH) src.piece(lds.hot[i / per], i % per, candidate);
+    __syncthreads();
   }
-  __syncthreads();
   const int c = lds.count;
   if (c > CAND) {
     __syncthreads();
@@ -343,32 +358,25 @@ __device__ __forceinline__ void top_select(const SRC &src, const float (&tm)[kCo
 template <class T, bool EX, int TH>
 struct RowSource {  // column q has vectors q, q + 4 TH, ..., and column q < TH tail element q
   static constexpr int N = Row<T, EX>::N;
-  struct Piece {
-    float x[N];
-  };
-  static constexpr int PIECES = 1;
+  static constexpr bool SHARED = true;
   Row<T, EX> row;
   int32_t first;  // item of the row's first element
   __device__ __forceinline__ int32_t per_column() const {
     return (row.vecs() + kCols * TH - 1) / (kCols * TH) + 1;
   }
-  __device__ __forceinline__ Piece load(int col, int32_t i) const {
-    Piece p;
-#pragma unroll
-    for (int e = 0; e < N; ++e) p.x[e] = -INFINITY;
-    const int32_t vecs = row.vecs(), v = col + (i - 1) * (kCols * TH);
-    if (i == 0) {
-      if (col < row.len - vecs * N) p.x[0] = row.one(vecs * N + col);
-    } else if (v < vecs) {
-      row.load(v, p.x);
-    }
-    return p;
-  }
   template <class F>
-  __device__ __forceinline__ void each(const Piece &p, int col, int32_t i, const F &f) const {
-    const int32_t at = i == 0 ? row.vecs() * N + col : (col + (i - 1) * (kCols * TH)) * N;
+  __device__ __forceinline__ void piece(int q, int32_t i, const F &f) const {
+    const int32_t vecs = row.vecs();
+    if (i == 0) {
+      if (q < row.len - vecs * N) f(row.one(vecs * N + q), first + vecs * N + q);
+      return;
+    }
+    const int32_t v = q + (i - 1) * (kCols * TH);
+    if (v >= vecs) return;
+    float x[N];
+    row.load(v, x);
 #pragma unroll
-    for (int e = 0; e < N; ++e) f(p.x[e], [&] { return first + at + e; });
+    for (int e = 0; e < N; ++e) f(x[e], first + v * N + e);
   }
   __device__ __forceinline__ int64_t size() const { return row.len; }
   __device__ __forceinline__ float at(int64_t p, int32_t &j) const {
@@ -494,20 +502,28 @@ __global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
   }
 }
 
-struct PartSource {  // column q has the list of part q
-  struct Piece {
-    float v;
-  };
-  static constexpr int PIECES = 4;
+struct PartSource {  // column q has the list of part q, larger scores first
+  static constexpr bool SHARED = false;
   const float *v;
   const int32_t *j;
   int64_t parts;
   int n;
-  __device__ __forceinline__ int32_t per_column() const { return n; }
-  __device__ __forceinline__ Piece load(int col, int32_t i) const { return {v[col * n + i]}; }
   template <class F>
-  __device__ __forceinline__ void each(const Piece &p, int col, int32_t i, const F &f) const {
-    f(p.v, [&] { return j[col * n + i]; });
+  __device__ __forceinline__ void column(int q, float bound, const F &f) const {
+    const float *x = v + (int64_t)q * n;
+    const int32_t *item = j + (int64_t)q * n;
+    for (int i = 0; i < n; i += 4) {  // few lists have more at or above the bound
+      float y[4];
+      int32_t k[4];
+#pragma unroll
+      for (int p = 0; p < 4; ++p) {
+        y[p] = i + p < n ? x[i + p] : -INFINITY;
+        k[p] = i + p < n ? item[i + p] : -1;
+      }
+#pragma unroll
+      for (int p = 0; p < 4; ++p) f(y[p], k[p]);
+      if (!(y[3] >= bound)) break;
+    }
   }
   __device__ __forceinline__ int64_t size() const { return parts * n; }
   __device__ __forceinline__ float at(int64_t p, int32_t &item) const {
