@@ -460,16 +460,14 @@ struct Many {
     r0 = (group * kGroup + in % size) * kUsers;
   }
 
-  // A thread's 16-byte chunks of step s of the tile at (j0, r0).  FULL: the step
+  // A thread's 16-byte chunks of step s of the items from j0 on.  FULL: the step
   // lies within k.
   template <bool ODD, bool FULL = false>
-  static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
-                                              i32x4 (&x)[kItemLoads],
-                                              i32x4 (&y)[kUserLoads]) {
+  static __device__ __forceinline__ void load_items(const Product &P, int64_t j0, int s,
+                                                    i32x4 (&x)[kItemLoads]) {
     const int row = threadIdx.x / kChunks;
     const int32_t c = s * STEP + threadIdx.x % kChunks * 16;
     const int8_t *b = P.b + (j0 + row) * P.b_stride;
-    const int8_t *a = P.a + (r0 + row) * P.kp + c;
     if (FULL || (s + 1) * STEP <= P.k) {
 #pragma unroll
       for (int h = 0; h < kItemLoads; ++h) x[h] = item_bytes(b + h * kPass * P.b_stride, c);
@@ -480,10 +478,64 @@ struct Many {
         else x[h] = c < P.k ? item_bytes(b + h * kPass * P.b_stride, c) : i32x4{0, 0, 0, 0};
       }
     }
+  }
+  // The same of the users from r0 on.
+  template <bool FULL = false>
+  static __device__ __forceinline__ void load_users(const Product &P, int64_t r0, int s,
+                                                    i32x4 (&y)[kUserLoads]) {
+    const int32_t c = s * STEP + threadIdx.x % kChunks * 16;
+    const int8_t *a = P.a + (r0 + threadIdx.x / kChunks) * P.kp + c;
     if (FULL || STEP <= kUnit || c < P.kp) {
 #pragma unroll
       for (int h = 0; h < kUserLoads; ++h)
         y[h] = *reinterpret_cast<const i32x4 *>(a + (int64_t)h * kPass * P.kp);
+    }
+  }
+  // The users' values in place of bytes, for k <= STEP = 64: the four threads of
+  // a row turn them into bytes, and the first writes the row's scale.
+  template <class X>
+  struct Values {
+    Vec<X> v[16 / Vec<X>::N];
+  };
+  template <bool ODD, class X>
+  static __device__ __forceinline__ void load_values(const Product &P, int64_t r0,
+                                                     Values<X> (&y)[kUserLoads]) {
+    constexpr int N = Vec<X>::N;
+    const int32_t c = threadIdx.x % kChunks * 16;
+#pragma unroll
+    for (int h = 0; h < kUserLoads; ++h) {
+      const int64_t j = r0 + threadIdx.x / kChunks + h * kPass, r = j < P.rows ? j : P.rows - 1;
+      const X *x = static_cast<const X *>(P.x) + r * P.x_stride + c;
+      if (c + 16 <= P.k) {
+#pragma unroll
+        for (int i = 0; i < 16 / N; ++i) y[h].v[i] = load_vec(x + i * N);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16 / N; ++i)
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            y[h].v[i].v[e] = ODD && c + i * N + e < P.k ? x[i * N + e] : from_float<X>(0.0f);
+      }
+    }
+  }
+  template <class X>
+  static __device__ __forceinline__ void to_bytes(const Values<X> (&values)[kUserLoads],
+                                                  i32x4 (&y)[kUserLoads], float *s_user) {
+    constexpr int N = Vec<X>::N;
+#pragma unroll
+    for (int h = 0; h < kUserLoads; ++h) {
+      Largest a;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) a.look(to_float(values[h].v[i / N].v[i % N]));
+      float most = a.get();
+      most = fmaxf(most, __shfl_xor(most, 1));
+      most = fmaxf(most, __shfl_xor(most, 2));
+      const Scale s(most);
+      int8_t b[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) b[i] = s.byte(to_float(values[h].v[i / N].v[i % N]));
+      __builtin_memcpy(&y[h], b, 16);
+      if (threadIdx.x % kChunks == 0) s_user[threadIdx.x / kChunks + h * kPass] = s.s;
     }
   }
   static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kItemLoads],
@@ -514,8 +566,8 @@ struct Many {
       for (int u = 0; u < BU; ++u)
         acc[i][u] = __builtin_amdgcn_mfma_i32_32x32x32_i8(fi[i], fu[u], acc[i][u], 0, 0, 0);
   }
-  // The scales of the tile's items, then of its users (those past the last
-  // user's are not used).
+  // The scales of the tile's items, then of its users if they came as bytes
+  // (those past the last user's are not used).
   static constexpr int kScaleLoads = (kItems + kUsers + kThreads - 1) / kThreads;
   static __device__ __forceinline__ void load_scales(const Product &P, int64_t j0, int64_t r0,
                                                      float (&scale)[kScaleLoads]) {
@@ -523,7 +575,8 @@ struct Many {
     for (int h = 0; h < kScaleLoads; ++h) {
       const int i = threadIdx.x + h * kThreads;
       const int64_t r = r0 + i - kItems;
-      scale[h] = i < kItems ? P.b_scale[j0 + i] : P.a_scale[r < P.rows ? r : P.rows - 1];
+      if (i < kItems) scale[h] = P.b_scale[j0 + i];
+      else if (P.a_scale) scale[h] = P.a_scale[r < P.rows ? r : P.rows - 1];
     }
   }
 
@@ -571,31 +624,39 @@ struct Many {
 
 // Tiles of 128 or 64 items x 128 or 64 users, 64 bytes of k at a time: four workgroups on a CU overlap their loads, products and stores.  A workgroup's bytes of the next step, or
 // of its next tile, are on their way into registers meanwhile.
-template <class O, int BI, int BU, bool ODD>
+template <class O, class X, int BI, int BU, bool ODD>
 __global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t tiles) {
   using M = Many<O, BI, BU, 64>;
+  constexpr bool OWN = !std::is_same<X, int8_t>::value;
   __shared__ i32x4 lds[M::kBuffer > M::kScores ? M::kBuffer : M::kScores];
   __shared__ float s_item[M::kScaleLoads * kThreads];
   const int steps = P.kp / 64;
   i32x4 x[M::kItemLoads], y[M::kUserLoads];
+  typename M::template Values<typename std::conditional<OWN, X, float>::type>
+      values[M::kUserLoads];
   float scale[M::kScaleLoads];
+  const auto load = [&](int64_t j0, int64_t r0, int s) {
+    M::template load_items<ODD>(P, j0, s, x);
+    if constexpr (OWN) M::template load_values<ODD>(P, r0, values);
+    else M::load_users(P, r0, s, y);
+    if (s == 0) M::load_scales(P, j0, r0, scale);
+  };
   i32x16 acc[BI][BU] = {};
   int64_t tile = blockIdx.x, j0, r0;
   M::place(P, tile, j0, r0);
-  M::template load<ODD>(P, j0, r0, 0, x, y);
-  M::load_scales(P, j0, r0, scale);
+  load(j0, r0, 0);
   for (int s = 0; tile < tiles;) {
     __syncthreads();
+    if constexpr (OWN) M::to_bytes(values, y, s_item + M::kItems);
     M::store(lds, x, y);
-    if (s == 0) s_item[threadIdx.x] = scale[0];
+    if (s == 0 && (!OWN || (int)threadIdx.x < M::kItems)) s_item[threadIdx.x] = scale[0];
     __syncthreads();
     const bool last = s + 1 == steps;
     int64_t jn = j0, rn = r0;
     const int64_t next = last ? tile + gridDim.x : tile;
     if (next < tiles) {
       if (last) M::place(P, next, jn, rn);
-      M::template load<ODD>(P, jn, rn, last ? 0 : s + 1, x, y);
-      if (last) M::load_scales(P, jn, rn, scale);
+      load(jn, rn, last ? 0 : s + 1);
     }
 #pragma unroll
     for (int sub = 0; sub < 2; ++sub) {
@@ -633,7 +694,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
   int64_t j0, r0;
   M::place(P, blockIdx.x, j0, r0);
   i32x4 x[M::kItemLoads], y[M::kUserLoads];
-  M::template load<ODD>(P, j0, r0, 0, x, y);
+  M::template load_items<ODD>(P, j0, 0, x);
+  M::load_users(P, r0, 0, y);
   {
     float scale[M::kScaleLoads];
     M::load_scales(P, j0, r0, scale);
@@ -641,7 +703,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
     for (int h = 0; h < M::kScaleLoads; ++h) s_item[threadIdx.x + h * kThreads] = scale[h];
   }
   M::store(lds, x, y);
-  if (steps > 1) M::template load<ODD>(P, j0, r0, 1, x, y);
+  if (steps > 1) {
+    M::template load_items<ODD>(P, j0, 1, x);
+    M::load_users(P, r0, 1, y);
+  }
   __syncthreads();
   i32x16 acc[4][4] = {};
   i32x4 fi[2][4], fu[2][4];
@@ -659,7 +724,8 @@ __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
     M::read(now, 3, fi[1], fu[1]);
     M::multiply(acc, fi[0], fu[0]);
     M::store(other, x, y);
-    M::template load<ODD, true>(P, j0, r0, s + 2, x, y);
+    M::template load_items<ODD, true>(P, j0, s + 2, x);
+    M::template load_users<true>(P, r0, s + 2, y);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
@@ -687,7 +753,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_product_large(Product P) {
     M::multiply(acc, fi[0], fu[0]);
     if (s + 1 < steps) {
       M::store(other, x, y);
-      if (s + 2 < steps) M::template load<ODD>(P, j0, r0, s + 2, x, y);
+      if (s + 2 < steps) {
+        M::template load_items<ODD>(P, j0, s + 2, x);
+        M::load_users(P, r0, s + 2, y);
+      }
     }
     __syncthreads();
     if (s + 1 < steps) M::read(other, 0, fi[0], fu[0]);
@@ -726,67 +795,87 @@ void launch_few(Product p, hipStream_t stream) {
   }
 }
 
-constexpr int64_t kFewUsers = 16;
-// Whether the product's waves turn the users' values into bytes themselves.
-bool takes_values(int64_t rows, int64_t k, int64_t items_bytes) {
-  return rows <= 16 && k <= 64 && items_bytes >= 16;
+constexpr int64_t kFewUsers = 16, kFewItems = 128;
+// Whether the product itself turns the users' values into bytes: one launch less
+// (64 x 18,000 x 64, 282 tiles, 4.6 us against 5.8; 512 users 9.5 against 10.3;
+// 4,000 x 3,000, 1,512 tiles, 10.8 against 12.0).  Each tile quantises its users
+// again, so with many of them the launch is cheaper (100 x 125,000, 1,954 tiles,
+// 14.1 us against 12.3; 2,048 x 18,000 24.7 against 20.3).
+bool takes_values(int64_t rows, int64_t items, int64_t k, int64_t items_bytes) {
+  if (k > 64) return false;
+  if (rows <= kFewUsers) return items_bytes >= 16;
+  return items >= kFewItems && (items + 127) / 128 * ((rows + 63) / 64) <= 1536;
 }
 
+template <class O, class X, int BI, int BU>
+void launch_many(const Product &p, hipStream_t stream) {
+  const int64_t all =
+      (p.items + 64 * BI - 1) / (64 * BI) * ((p.rows + 64 * BU - 1) / (64 * BU));
+  const dim3 groups((unsigned)std::min<int64_t>(all, 1024)), threads(kThreads);
+  if (p.k % 16)
+    hipLaunchKernelGGL((k_product_many<O, X, BI, BU, true>), groups, threads, 0, stream, p, all);
+  else
+    hipLaunchKernelGGL((k_product_many<O, X, BI, BU, false>), groups, threads, 0, stream, p, all);
+}
+
+// X: int8_t, or the type of the users' values that the product itself quantises.
 template <class O, class X>
-void launch_values(const Product &p, bool small, hipStream_t stream) {
-  if (small) launch_few<O, X, 1, 1, false>(p, stream);
-  else launch_few<O, X, 1, 8, false>(p, stream);
+void launch_product(const Product &p, hipStream_t stream) {
+  constexpr bool OWN = !std::is_same<X, int8_t>::value;
+  const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
+  // few tiles and a long k: the waves of a workgroup share a tile
+  const bool split = !OWN && p.items < (p.rows <= 16 ? 32768 : 8193) && p.kp >= 512;
+  const auto tiles = [&](int64_t items, int64_t users) {
+    return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
+  };
+  if (p.rows <= kFewUsers) {
+    if constexpr (OWN) {
+      if (small) launch_few<O, X, 1, 1, false>(p, stream);
+      else launch_few<O, X, 1, 8, false>(p, stream);
+    } else {
+      if (split) launch_few<O, X, 1, 1, true>(p, stream);
+      else if (small) launch_few<O, X, 1, 1, false>(p, stream);
+      else launch_few<O, X, 1, 4, false>(p, stream);
+    }
+    return;
+  }
+  if constexpr (!OWN) {
+    if (p.items < kFewItems || (p.rows <= 64 && split)) {
+      if (split) launch_few<O, X, 2, 1, true>(p, stream);
+      else launch_few<O, X, 2, 1, false>(p, stream);
+      return;
+    }
+    if (p.k >= 512 && p.items >= 256 && tiles(256, 256) >= 256) {
+      const dim3 groups((unsigned)tiles(256, 256)), threads(kThreads);
+      if (p.k % 16)
+        hipLaunchKernelGGL((k_product_large<O, true>), groups, threads, 0, stream, p);
+      else hipLaunchKernelGGL((k_product_large<O, false>), groups, threads, 0, stream, p);
+      return;
+    }
+    // the largest tiles of which every CU gets one
+    if (p.rows > 64 && tiles(128, 128) >= 256) {
+      launch_many<O, X, 2, 2>(p, stream);
+      return;
+    }
+  }
+  // (values take the registers that a second 64 users would need)
+  if (tiles(128, 64) >= 256) launch_many<O, X, 2, 1>(p, stream);
+  else launch_many<O, X, 1, 1>(p, stream);
 }
 
 template <class O>
 hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
-  const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
-  // few tiles and a long k: the waves of a workgroup share a tile
-  const bool split = p.items < (p.rows <= 16 ? 32768 : 8193) && p.kp >= 512;
   if (p.b_end - p.b < 16) {
     const int64_t groups = std::min((p.rows * p.items + kThreads - 1) / kThreads, kFullGpu);
     hipLaunchKernelGGL(k_product_tiny<O>, dim3((unsigned)groups), dim3(kThreads), 0, stream, p);
-  } else if (p.x) {
-    if (type == BGMF_TYPE_F32) launch_values<O, float>(p, small, stream);
-    else if (type == BGMF_TYPE_BF16) launch_values<O, bf16_t>(p, small, stream);
-    else launch_values<O, f16_t>(p, small, stream);
-  } else if (p.rows <= kFewUsers || p.items < 128 || (p.rows <= 64 && split)) {
-    if (p.rows <= 16) {
-      if (split) launch_few<O, int8_t, 1, 1, true>(p, stream);
-      else if (small) launch_few<O, int8_t, 1, 1, false>(p, stream);
-      else launch_few<O, int8_t, 1, 4, false>(p, stream);
-    } else {
-      if (split) launch_few<O, int8_t, 2, 1, true>(p, stream);
-      else launch_few<O, int8_t, 2, 1, false>(p, stream);
-    }
+  } else if (!p.x) {
+    launch_product<O, int8_t>(p, stream);
+  } else if (type == BGMF_TYPE_F32) {
+    launch_product<O, float>(p, stream);
+  } else if (type == BGMF_TYPE_BF16) {
+    launch_product<O, bf16_t>(p, stream);
   } else {
-    const auto tiles = [&](int64_t items, int64_t users) {
-      return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
-    };
-    const bool odd = p.k % 16;
-    const dim3 threads(kThreads);
-    if (p.k >= 512 && p.items >= 256 && tiles(256, 256) >= 256) {
-      const dim3 groups((unsigned)tiles(256, 256));
-      if (odd) hipLaunchKernelGGL((k_product_large<O, true>), groups, threads, 0, stream, p);
-      else hipLaunchKernelGGL((k_product_large<O, false>), groups, threads, 0, stream, p);
-    } else {
-      const auto many = [&](auto bi, auto bu) {
-        constexpr int BI = decltype(bi)::value, BU = decltype(bu)::value;
-        const int64_t all = tiles(64 * BI, 64 * BU);
-        const dim3 groups((unsigned)std::min<int64_t>(all, 1024));
-        if (odd)
-          hipLaunchKernelGGL((k_product_many<O, BI, BU, true>), groups, threads, 0, stream, p, all);
-        else
-          hipLaunchKernelGGL((k_product_many<O, BI, BU, false>), groups, threads, 0, stream, p,
-                             all);
-      };
-      // the largest tiles of which every CU gets one
-      using std::integral_constant;
-      if (p.rows > 64 && tiles(128, 128) >= 256)
-        many(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-      else if (tiles(128, 64) >= 256) many(integral_constant<int, 2>{}, integral_constant<int, 1>{});
-      else many(integral_constant<int, 1>{}, integral_constant<int, 1>{});
-    }
+    launch_product<O, f16_t>(p, stream);
   }
   return hipGetLastError();
 }
@@ -880,7 +969,7 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
     hipLaunchKernelGGL(k_pad_rows, dim3((unsigned)groups), dim3(kThreads), 0, stream,
                        static_cast<const int8_t *>(x), rows, (int32_t)k, row_stride, q, kp);
     e = hipGetLastError();
-  } else if (takes_values(rows, k, p.b_end - p.b)) {
+  } else if (takes_values(rows, item_count, k, p.b_end - p.b)) {
     p.x = x, p.x_stride = row_stride;
   } else {
     float *scale = reinterpret_cast<float *>(q + bytes_part(rows, k));

@@ -288,3 +288,26 @@ def test_refusals():
         ranking.quantized_scores(torch.zeros(1, k, device="cuda"),
                                  torch.zeros(1, k, dtype=torch.int8, device="cuda"), b[:1])
     assert e.value.code == bgmf.BGMF_E_ARG
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("rows,items,k", [
+    (17, 128, 64), (17, 129, 1), (64, 18000, 64), (65, 300, 50), (100, 20000, 48), (513, 700, 33),
+    (130, 20001, 64), (1000, 130, 16), (30, 4097, 17), (700, 30000, 64)])
+def test_values_quantised_within_the_product(dtype, rows, items, k):
+    """The same scores whether the product or quantize_rows made the bytes."""
+    x = draw(rows, k, dtype, rows)
+    if rows > 20:
+        x[3], x[5, 0] = 0.0, float("nan")
+    v = draw(items, k, "f32", items)
+    c = ranking.Catalogue(v.cuda())
+    r, s = ranking.quantize_rows(x.cuda())
+    one = c.scores(x.cuda())
+    two = ranking.quantized_scores(r, c.items, c.scale, s)
+    assert torch.equal(one.nan_to_num(7.0), two.nan_to_num(7.0))
+    q, a = quantized(x)
+    np.testing.assert_array_equal(r.cpu().numpy(), q)
+    np.testing.assert_array_equal(s.cpu().numpy(), a)
+    w, b = quantized(v)
+    want = product(q, a, w, b, torch.float32)
+    assert torch.equal(one.cpu().nan_to_num(7.0), want.nan_to_num(7.0))
