@@ -625,7 +625,7 @@ struct Many {
 // Tiles of 128 or 64 items x 128 or 64 users, 64 bytes of k at a time: four workgroups on a CU overlap their loads, products and stores.  A workgroup's bytes of the next step, or
 // of its next tile, are on their way into registers meanwhile.
 template <class O, class X, int BI, int BU, bool ODD>
-__global__ void __launch_bounds__(kThreads, 4) k_product_many(Product P, int64_t tiles) {
+__global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4) k_product_many(Product P, int64_t tiles) {
   using M = Many<O, BI, BU, 64>;
   constexpr bool OWN = !std::is_same<X, int8_t>::value;
   __shared__ i32x4 lds[M::kBuffer > M::kScores ? M::kBuffer : M::kScores];
@@ -811,7 +811,8 @@ template <class O, class X, int BI, int BU>
 void launch_many(const Product &p, hipStream_t stream) {
   const int64_t all =
       (p.items + 64 * BI - 1) / (64 * BI) * ((p.rows + 64 * BU - 1) / (64 * BU));
-  const dim3 groups((unsigned)std::min<int64_t>(all, 1024)), threads(kThreads);
+  constexpr int64_t kAtOnce = 256 * (BI * BU == 4 ? 3 : 4);
+  const dim3 groups((unsigned)std::min(all, kAtOnce)), threads(kThreads);
   if (p.k % 16)
     hipLaunchKernelGGL((k_product_many<O, X, BI, BU, true>), groups, threads, 0, stream, p, all);
   else
