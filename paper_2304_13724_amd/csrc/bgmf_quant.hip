@@ -424,7 +424,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_product_few(Product P) {
 // users, each wave a quarter of it in BI x BU blocks of v_mfma_i32_32x32x32_i8
 // (lane l holds 16 bytes of item or user l % 32).  STEP bytes of k at a time
 // pass through LDS, in 16-byte chunks whose place in a row is swizzled so that
-// eight lanes that read eight rows meet all banks.  items >= 64 BI; the users'
+// 16 lanes that read 16 rows meet all 64 banks (places by eight rows, as for 32
+// banks, cost a third of the LDS cycles in conflicts).  items >= 64 BI; the users'
 // bytes are allocated up to a multiple of kUserPad rows.
 constexpr int64_t kUserPad = 256;
 
@@ -438,8 +439,8 @@ struct Many {
   static constexpr int kScores = kWaves * 32 * kPitch * (int)sizeof(O) / 16;  // i32x4
 
   static __device__ __forceinline__ int at(int row, int c) {
-    if constexpr (STEP == 64) return row * 4 + (c ^ ((row >> 1) & 3));
-    else return row * 8 + (c ^ (row & 7));
+    if constexpr (STEP == 64) return row * 4 + (c ^ ((row >> 2) & 3));
+    else return row * 8 + (c ^ ((row >> 1) & 7));
   }
 
   // Tile t in the order in which workgroups take them: these go to the eight
