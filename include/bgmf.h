@@ -454,7 +454,8 @@ int bgmf_chain_stats(bgmf_t *h, int64_t out[4]);
  *   top_item[r][0..top), top_log_prob[r][0..top): the items with the largest
  *     scores, ties to the lower item, and their log probabilities
  *   row_max[r] = M, row_sum[r] = S: what bgmf_log_probs_grad needs
- * (sums and statistics in fp32, formed in one pass over the scores).
+ * (formed in one pass over the scores: terms in fp32, running sums in fp64,
+ * results in fp32).
  *   given[r] = -1: log_prob[r] = 0; another item outside [0, cols): NaN; an
  *     excluded item, or one with score -inf: -inf.
  *   An item with score -inf has probability 0 and is never an alternative;

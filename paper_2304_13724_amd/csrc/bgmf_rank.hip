@@ -432,6 +432,11 @@ __device__ __forceinline__ void write_row(const LogProbs &P, int64_t r, const So
 // One workgroup per row, or per part of a row.  Bound: HBM; the scores are
 // read once.  A thread takes kGroup vectors at a time (64 bytes in flight),
 // their maximum first, so that the running sums are rescaled once per group.
+// 4,001 x 10,007 fp32 without alternatives takes 29 us, 5.5 TB/s.  Choosing
+// them comes after a row's last score: 5 us for ten on each of 1,999 rows of
+// 18,000, all of which are on the GPU at once; these in bf16 with exclusions
+// take 31 us, and 26 without alternatives, bound by the vector units (some 14
+// cycles a score).
 constexpr int kGroup = kCols;
 template <class T, bool EX, bool TOP, int TH>
 __global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
@@ -532,7 +537,8 @@ struct PartSource {  // column q has the list of part q, larger scores first
   }
 };
 
-// Joins the parts of a row: one workgroup per row.
+// Joins the parts of a row: one workgroup per row.  Bound: latency (eight rows
+// of 153 parts with 50 alternatives each: 7 us).
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_log_probs_join(LogProbs P) {
   __shared__ SoftLds<kThreads> soft_lds;
@@ -571,7 +577,8 @@ __global__ void __launch_bounds__(kThreads) k_log_probs_join(LogProbs P) {
 
 // ---------------------------------------------------------------------------
 // Gradient: every score is read and its gradient written once.  A workgroup
-// takes a tile of one row at a time.  Bound: HBM.
+// takes a tile of one row at a time.  Bound: HBM: 4,096 x 18,000 fp32 take 104
+// us, 5.7 TB/s.
 // ---------------------------------------------------------------------------
 struct LogProbsGrad {
   const void *x;
