@@ -688,7 +688,7 @@ __global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4) k_product_many
 // do).  One workgroup fills a CU, so a wave itself reads its next 32 columns
 // from LDS while the matrix unit works, and a step's bytes are loaded a whole
 // step before they go to the other LDS buffer.  Bound: the matrix units, which
-// work 53% of the cycles; the clock falls to about 1.75 GHz meanwhile.  4,096 x
+// work 56% of the cycles; the clock falls to about 1.75 GHz meanwhile.  4,096 x
 // 8,192 x 4,096 takes 140 us, 2.0e15 operations a second (the library's int8
 // product of these sizes: 141 us).
 // Kinds of instructions that the scheduler is told to place.

@@ -87,6 +87,7 @@ class _LogProbs(torch.autograd.Function):
         return tuple(r)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, g_log_prob, g_entropy, *_):
         scores, given, excluded, row_max, row_sum, entropy = ctx.saved_tensors
         if g_log_prob is None and g_entropy is None:

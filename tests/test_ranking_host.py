@@ -117,3 +117,19 @@ def test_workspace_sizes_of_degenerate_calls():
     assert bgmf.bgmf_quantized_scores_workspace(0, 10, 64, F32) == 0
     assert bgmf.bgmf_quantized_scores_workspace(5, 10, -1, F32) == 0
     assert bgmf.bgmf_clip_grad_norm_workspace(-1) == 0
+
+
+def test_tensors_that_do_not_fit_are_refused_without_a_gpu():
+    import torch
+    from paper_2304_13724_amd import ranking
+    x = torch.zeros(4, 8)
+    for call in (lambda: ranking.log_probs(x), lambda: ranking.log_probs([1.0, 2.0]),
+                 lambda: ranking.log_probs(x.requires_grad_()),
+                 lambda: ranking.log_probs_backward(x, None, x[0], x[0], None, None),
+                 lambda: ranking.quantize_rows(x), lambda: ranking.quantize_rows(None),
+                 lambda: ranking.Catalogue(x), lambda: ranking.quantized_scores(x, x, x[0]),
+                 lambda: ranking.quantized_scores(x, x, x[0], dtype=torch.int8),
+                 lambda: ranking.clip_grad_norm([], 1.0), lambda: ranking.clip_grad_norm([x], 1.0),
+                 lambda: ranking.clip_grad_norm([None], 1.0)):
+        with pytest.raises(ValueError):
+            call()
