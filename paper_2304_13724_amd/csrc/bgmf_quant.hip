@@ -813,9 +813,9 @@ constexpr int64_t kFewUsers = 16, kFewItems = 128;
 // again, so with many of them the launch is cheaper (100 x 125,000, 1,954 tiles,
 // 14.1 us against 12.3; 2,048 x 18,000 24.7 against 20.3).
 bool takes_values(int64_t rows, int64_t items, int64_t k, int64_t items_bytes) {
-  if (k > 64) return false;
-  if (rows <= kFewUsers) return items_bytes >= 16;
-  return items >= kFewItems && (items + 127) / 128 * ((rows + 63) / 64) <= 1536;
+  if (k > 64 || items_bytes < 16) return false;  // (fewer bytes: k_product_tiny)
+  return rows <= kFewUsers ||
+         (items >= kFewItems && (items + 127) / 128 * ((rows + 63) / 64) <= 1536);
 }
 
 template <class O, class X, int BI, int BU>

@@ -311,3 +311,25 @@ def test_values_quantised_within_the_product(dtype, rows, items, k):
     w, b = quantized(v)
     want = product(q, a, w, b, torch.float32)
     assert torch.equal(one.cpu().nan_to_num(7.0), want.nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("rows", [1, 3, 20, 70, 300])
+@pytest.mark.parametrize("k", [3, 8, 16, 50, 64, 600])
+def test_broadcast_and_overlapping_items(rows, k):
+    """Item rows with a stride of 0 (one item's bytes, fewer than a load's 16
+    among them) and of 1."""
+    x = draw(rows, k, "f32", rows + k)
+    q, a = quantized(x)
+    line = torch.randint(-127, 128, (400 + k,), dtype=torch.int8,
+                         generator=torch.Generator().manual_seed(k))
+    for stride in (0, 1):
+        # the last item's last byte is the last of its memory
+        flat = line[:k + 299 * stride].clone()
+        b = torch.rand(300, generator=torch.Generator().manual_seed(1))
+        items = flat.as_strided((300, k), (stride, 1))
+        on = flat.cuda().as_strided((300, k), (stride, 1))
+        want = product(q, a, items.contiguous().numpy(), b.numpy(), torch.float32)
+        assert torch.equal(ranking.quantized_scores(x.cuda(), on, b.cuda()).cpu(), want)
+        got = ranking.quantized_scores(torch.from_numpy(q).cuda(), on, b.cuda(),
+                                       torch.from_numpy(a).cuda())
+        assert torch.equal(got.cpu(), want)
