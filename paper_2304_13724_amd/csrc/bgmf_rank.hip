@@ -68,14 +68,31 @@ struct Row {
       if (ex[i]) return -INFINITY;
     return to_float(x[i]);
   }
-  __device__ __forceinline__ void load(int32_t v, float (&out)[N]) const {
-    const Vec<T> a = load_vec(x + (int64_t)v * N);
-    uint8_t b[N];
-    if constexpr (EX) __builtin_memcpy(b, ex + (int64_t)v * N, N);
+  // A vector as it is in memory, and its scores: several are fetched before the
+  // first is looked at.
+  struct Raw {
+    Vec<T> a;
+    uint32_t b[EX ? N / 4 : 1];
+  };
+  __device__ __forceinline__ Raw fetch(int32_t v) const {
+    Raw r;
+    r.a = load_vec(x + (int64_t)v * N);
+    if constexpr (EX) __builtin_memcpy(r.b, ex + (int64_t)v * N, N);
+    return r;
+  }
+  static __device__ __forceinline__ Raw nothing() {  // scores of -inf
+    Raw r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r.a.v[i] = from_float<T>(-INFINITY);
+    if constexpr (EX)
+      for (int i = 0; i < N / 4; ++i) r.b[i] = 0;
+    return r;
+  }
+  static __device__ __forceinline__ void scores(const Raw &r, float (&out)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      out[i] = to_float(a.v[i]);
-      if constexpr (EX) out[i] = b[i] ? -INFINITY : out[i];
+      out[i] = to_float(r.a.v[i]);
+      if constexpr (EX) out[i] = r.b[i / 4] >> (i % 4 * 8) & 0xFF ? -INFINITY : out[i];
     }
   }
 };
@@ -374,7 +391,7 @@ struct RowSource {  // column q has vectors q, q + 4 TH, ..., and column q < TH 
     const int32_t v = q + (i - 1) * (kCols * TH);
     if (v >= vecs) return;
     float x[N];
-    row.load(v, x);
+    row.scores(row.fetch(v), x);
 #pragma unroll
     for (int e = 0; e < N; ++e) f(x[e], first + v * N + e);
   }
@@ -458,15 +475,21 @@ __global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
 #pragma unroll
     for (int g = 0; g < kCols; ++g) tm[g] = -INFINITY;
     const int32_t vecs = row.vecs();
-    for (int32_t v = tid; v < vecs; v += TH * kGroup) {
+    for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
+      typename Row<T, EX>::Raw raw[kGroup];
+      if (v0 + TH * kGroup <= vecs) {
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g) raw[g] = row.fetch(v0 + g * TH + tid);
+      } else {
+#pragma unroll
+        for (int g = 0; g < kGroup; ++g) {
+          raw[g] = Row<T, EX>::nothing();
+          if (v0 + g * TH + tid < vecs) raw[g] = row.fetch(v0 + g * TH + tid);
+        }
+      }
       float x[kGroup][N];
 #pragma unroll
-      for (int g = 0; g < kGroup; ++g) {
-        if (v + g * TH < vecs) row.load(v + g * TH, x[g]);
-        else
-#pragma unroll
-          for (int i = 0; i < N; ++i) x[g][i] = -INFINITY;
-      }
+      for (int g = 0; g < kGroup; ++g) Row<T, EX>::scores(raw[g], x[g]);
       float gm = -INFINITY;
 #pragma unroll
       for (int g = 0; g < kGroup; ++g) {
