@@ -487,19 +487,21 @@ __global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
           if (v0 + g * TH + tid < vecs) raw[g] = row.fetch(v0 + g * TH + tid);
         }
       }
-      float x[kGroup][N];
+      constexpr int kOnce = 16 / N;  // vectors whose scores are in registers at a time
 #pragma unroll
-      for (int g = 0; g < kGroup; ++g) Row<T, EX>::scores(raw[g], x[g]);
-      float gm = -INFINITY;
+      for (int g0 = 0; g0 < kGroup; g0 += kOnce) {
+        float x[kOnce][N], gm = -INFINITY;
 #pragma unroll
-      for (int g = 0; g < kGroup; ++g) {
-        float vm = x[g][0];
+        for (int g = 0; g < kOnce; ++g) {
+          Row<T, EX>::scores(raw[g0 + g], x[g]);
+          float vm = x[g][0];
 #pragma unroll
-        for (int i = 1; i < N; ++i) vm = fmaxf(vm, x[g][i]);
-        if constexpr (TOP) tm[g] = fmaxf(tm[g], vm);
-        gm = fmaxf(gm, vm);
+          for (int i = 1; i < N; ++i) vm = fmaxf(vm, x[g][i]);
+          if constexpr (TOP) tm[g0 + g] = fmaxf(tm[g0 + g], vm);
+          gm = fmaxf(gm, vm);
+        }
+        a.add(reinterpret_cast<float(&)[kOnce * N]>(x), gm, c);
       }
-      a.add(reinterpret_cast<float(&)[kGroup * N]>(x), gm, c);
     }
     if (tid < row.len - vecs * N) {
       const float x[1] = {row.one(vecs * N + tid)};
