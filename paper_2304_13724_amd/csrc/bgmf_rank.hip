@@ -452,7 +452,7 @@ __device__ __forceinline__ void write_row(const LogProbs &P, int64_t r, const So
 // 4,001 x 10,007 fp32 without alternatives takes 29 us, 5.5 TB/s.  Choosing
 // them comes after a row's last score: 5 us for ten on each of 1,999 rows of
 // 18,000, all of which are on the GPU at once; these in bf16 with exclusions
-// take 31 us, and 26 without alternatives, bound by the vector units (some 14
+// take 30 us, and 25 without alternatives, bound by the vector units (some 14
 // cycles a score).
 constexpr int kGroup = kCols;
 template <class T, bool EX, bool TOP, int TH>
