@@ -519,7 +519,8 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
 
 /* One gradient of bgmf_clip_grad_norm: a rows x cols matrix in (row stride
  * in_stride) and the place out of its clipped values (out_stride), which may
- * be in itself (with the same stride).  A vector is one row. */
+ * be in itself (with the same stride).  Both strides are at least cols.  A
+ * vector is one row. */
 typedef struct {
   const void *in;
   void *out;
