@@ -68,13 +68,13 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
 //
 // The slice is written back with device-scope (sc1) stores and staged in
 // with device-scope (sc1) loads, both coherent across the XCDs' L2 caches.
-// The writer waits for its stores to complete (vmcnt(0), the release fence
-// at workgroup scope) before it stores its progress word; the reader waits
-// for the progress word (and for that load to return) before it issues the
-// loads of the slice, and a workgroup-scope acquire fence keeps the compiler
-// from moving them earlier.  An agent-scope release/acquire fence would add
-// a write-back / invalidation of the whole L2 of the XCD; it is only needed
-// to publish or refresh plain cached accesses, and the hand-over uses none.
+// The writer waits for its stores to complete (vmcnt(0)) before it stores its
+// progress word; the reader waits for the progress word (and for that load to
+// return) before it issues the loads of the slice, and a workgroup-scope
+// acquire fence keeps the compiler from moving them earlier.  An agent-scope
+// release/acquire fence would add a write-back / invalidation of the whole L2
+// of the XCD; it is only needed to publish or refresh plain cached accesses,
+// and the hand-over uses none.
 constexpr int kCoherent = 16;  // cache-policy bits of a device-scope access (sc1)
 
 // Buffer descriptor word 3 for gfx9 (32-bit data format); accesses whose
@@ -219,9 +219,12 @@ __device__ __forceinline__ bool wait_lds_progress(volatile __attribute__((addres
 }
 
 // Publish progress: all earlier stores of the wave (the column slice) have
-// completed before the progress word is written.
+// completed before the progress word is written.  The wait is written out: a
+// release fence at workgroup scope has none for global memory, since the waves
+// of a workgroup share a CU's L1, and a slice still on its way when the word is
+// seen would be read as it was.
 __device__ __forceinline__ void publish_progress(int64_t *flag, int64_t value) {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __hip_atomic_store(flag, value, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
