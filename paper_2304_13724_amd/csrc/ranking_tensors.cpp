@@ -122,6 +122,15 @@ at::Tensor output(PyObject *o, const char *name, const at::Tensor &like, int64_t
   return t;
 }
 
+// A tensor of the caller's has been written: graphs that hold it from before
+// notice at their backward pass, as after PyTorch's in-place functions.
+void written(const at::Tensor &t) {
+  if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+void written(PyObject *o, const at::Tensor &t) {
+  if (o != Py_None) written(t);
+}
+
 double number(PyObject *o, const char *name) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) {
@@ -198,7 +207,9 @@ PyObject *log_probs_backward(PyObject *const *a) {
       x.const_data_ptr(), type, rows, cols, x.stride(0), ex, ex_stride,
       static_cast<const int32_t *>(given), (float)number(a[7], "temperature"), row_max, row_sum,
       entropy, g_log_prob, g_entropy, out.mutable_data_ptr(), out.stride(0), stream_of(a[10]));
-  return rc == BGMF_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[9], out);
+  return THPVariable_Wrap(out);
 }
 
 // (x, stream) -> (q, scale); the rows of q start on 16-byte boundaries
@@ -240,7 +251,9 @@ PyObject *quantized_scores(PyObject *const *a) {
       static_cast<const int8_t *>(items.const_data_ptr()), m, items.stride(0),
       static_cast<const float *>(item_scale), out.mutable_data_ptr(), out_type, out.stride(0),
       ws_bytes ? ws.mutable_data_ptr() : nullptr, ws_bytes, stream_of(a[6]));
-  return rc == BGMF_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[5], out);
+  return THPVariable_Wrap(out);
 }
 
 // rows x cols with a row stride that cover a gradient's elements.
@@ -289,7 +302,10 @@ PyObject *clip_grad_norm(PyObject *const *a) {
   const int rc = bgmf_clip_grad_norm(table.data(), count, (float)number(a[1], "max_norm"),
                                      at_<float>(norm), ws.mutable_data_ptr(), ws_bytes,
                                      stream_of(a[3]));
-  return rc == BGMF_OK ? THPVariable_Wrap(norm) : PyLong_FromLong(rc);
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  PyObject *outs = in_place ? a[0] : a[2];
+  for (Py_ssize_t i = 0; i < count; ++i) written(THPVariable_Unpack(PyList_GET_ITEM(outs, i)));
+  return THPVariable_Wrap(norm);
 }
 
 // Argument count, and C++ exceptions as Python's.

@@ -1,0 +1,66 @@
+"""The ranking calls as PyTorch's own functions behave beside autograd: writes
+into tensors of the caller's are seen by earlier graphs."""
+import pytest
+
+from paper_2304_13724_amd import ranking
+
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+def scores(rows=4, cols=50):
+    g = torch.Generator().manual_seed(rows + cols)
+    return torch.randn(rows, cols, generator=g).cuda()
+
+
+GIVEN = [1, 2, 3, -1]
+
+
+# --- writes into the caller's tensors -------------------------------------------
+
+def test_backward_after_the_scores_were_overwritten_raises():
+    leaf = scores().requires_grad_()
+    x = leaf * 1  # not a leaf: what a model computes
+    given = torch.tensor(GIVEN).int().cuda()
+    r = ranking.log_probs(x, given)
+    with torch.no_grad():
+        ranking.log_probs_backward(x, given, r.row_max, r.row_sum, None, torch.ones(4).cuda(), out=x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        r.log_prob.sum().backward()
+
+
+def test_written_tensors_have_a_new_version():
+    x = scores()
+    given = torch.tensor(GIVEN).int().cuda()
+    r = ranking.log_probs(x, given)
+    gl = torch.ones(4).cuda()
+    before = [t._version for t in (x, given, r.row_max, r.row_sum, gl)]
+    out = torch.empty_like(x)
+    ranking.log_probs_backward(x, given, r.row_max, r.row_sum, None, gl, out=out)
+    assert out._version == 1
+    assert [t._version for t in (x, given, r.row_max, r.row_sum, gl)] == before
+
+    c = ranking.Catalogue(torch.ones(5, 50).cuda())
+    to = torch.empty(4, 5).cuda()
+    ranking.quantized_scores(x, c.items, c.scale, out=to)
+    assert (to._version, x._version, c.items._version) == (1, before[0], 0)
+
+    bucket = torch.ones(12).cuda()
+    grads = list(bucket.split([5, 7]))
+    ranking.clip_grad_norm(grads, 1.0)
+    assert bucket._version == 2  # one write for each view
+    clipped = [torch.empty_like(t) for t in grads]
+    ranking.clip_grad_norm(grads, 1.0, out=clipped)
+    assert bucket._version == 2 and [t._version for t in clipped] == [1, 1]
+
+
+def test_tensors_of_inference_mode_can_be_written():
+    """They have no version, and no graph can hold them."""
+    with torch.inference_mode():
+        g = torch.full((9,), 2.0, device="cuda")
+    ranking.clip_grad_norm([g], 1.0)
+    assert torch.allclose(g, torch.full((9,), 1 / 3, device="cuda"))
+    with torch.inference_mode():
+        ranking.clip_grad_norm([g], 0.5)
+        assert torch.allclose(g, torch.full((9,), 1 / 6, device="cuda"))
