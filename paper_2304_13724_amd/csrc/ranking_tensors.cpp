@@ -56,10 +56,14 @@ at::ScalarType dtype_of(int type) {
   return type == BGMF_TYPE_F32 ? at::kFloat : type == BGMF_TYPE_BF16 ? at::kBFloat16 : at::kHalf;
 }
 
-// The tensor behind a Python object, which keeps it alive during the call.
+// The tensor behind a Python object, which keeps it alive during the call.  No
+// call has a forward-mode derivative, and none drops a tangent silently.
 const at::Tensor &tensor(PyObject *o, const char *name) {
   if (!THPVariable_Check(o)) refuse("%s must be a tensor", name);
-  return THPVariable_Unpack(o);
+  const at::Tensor &t = THPVariable_Unpack(o);
+  if (t._fw_grad(0).defined())
+    refuse("%s has a tangent: forward-mode derivatives are not supported", name);
+  return t;
 }
 
 // A 2-D tensor on the GPU of one of the types, the elements of a row adjacent.

@@ -5,6 +5,7 @@ import pytest
 from paper_2304_13724_amd import ranking
 
 import torch
+import torch.autograd.forward_ad as forward_ad
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +65,15 @@ def test_tensors_of_inference_mode_can_be_written():
     with torch.inference_mode():
         ranking.clip_grad_norm([g], 0.5)
         assert torch.allclose(g, torch.full((9,), 1 / 6, device="cuda"))
+
+
+# --- forward mode ----------------------------------------------------------------
+
+@pytest.mark.parametrize("needs_grad", [False, True])
+def test_a_tangent_is_refused(needs_grad):
+    x = scores().requires_grad_(needs_grad)
+    given = torch.tensor(GIVEN).int().cuda()
+    with forward_ad.dual_level():
+        with pytest.raises((ValueError, RuntimeError), match="tangent|jvp"):
+            ranking.log_probs(forward_ad.make_dual(x, torch.ones_like(x)), given)
+        assert torch.isfinite(ranking.log_probs(x, given).log_prob).all()
