@@ -63,6 +63,8 @@ const at::Tensor &tensor(PyObject *o, const char *name) {
   const at::Tensor &t = THPVariable_Unpack(o);
   if (t._fw_grad(0).defined())
     refuse("%s has a tangent: forward-mode derivatives are not supported", name);
+  if (t.is_neg() || t._is_zerotensor())
+    refuse("%s: its memory does not hold its values (call .resolve_neg() or .clone())", name);
   return t;
 }
 

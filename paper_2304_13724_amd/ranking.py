@@ -92,7 +92,7 @@ class _LogProbs(torch.autograd.Function):
         scores, given, excluded, row_max, row_sum, entropy = ctx.saved_tensors
         if g_log_prob is None and g_entropy is None:
             return None, None, None, None, None
-        g = [None if x is None else x.contiguous() for x in (g_log_prob, g_entropy)]
+        g = [None if x is None else x.resolve_neg().contiguous() for x in (g_log_prob, g_entropy)]
         if given is None:
             g[0] = None
         grad = log_probs_backward(scores, given, row_max, row_sum, entropy, g[0], g[1],

@@ -77,3 +77,17 @@ def test_a_tangent_is_refused(needs_grad):
         with pytest.raises((ValueError, RuntimeError), match="tangent|jvp"):
             ranking.log_probs(forward_ad.make_dual(x, torch.ones_like(x)), given)
         assert torch.isfinite(ranking.log_probs(x, given).log_prob).all()
+
+
+# --- gradients as autograd may pass them -----------------------------------------
+
+def test_gradients_that_negate_their_memory_or_are_broadcast():
+    given = torch.tensor(GIVEN).int().cuda()
+    got = []
+    for g in (torch._neg_view(torch.ones(4).cuda()), torch.full((1,), -1.0).cuda().expand(4),
+              -torch.ones(4).cuda()):
+        leaf = scores().requires_grad_()
+        r = ranking.log_probs(leaf, given)
+        torch.autograd.backward([r.log_prob, r.entropy], [g, g])
+        got.append(leaf.grad)
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[2])

@@ -28,3 +28,13 @@ def test_a_tangent_is_refused():
         for call in calls(lambda t: forward_ad.make_dual(t, torch.ones_like(t))):
             with pytest.raises(ValueError, match="tangent"):
                 call()
+
+
+def test_tensors_whose_memory_is_not_their_values_are_refused():
+    """A view that negates its memory (the imaginary part of a conjugated
+    tensor), and a tensor of zeros without memory."""
+    for change in (torch._neg_view, lambda t: torch._efficientzerotensor(t.shape),
+                   lambda t: torch.zeros(*t.shape, dtype=torch.complex64).conj().imag):
+        for call in calls(change):
+            with pytest.raises(ValueError, match="memory"):
+                call()
