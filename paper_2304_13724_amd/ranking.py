@@ -55,6 +55,42 @@ def _checked(result):
     return result
 
 
+def _in_graph(*tensors) -> bool:
+    """Whether autograd would want the derivative of a call on these tensors."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                return True
+    return False
+
+
+class _NoDerivative(torch.autograd.Function):
+    """Results of a call that has no derivative: a backward pass that reaches
+    them raises, as with PyTorch's functions that have none."""
+    @staticmethod
+    def forward(ctx, name, call, *tensors):
+        ctx.name = name
+        results = call()
+        for r in results if isinstance(results, tuple) else (results,):
+            if not r.is_floating_point():
+                ctx.mark_non_differentiable(r)
+        return results
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError(f"{ctx.name} has no derivative: call it under torch.no_grad(), or on "
+                           "detached tensors")
+
+
+def _without_derivative(name, call, out, *tensors):
+    if not _in_graph(*tensors):
+        return _checked(call())
+    if out is not None:
+        raise ValueError(f"{name}: out takes no part in a graph, and one of the tensors requires "
+                         "grad")
+    return _NoDerivative.apply(name, lambda: _checked(call()), *tensors)
+
+
 # --- log probabilities ----------------------------------------------------------
 
 def _forward(scores, given, top, temperature, excluded) -> LogProbs:
@@ -70,10 +106,13 @@ def log_probs_backward(scores: torch.Tensor, given: Optional[torch.Tensor], row_
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient with respect to the scores of a loss whose gradients with
     respect to ``log_prob`` and ``entropy`` are given (None: zero), from the
-    results of ``log_probs``.  ``out`` may be the scores themselves."""
-    return _checked(_ranking.log_probs_backward(
-        scores, given, row_max, row_sum, entropy, grad_log_prob, grad_entropy, temperature,
-        excluded, out, _stream(scores)))
+    results of ``log_probs``.  ``out`` may be the scores themselves.  Has no
+    derivative of its own."""
+    return _without_derivative(
+        "log_probs_backward", lambda: _ranking.log_probs_backward(
+            scores, given, row_max, row_sum, entropy, grad_log_prob, grad_entropy, temperature,
+            excluded, out, _stream(scores)),
+        out, scores, row_max, row_sum, entropy, grad_log_prob, grad_entropy)
 
 
 class _LogProbs(torch.autograd.Function):
@@ -119,8 +158,10 @@ def log_probs(scores: torch.Tensor, given: Optional[torch.Tensor] = None, *, top
 def quantize_rows(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
     """Rows in 8-bit integers: (q int8, scale float32) with x ~ q * scale,
     scale the row's largest magnitude / 127.  The rows of q start on 16-byte
-    boundaries (q is a view of a wider tensor where k needs it)."""
-    return _checked(_ranking.quantize_rows(x, _stream(x)))
+    boundaries (q is a view of a wider tensor where k needs it).  Has no
+    derivative."""
+    return _without_derivative("quantize_rows", lambda: _ranking.quantize_rows(x, _stream(x)),
+                               None, x)
 
 
 def quantized_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.Tensor,
@@ -130,12 +171,15 @@ def quantized_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.
     """Scores rows . items^T with both in 8-bit integers, times row_scale and
     item_scale, as ``dtype``.  ``rows``: int8 with ``row_scale``, or float32,
     bfloat16 or float16 without it, quantised in the call as by
-    ``quantize_rows``.  ``items``: int8 with ``item_scale``."""
+    ``quantize_rows``.  ``items``: int8 with ``item_scale``.  Has no
+    derivative."""
     code = _TYPES.get(dtype)
     if code is None:
         raise ValueError(f"dtype must be float32, bfloat16 or float16: {dtype}")
-    return _checked(_ranking.quantized_scores(rows, items, item_scale, row_scale, code, out,
-                                              _stream(rows)))
+    return _without_derivative(
+        "quantized_scores", lambda: _ranking.quantized_scores(
+            rows, items, item_scale, row_scale, code, out, _stream(rows)),
+        out, rows, item_scale, row_scale)
 
 
 class Catalogue:
@@ -152,7 +196,8 @@ class Catalogue:
     def rank(self, users: torch.Tensor, given: Optional[torch.Tensor] = None, *, top: int = 10,
              temperature: float = 1.0, excluded: Optional[torch.Tensor] = None) -> LogProbs:
         """The best items for each user, with the log probability of a given
-        item and the entropy, as by ``log_probs``."""
+        item and the entropy, as by ``log_probs``, but without a derivative
+        with respect to the users: the scores are in 8-bit integers."""
         return log_probs(self.scores(users), given, top=top, temperature=temperature,
                          excluded=excluded)
 

@@ -1,5 +1,6 @@
-"""The ranking calls as PyTorch's own functions behave beside autograd: writes
-into tensors of the caller's are seen by earlier graphs."""
+"""The ranking calls behave beside autograd as PyTorch's own functions do: writes
+into tensors of the caller's are seen by earlier graphs, and no derivative is
+dropped silently."""
 import pytest
 
 from paper_2304_13724_amd import ranking
@@ -91,3 +92,60 @@ def test_gradients_that_negate_their_memory_or_are_broadcast():
         torch.autograd.backward([r.log_prob, r.entropy], [g, g])
         got.append(leaf.grad)
     assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[2])
+
+
+# --- results without a derivative -----------------------------------------------
+
+def test_scores_in_8_bit_integers_have_no_derivative_and_say_so():
+    users, items = scores(3, 64).requires_grad_(), scores(7, 64)
+    c = ranking.Catalogue(items)
+    s = c.scores(users)
+    want = c.scores(users.detach())
+    assert s.requires_grad and not want.requires_grad and torch.equal(s.detach(), want)
+    with pytest.raises(RuntimeError, match="derivative"):
+        s.sum().backward()
+    r = c.rank(users, torch.tensor([1, 2, 3]).int().cuda(), top=2)
+    with pytest.raises(RuntimeError, match="derivative"):
+        r.log_prob.sum().backward()
+    # the scales: of the items, and of users' rows
+    q, a = ranking.quantize_rows(users)
+    assert a.requires_grad and not q.requires_grad
+    with pytest.raises(RuntimeError, match="derivative"):
+        a.sum().backward()
+    with pytest.raises(RuntimeError, match="derivative"):
+        ranking.quantized_scores(q, c.items, c.scale, a).sum().backward()
+    learned = ranking.Catalogue(items.clone().requires_grad_())
+    with pytest.raises(RuntimeError, match="derivative"):
+        learned.scores(users.detach()).sum().backward()
+    with torch.no_grad():
+        assert not c.scores(users).requires_grad and not c.rank(users).log_prob.requires_grad
+        assert not ranking.quantize_rows(users)[1].requires_grad
+
+
+def test_given_outputs_take_no_part_in_a_graph():
+    users, items = scores(3, 64).requires_grad_(), scores(7, 64)
+    c = ranking.Catalogue(items)
+    to = torch.empty(3, 7, device="cuda")
+    with pytest.raises(ValueError, match="out"):
+        ranking.quantized_scores(users, c.items, c.scale, out=to)
+    with torch.no_grad():
+        ranking.quantized_scores(users, c.items, c.scale, out=to)
+    assert torch.equal(to, c.scores(users.detach()))
+
+
+def test_the_backward_call_has_no_derivative_and_says_so():
+    x = scores().requires_grad_()
+    given = torch.tensor(GIVEN).int().cuda()
+    r = ranking.log_probs(x.detach(), given)
+    gl = torch.ones(4).cuda()
+    d = ranking.log_probs_backward(x, given, r.row_max, r.row_sum, None, gl)
+    want = ranking.log_probs_backward(x.detach(), given, r.row_max, r.row_sum, None, gl)
+    assert torch.equal(d.detach(), want) and not want.requires_grad
+    with pytest.raises(RuntimeError, match="derivative"):
+        d.sum().backward()
+    with pytest.raises(RuntimeError, match="derivative"):
+        ranking.log_probs_backward(x.detach(), given, r.row_max, r.row_sum, None,
+                                   gl.clone().requires_grad_()).sum().backward()
+    with pytest.raises(ValueError, match="out"):
+        ranking.log_probs_backward(x, given, r.row_max, r.row_sum, None, gl,
+                                   out=torch.empty_like(want))
