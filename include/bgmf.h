@@ -536,8 +536,9 @@ typedef struct {
  * with the squares summed in fp64 in a fixed order, and the factor in fp32.
  * A norm that is NaN or infinite leaves the gradients as they are (out = g):
  * the caller reads *norm.  max_norm >= 0, not NaN (infinity: never clips).
- * No out may overlap another gradient.  More than 2^43 elements or 2^30
- * gradients: BGMF_E_UNSUPPORTED. */
+ * An out that meets another gradient's in or out, or its own in without being
+ * it: BGMF_E_ARG (their extents may interleave, as columns of one matrix do).
+ * More than 2^43 elements or 2^30 gradients: BGMF_E_UNSUPPORTED. */
 int64_t bgmf_clip_grad_norm_workspace(int64_t count);
 int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm, float *norm,
                         void *ws, int64_t ws_bytes, void *hip_stream);

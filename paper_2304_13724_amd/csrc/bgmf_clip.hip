@@ -1,6 +1,8 @@
 // Clipping of many gradients by their global norm (bgmf_clip_grad_norm).
 #include <algorithm>
 #include <cmath>
+#include <memory>
+#include <new>
 
 #include "bgmf_rank.h"
 
@@ -211,6 +213,122 @@ __global__ void __launch_bounds__(kThreads) k_clip(const Slot *table, int32_t co
 
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
 
+// ---------------------------------------------------------------------------
+// Whether gradients share memory.  One that is written while another's chunks
+// are read or written would come out scaled once or twice, as it happens.
+// ---------------------------------------------------------------------------
+
+// Rows of `bytes` bytes, `stride` apart, from lo on; the last ends at hi.
+struct Region {
+  int64_t lo, hi, bytes, stride, rows;
+  int32_t grad;
+  bool written;
+};
+
+// Whether row i of a meets a row of b: the first of b's rows that ends past its
+// start begins before its end.
+bool row_meets(const Region &a, int64_t i, const Region &b) {
+  const int64_t lo = a.lo + i * a.stride, past = lo - b.lo - b.bytes;
+  const int64_t row = past < 0 ? 0 : past / b.stride + 1;
+  return row < b.rows && b.lo + row * b.stride < lo + a.bytes;
+}
+
+bool meets(const Region &a, const Region &b) {
+  if (a.hi <= b.lo || b.hi <= a.lo) return false;
+  if (a.rows > b.rows) return meets(b, a);
+  if (a.rows > 1 && a.stride == b.stride) {
+    // rows of a that lie before b's second row all look at b's first one, and
+    // the last of them comes nearest; the later ones look at rows of b that
+    // are as far from them as the first of them is
+    const int64_t before = b.lo + b.bytes - a.lo, rows = a.rows;
+    const int64_t later = before <= 0 ? 0 : (before + a.stride - 1) / a.stride;
+    return (later > 0 && row_meets(a, std::min(later, rows) - 1, b)) ||
+           (later < rows && row_meets(a, later, b));
+  }
+  for (int64_t i = 0; i < a.rows; ++i)
+    if (row_meets(a, i, b)) return true;
+  return false;
+}
+
+// The first pair of gradients found of which one is written where the other
+// lies (or one whose out meets its own in without being it); 0 if there is
+// none, -1 without memory for the check.  Gradients in the order of their
+// addresses, such as the parts of a bucket, are only compared with the one
+// before; others are sorted (3 us more for 211 in place).
+int shared_memory(const bgmf_grad_t *grads, int64_t count, int64_t *first, int64_t *second) {
+  const auto region = [&](int64_t i, bool written) {
+    const bgmf_grad_t &g = grads[i];
+    const int64_t size = type_bytes(g.type);
+    Region r;
+    r.lo = reinterpret_cast<int64_t>(written ? g.out : g.in);
+    r.bytes = g.cols * size;
+    r.stride = g.rows > 1 ? (written ? g.out_stride : g.in_stride) * size : r.bytes;
+    r.rows = g.rows;
+    r.hi = r.lo + (r.rows - 1) * r.stride + r.bytes;
+    r.grad = (int32_t)i, r.written = written;
+    return r;
+  };
+  int64_t some = 0, in_lo = INT64_MAX, in_hi = 0, out_lo = INT64_MAX, out_hi = 0, last = 0;
+  bool ordered = true, in_place = true;
+  for (int64_t i = 0; i < count; ++i) {
+    if (grads[i].rows == 0 || grads[i].cols == 0) continue;
+    const Region w = region(i, true);
+    ordered &= w.lo >= last;
+    last = w.hi;
+    out_lo = std::min(out_lo, w.lo), out_hi = std::max(out_hi, w.hi);
+    if (grads[i].in != grads[i].out) {
+      const Region r = region(i, false);
+      in_lo = std::min(in_lo, r.lo), in_hi = std::max(in_hi, r.hi);
+      in_place = false;
+    }
+    ++some;
+  }
+  if (ordered && (in_place || in_hi <= out_lo || out_hi <= in_lo)) return 0;
+  const std::unique_ptr<Region[]> all(new (std::nothrow) Region[2 * some]);
+  const std::unique_ptr<int64_t[]> open(new (std::nothrow) int64_t[2 * some]);
+  if (!all || !open) return -1;
+  int64_t n = 0;
+  for (int64_t i = 0; i < count; ++i) {
+    if (grads[i].rows == 0 || grads[i].cols == 0) continue;
+    all[n++] = region(i, true);
+    if (grads[i].in != grads[i].out) all[n++] = region(i, false);
+  }
+  std::sort(all.get(), all.get() + n, [](const Region &a, const Region &b) { return a.lo < b.lo; });
+  // open: the regions before i that end past its start, the written ones from
+  // the front, the others from the back
+  int64_t written = 0, read = 0;
+  for (int64_t i = 0; i < n; ++i) {
+    const Region &r = all[i];
+    int64_t keep = 0;
+    for (int64_t q = 0; q < written; ++q) {
+      const Region &w = all[open[q]];
+      if (w.hi <= r.lo) continue;
+      open[keep++] = open[q];
+      if (meets(w, r)) {
+        *first = std::min(w.grad, r.grad), *second = std::max(w.grad, r.grad);
+        return 1;
+      }
+    }
+    written = keep, keep = 0;
+    if (r.written) {
+      for (int64_t q = 0; q < read; ++q) {
+        const int64_t at = open[2 * some - 1 - q];
+        if (all[at].hi <= r.lo) continue;
+        open[2 * some - 1 - keep++] = at;
+        if (meets(all[at], r)) {
+          *first = std::min(all[at].grad, r.grad), *second = std::max(all[at].grad, r.grad);
+          return 1;
+        }
+      }
+      read = keep;
+      open[written++] = i;
+    } else {
+      open[2 * some - 1 - read++] = i;
+    }
+  }
+  return 0;
+}
+
 }  // namespace
 }  // namespace bgmfk
 
@@ -231,12 +349,6 @@ int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm,
   if (!(max_norm >= 0.0f))
     return fail_call(BGMF_E_ARG, "%s: max_norm must be at least 0: %g", call, max_norm);
   if (!norm) return fail_call(BGMF_E_ARG, "%s: null norm", call);
-  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256)
-    return fail_call(BGMF_E_ARG, "%s: the workspace must start on a 256-byte boundary", call);
-  const int64_t need = bgmf_clip_grad_norm_workspace(count);
-  if (ws_bytes < need)
-    return fail_call(BGMF_E_BUDGET, "%s: the workspace has %lld bytes, %lld are needed", call,
-                     (long long)ws_bytes, (long long)need);
   for (int64_t i = 0; i < count; ++i) {
     const bgmf_grad_t &g = grads[i];
     if (!is_float_type(g.type))
@@ -253,15 +365,27 @@ int bgmf_clip_grad_norm(const bgmf_grad_t *grads, int64_t count, float max_norm,
       return fail_call(BGMF_E_ARG, "%s: gradient %lld: in place, the row strides must be equal",
                        call, (long long)i);
   }
-  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  double *partial = static_cast<double *>(ws);
-  Slot *table = reinterpret_cast<Slot *>(static_cast<char *>(ws) + padded(kGroups * 8));
   int64_t total = 0;
   for (int64_t i = 0; i < count; ++i) {
     total += (grads[i].rows * grads[i].cols + kChunk - 1) / kChunk;
     if (total >= kPast - (1 << 20) || count >= (1 << 30))
       return fail_call(BGMF_E_UNSUPPORTED, "%s: more than 2^43 elements or 2^30 gradients", call);
   }
+  int64_t first = 0, second = 0;
+  if (const int shared = shared_memory(grads, count, &first, &second))
+    return shared < 0 ? fail_call(BGMF_E_NOMEM, "%s: out of host memory", call)
+                      : fail_call(BGMF_E_ARG,
+                                  "%s: gradients %lld and %lld share memory that is written", call,
+                                  (long long)first, (long long)second);
+  if (!ws || reinterpret_cast<uintptr_t>(ws) % 256)
+    return fail_call(BGMF_E_ARG, "%s: the workspace must start on a 256-byte boundary", call);
+  const int64_t need = bgmf_clip_grad_norm_workspace(count);
+  if (ws_bytes < need)
+    return fail_call(BGMF_E_BUDGET, "%s: the workspace has %lld bytes, %lld are needed", call,
+                     (long long)ws_bytes, (long long)need);
+  hipStream_t stream = static_cast<hipStream_t>(hip_stream);
+  double *partial = static_cast<double *>(ws);
+  Slot *table = reinterpret_cast<Slot *>(static_cast<char *>(ws) + padded(kGroups * 8));
   int32_t chunks = 0, slots = 0, held = 0;
   Batch b;
   const auto send = [&] {

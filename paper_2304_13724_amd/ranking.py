@@ -210,7 +210,8 @@ def clip_grad_norm(grads: Sequence[torch.Tensor], max_norm: float,
     their global norm is at most max_norm, in place or into ``out``; returns
     the norm before (a float32 tensor on the GPU).  A norm that is not finite
     leaves the gradients as they are.  Each must be contiguous, or 2-D with
-    adjacent row elements."""
+    adjacent row elements, and none may share written memory with another (the
+    same gradient twice, say): BgmfError.  The results are in no graph."""
     grads = list(grads)
     return _checked(_ranking.clip_grad_norm(grads, max_norm, None if out is None else list(out),
                                             _stream(grads[0]) if grads else 0))
