@@ -429,6 +429,10 @@ int bgmf_chain_stats(bgmf_t *h, int64_t out[4]);
  *   - A workspace (ws) starts on a 256-byte boundary and has at least the
  *     bytes that the call's ..._workspace function returns for the same
  *     sizes; what it holds before and after is of no meaning.
+ *   - An output may share no element with an input or another output, but
+ *     where a description allows it (a matrix's rows may interleave with
+ *     another's, as columns of one wider matrix do).  For grad_scores, out and
+ *     q this is checked.
  *   - Sizes of zero are valid and do what the formulas say of empty sums.
  *   - Errors are reported by bgmf_last_error(NULL).  BGMF_E_ARG for what the
  *     descriptions exclude, BGMF_E_BUDGET for a workspace that is too small.

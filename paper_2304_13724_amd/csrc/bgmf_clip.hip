@@ -217,38 +217,10 @@ int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
 // Whether gradients share memory.  One that is written while another's chunks
 // are read or written would come out scaled once or twice, as it happens.
 // ---------------------------------------------------------------------------
-
-// Rows of `bytes` bytes, `stride` apart, from lo on; the last ends at hi.
-struct Region {
-  int64_t lo, hi, bytes, stride, rows;
+struct GradRegion : Region {
   int32_t grad;
   bool written;
 };
-
-// Whether row i of a meets a row of b: the first of b's rows that ends past its
-// start begins before its end.
-bool row_meets(const Region &a, int64_t i, const Region &b) {
-  const int64_t lo = a.lo + i * a.stride, past = lo - b.lo - b.bytes;
-  const int64_t row = past < 0 ? 0 : past / b.stride + 1;
-  return row < b.rows && b.lo + row * b.stride < lo + a.bytes;
-}
-
-bool meets(const Region &a, const Region &b) {
-  if (a.hi <= b.lo || b.hi <= a.lo) return false;
-  if (a.rows > b.rows) return meets(b, a);
-  if (a.rows > 1 && a.stride == b.stride) {
-    // rows of a that lie before b's second row all look at b's first one, and
-    // the last of them comes nearest; the later ones look at rows of b that
-    // are as far from them as the first of them is
-    const int64_t before = b.lo + b.bytes - a.lo, rows = a.rows;
-    const int64_t later = before <= 0 ? 0 : (before + a.stride - 1) / a.stride;
-    return (later > 0 && row_meets(a, std::min(later, rows) - 1, b)) ||
-           (later < rows && row_meets(a, later, b));
-  }
-  for (int64_t i = 0; i < a.rows; ++i)
-    if (row_meets(a, i, b)) return true;
-  return false;
-}
 
 // The first pair of gradients found of which one is written where the other
 // lies (or one whose out meets its own in without being it); 0 if there is
@@ -258,33 +230,27 @@ bool meets(const Region &a, const Region &b) {
 int shared_memory(const bgmf_grad_t *grads, int64_t count, int64_t *first, int64_t *second) {
   const auto region = [&](int64_t i, bool written) {
     const bgmf_grad_t &g = grads[i];
-    const int64_t size = type_bytes(g.type);
-    Region r;
-    r.lo = reinterpret_cast<int64_t>(written ? g.out : g.in);
-    r.bytes = g.cols * size;
-    r.stride = g.rows > 1 ? (written ? g.out_stride : g.in_stride) * size : r.bytes;
-    r.rows = g.rows;
-    r.hi = r.lo + (r.rows - 1) * r.stride + r.bytes;
-    r.grad = (int32_t)i, r.written = written;
-    return r;
+    return GradRegion{written ? region_of(g.out, g.type, g.rows, g.cols, g.out_stride)
+                              : region_of(g.in, g.type, g.rows, g.cols, g.in_stride),
+                      (int32_t)i, written};
   };
   int64_t some = 0, in_lo = INT64_MAX, in_hi = 0, out_lo = INT64_MAX, out_hi = 0, last = 0;
   bool ordered = true, in_place = true;
   for (int64_t i = 0; i < count; ++i) {
     if (grads[i].rows == 0 || grads[i].cols == 0) continue;
-    const Region w = region(i, true);
+    const GradRegion w = region(i, true);
     ordered &= w.lo >= last;
     last = w.hi;
     out_lo = std::min(out_lo, w.lo), out_hi = std::max(out_hi, w.hi);
     if (grads[i].in != grads[i].out) {
-      const Region r = region(i, false);
+      const GradRegion r = region(i, false);
       in_lo = std::min(in_lo, r.lo), in_hi = std::max(in_hi, r.hi);
       in_place = false;
     }
     ++some;
   }
   if (ordered && (in_place || in_hi <= out_lo || out_hi <= in_lo)) return 0;
-  const std::unique_ptr<Region[]> all(new (std::nothrow) Region[2 * some]);
+  const std::unique_ptr<GradRegion[]> all(new (std::nothrow) GradRegion[2 * some]);
   const std::unique_ptr<int64_t[]> open(new (std::nothrow) int64_t[2 * some]);
   if (!all || !open) return -1;
   int64_t n = 0;
@@ -298,10 +264,10 @@ int shared_memory(const bgmf_grad_t *grads, int64_t count, int64_t *first, int64
   // the front, the others from the back
   int64_t written = 0, read = 0;
   for (int64_t i = 0; i < n; ++i) {
-    const Region &r = all[i];
+    const GradRegion &r = all[i];
     int64_t keep = 0;
     for (int64_t q = 0; q < written; ++q) {
-      const Region &w = all[open[q]];
+      const GradRegion &w = all[open[q]];
       if (w.hi <= r.lo) continue;
       open[keep++] = open[q];
       if (meets(w, r)) {

@@ -921,6 +921,10 @@ int bgmf_quantize_rows(const void *x, int32_t type, int64_t rows, int64_t k, int
                      (long long)q_stride);
   if (rows == 0) return BGMF_OK;
   if (!scale) return fail_call(BGMF_E_ARG, "%s: null scale", call);
+  if (share(q, BGMF_TYPE_I8, rows, k, q_stride, x, type, rows, k, row_stride) ||
+      share(scale, BGMF_TYPE_F32, 1, rows, rows, x, type, rows, k, row_stride) ||
+      share(scale, BGMF_TYPE_F32, 1, rows, rows, q, BGMF_TYPE_I8, rows, k, q_stride))
+    return fail_call(BGMF_E_ARG, "%s: q or scale shares memory with another argument", call);
   const hipError_t e = quantize_by_type(type, x, rows, (int32_t)k, row_stride, q, q_stride,
                                         (int32_t)k, scale, static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return fail_call(BGMF_E_HIP, "%s: %s", call, hipGetErrorString(e));
@@ -969,6 +973,15 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
   if (ws_bytes < need)
     return fail_call(BGMF_E_BUDGET, "%s: the workspace has %lld bytes, %lld are needed", call,
                      (long long)ws_bytes, (long long)need);
+  const auto shares = [&](const void *y, int32_t y_type, int64_t y_rows, int64_t y_cols,
+                          int64_t y_stride) {
+    return share(out, out_type, rows, item_count, out_stride, y, y_type, y_rows, y_cols, y_stride);
+  };
+  if (shares(x, type, rows, k, row_stride) ||
+      shares(items, BGMF_TYPE_I8, item_count, k, items_stride) ||
+      shares(row_scale, BGMF_TYPE_F32, 1, rows, rows) ||
+      shares(item_scale, BGMF_TYPE_F32, 1, item_count, item_count))
+    return fail_call(BGMF_E_ARG, "%s: out shares memory with an input", call);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const int32_t kp = (int32_t)round_up(k, kUnit);
   int8_t *q = static_cast<int8_t *>(ws);

@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/bgmf.h"
 
 namespace bgmfk {
@@ -27,6 +29,58 @@ inline bool bad_matrix(const void *p, int64_t rows, int64_t cols, int64_t stride
   if (rows <= 0 || cols <= 0) return false;
   if (!p || reinterpret_cast<uintptr_t>(p) % (uintptr_t)esize) return true;
   return rows > 1 && (stride < min_stride || stride > ((int64_t)1 << 60) / rows);
+}
+
+// Whether matrices share memory: what one workgroup writes where another has yet
+// to read would make the results a matter of timing.
+
+// Rows of `bytes` bytes, `stride` apart, from lo on; the last ends at hi.
+struct Region {
+  int64_t lo, hi, bytes, stride, rows;
+};
+
+// Of a matrix argument that is neither bad nor empty.  Rows that overlap each
+// other are one row of all their bytes.
+inline Region region_of(const void *p, int32_t type, int64_t rows, int64_t cols, int64_t stride) {
+  const int64_t size = type_bytes(type), lo = reinterpret_cast<int64_t>(p);
+  if (rows == 1) stride = cols;
+  Region r{lo, lo + ((rows - 1) * stride + cols) * size, cols * size, stride * size, rows};
+  if (stride <= cols) r.bytes = r.stride = r.hi - lo, r.rows = 1;
+  return r;
+}
+
+// Whether row i of a meets a row of b: the first of b's rows that ends past its
+// start begins before its end.
+inline bool row_meets(const Region &a, int64_t i, const Region &b) {
+  const int64_t lo = a.lo + i * a.stride, past = lo - b.lo - b.bytes;
+  const int64_t row = past < 0 ? 0 : past / b.stride + 1;
+  return row < b.rows && b.lo + row * b.stride < lo + a.bytes;
+}
+
+inline bool meets(const Region &a, const Region &b) {
+  if (a.hi <= b.lo || b.hi <= a.lo) return false;
+  if (a.rows > b.rows) return meets(b, a);
+  if (a.rows > 1 && a.stride == b.stride) {
+    // rows of a that lie before b's second row all look at b's first one, and
+    // the last of them comes nearest; the later ones look at rows of b that
+    // are as far from them as the first of them is
+    const int64_t before = b.lo + b.bytes - a.lo, rows = a.rows;
+    const int64_t later = before <= 0 ? 0 : (before + a.stride - 1) / a.stride;
+    return (later > 0 && row_meets(a, std::min(later, rows) - 1, b)) ||
+           (later < rows && row_meets(a, later, b));
+  }
+  for (int64_t i = 0; i < a.rows; ++i)
+    if (row_meets(a, i, b)) return true;
+  return false;
+}
+
+// The same for two arguments, empty ones among them.
+inline bool share(const void *p, int32_t type, int64_t rows, int64_t cols, int64_t stride,
+                  const void *q, int32_t q_type, int64_t q_rows, int64_t q_cols,
+                  int64_t q_stride) {
+  if (!p || !q || !rows || !cols || !q_rows || !q_cols) return false;
+  return meets(region_of(p, type, rows, cols, stride),
+               region_of(q, q_type, q_rows, q_cols, q_stride));
 }
 
 using f16_t = _Float16;

@@ -833,6 +833,18 @@ int bgmf_log_probs_grad(const void *scores, int32_t type, int64_t rows, int64_t 
     return fail_call(BGMF_E_ARG, "%s: grad_entropy needs entropy", call);
   if (grad_scores == scores && grad_stride != row_stride && rows > 1)
     return fail_call(BGMF_E_ARG, "%s: in place, the row strides must be equal", call);
+  const auto shares = [&](const void *q, int32_t q_type, int64_t q_rows, int64_t q_cols,
+                          int64_t q_stride) {
+    return share(grad_scores, type, rows, cols, grad_stride, q, q_type, q_rows, q_cols, q_stride);
+  };
+  if ((grad_scores != scores && shares(scores, type, rows, cols, row_stride)) ||
+      shares(excluded, BGMF_TYPE_I8, rows, cols, excluded_stride) ||
+      shares(given, BGMF_TYPE_F32, 1, rows, rows) || shares(row_max, BGMF_TYPE_F32, 1, rows, rows) ||
+      shares(row_sum, BGMF_TYPE_F32, 1, rows, rows) ||
+      shares(entropy, BGMF_TYPE_F32, 1, rows, rows) ||
+      shares(grad_log_prob, BGMF_TYPE_F32, 1, rows, rows) ||
+      shares(grad_entropy, BGMF_TYPE_F32, 1, rows, rows))
+    return fail_call(BGMF_E_ARG, "%s: grad_scores shares memory with an input", call);
   const LogProbsGrad p{scores, excluded, given, rows, cols, row_stride, excluded_stride,
                        grad_stride, temperature, row_max, row_sum, entropy, grad_log_prob,
                        grad_entropy, grad_scores, 0};
