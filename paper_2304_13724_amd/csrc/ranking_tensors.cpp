@@ -13,10 +13,12 @@
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
+#include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdarg>
 #include <cstdio>
+#include <new>
 #include <stdexcept>
 #include <vector>
 
@@ -314,6 +316,15 @@ PyObject *clip_grad_norm(PyObject *const *a) {
   return THPVariable_Wrap(norm);
 }
 
+// PyTorch's exception for a full device, which callers catch by its type.
+void set_out_of_memory(const c10::Error &e) {
+  PyObject *torch = PyImport_ImportModule("torch");
+  PyObject *type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+  if (type) PyErr_SetString(type, e.what_without_backtrace());
+  Py_XDECREF(type);
+  Py_XDECREF(torch);
+}
+
 // Argument count, and C++ exceptions as Python's.
 template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -322,6 +333,10 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return F(args);
   } catch (const Refused &e) {
     PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const c10::OutOfMemoryError &e) {
+    set_out_of_memory(e);
+  } catch (const std::bad_alloc &) {
+    PyErr_NoMemory();
   } catch (const std::exception &e) {
     PyErr_SetString(PyExc_RuntimeError, e.what());
   }

@@ -149,3 +149,18 @@ def test_the_backward_call_has_no_derivative_and_says_so():
     with pytest.raises(ValueError, match="out"):
         ranking.log_probs_backward(x, given, r.row_max, r.row_sum, None, gl,
                                    out=torch.empty_like(want))
+
+
+# --- memory ----------------------------------------------------------------------
+
+def test_out_of_memory_is_pytorchs_error():
+    """4 TiB of scores, and half a TiB of alternatives: refused by the allocator."""
+    one = torch.ones(1, 1, device="cuda")
+    rows = one.expand(1 << 20, 1)
+    with pytest.raises(torch.OutOfMemoryError):
+        ranking.quantized_scores(rows, one.to(torch.int8).expand(1 << 20, 1),
+                                 torch.ones(1 << 20, device="cuda"))
+    with pytest.raises(torch.OutOfMemoryError):
+        ranking.log_probs(one.expand(1 << 30, 1), top=128)
+    r = ranking.log_probs(torch.zeros(2, 3, device="cuda"), top=1)  # and calls go on
+    assert r.top_item.tolist() == [[0], [0]]
