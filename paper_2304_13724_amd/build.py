@@ -76,11 +76,17 @@ def build_tensors(verbose: bool = False) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every HIP source into paper_2304_13724_amd/libbgmf.so, and
-    paper_2304_13724_amd/_ranking.so."""
+    """Compile every HIP source into paper_2304_13724_amd/libbgmf.so and, where
+    PyTorch is installed, paper_2304_13724_amd/_ranking.so (ranking.py raises
+    without it; the rest of the package needs the library alone)."""
     _compile([HIPCC, *FLAGS, "-L", _runtime_name_stub(), "-I", os.path.join(ROOT, "include"),
               *sources(), "-lrocprofiler-sdk-roctx"], LIB, verbose)
-    build_tensors(verbose)
+    try:
+        import torch  # noqa: F401
+    except ImportError:
+        print("PyTorch is not installed: _ranking.so is not built", file=sys.stderr)
+    else:
+        build_tensors(verbose)
     return LIB
 
 
