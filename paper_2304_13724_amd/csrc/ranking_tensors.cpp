@@ -14,6 +14,7 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/util/Exception.h>
+#include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdarg>
@@ -58,12 +59,16 @@ at::ScalarType dtype_of(int type) {
   return type == BGMF_TYPE_F32 ? at::kFloat : type == BGMF_TYPE_BF16 ? at::kBFloat16 : at::kHalf;
 }
 
+// Whether forward-mode derivatives are being computed: tensors have tangents at
+// no other time, and looking for one takes 10 ns a tensor.
+thread_local bool t_forward_mode = false;
+
 // The tensor behind a Python object, which keeps it alive during the call.  No
 // call has a forward-mode derivative, and none drops a tangent silently.
 const at::Tensor &tensor(PyObject *o, const char *name) {
   if (!THPVariable_Check(o)) refuse("%s must be a tensor", name);
   const at::Tensor &t = THPVariable_Unpack(o);
-  if (t._fw_grad(0).defined())
+  if (t_forward_mode && t._fw_grad(0).defined())
     refuse("%s has a tangent: forward-mode derivatives are not supported", name);
   if (t.is_neg() || t._is_zerotensor())
     refuse("%s: its memory does not hold its values (call .resolve_neg() or .clone())", name);
@@ -330,6 +335,7 @@ template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
   try {
     if (n != N) refuse("%lld arguments are needed", (long long)N);
+    t_forward_mode = torch::autograd::ForwardADLevel::try_get_by_idx(0) != nullptr;
     return F(args);
   } catch (const Refused &e) {
     PyErr_SetString(PyExc_ValueError, e.what());
