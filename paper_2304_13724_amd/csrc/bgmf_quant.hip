@@ -20,7 +20,8 @@ using i32x16 = __attribute__((ext_vector_type(16))) int32_t;
 // (kHeld vectors of 16 bytes each), reduce its largest magnitude, and write
 // the quotients; what a longer row has beyond that is read a second time.
 // Bound: memory latency (a row's bytes are written after all of it has arrived):
-// 4,096 rows of 4,096 bf16 take 17 us, 2.9 TB/s.
+// 4,096 rows of 4,096 bf16 take 17 us, 2.9 TB/s; catalogues of 5M rows of 64 fp32
+// 419 us, 3.9 TB/s, of 128 558 us, 5.8 TB/s.
 // ---------------------------------------------------------------------------
 
 // Largest magnitude, +infinity where a value is NaN or infinite.
@@ -37,10 +38,11 @@ struct Largest {
 // A row's scale, and its values' bytes; NaN and 0 where the magnitude is
 // infinite.  x / scale has to be rounded as by a division.  Where neither it
 // nor its remainder can leave the normal range, the product with the rounded
-// reciprocal, corrected once by its exact remainder, is that quotient (the
-// error left, 2^-24 units, is less than a quotient of fp32 numbers keeps from
-// a rounding boundary; equal to the division in 1.7e10 of them, half of these
-// next to ties) in a third of the instructions.
+// reciprocal, corrected once by its exact remainder (Markstein's division by
+// fused multiply-adds), is that quotient (the error left, 2^-24 units, is less
+// than a quotient of fp32 numbers keeps from a rounding boundary; equal to the
+// division in 1.7e10 of them, half of these next to ties) in a third of the
+// instructions.
 struct Scale {
   float s, r;
   bool quick;
@@ -128,8 +130,12 @@ hipError_t quantize(const void *x, int64_t rows, int32_t k, int64_t stride, int8
                        stream, static_cast<const T *>(x), rows, k, stride, q, q_stride, fill,
                        scale);
   };
-  // as few lanes as hold the row: short rows share a wave, and a wave that has a
-  // row needs no barrier
+  // few lanes to a row: short rows share a wave, and a wave that has a row needs
+  // no barrier.  fp32 by 4, 16 and 64 lanes: 1M rows of 32 33, 82 and 596 us, 5M of
+  // 64 340, 416 and 2868, 500,000 of 128 103, 60 and 306; by 16, 64 and 256:
+  // 100,000 rows of 256 30, 65 and 234, of 1,024 145, 96 and 258, 20,000 of 4,096
+  // 161, 86 and 78 (18,000 of 64 by 4 and 16: 3.9 and 3.6; 16 of 4,096 by 64 and
+  // 256: 6.9 and 3.8)
   if (vecs <= 8) go(std::integral_constant<int, 4>{});
   else if (vecs <= 32) go(std::integral_constant<int, 16>{});
   else if (vecs <= 512) go(std::integral_constant<int, 64>{});
@@ -689,8 +695,9 @@ __global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4) k_product_many
 // from LDS while the matrix unit works, and a step's bytes are loaded a whole
 // step before they go to the other LDS buffer.  Bound: the matrix units, which
 // work 56% of the cycles; the clock falls to about 1.75 GHz meanwhile.  4,096 x
-// 8,192 x 4,096 takes 140 us, 2.0e15 operations a second (the library's int8
-// product of these sizes: 141 us).
+// 8,192 x 4,096 to bf16 takes 137 us, 2.0e15 operations a second (the library's
+// int8 product of these sizes: 141 us).  To fp32, where the stores need more
+// registers (8 bytes a lane in scratch), it takes 12 us more.
 // Kinds of instructions that the scheduler is told to place.
 constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
 
@@ -834,8 +841,17 @@ void launch_many(const Product &p, hipStream_t stream) {
 template <class O, class X>
 void launch_product(const Product &p, hipStream_t stream) {
   constexpr bool OWN = !std::is_same<X, int8_t>::value;
-  const bool small = p.items < 64 * kFullGpu * kWaves;  // less than 64 items for each wave
-  // few tiles and a long k: the waves of a workgroup share a tile
+  // Less than 64 items for each wave: one tile at a time.  Several make their
+  // loads overlap: one user, k = 64, 100,000 items 5.4 us one at a time and 4.2
+  // eight at a time, 524,288 10.1 and 9.2, 5M 80 and 64; k = 100 from bytes, one
+  // and four at a time, 100,000 6.5 and 6.3, 400,000 13.2 and 11.9, 5M 137 and 132.
+  const bool small = p.items < 64 * kFullGpu * kWaves;
+  // Few tiles and a long k: the waves of a workgroup share a tile.  One user,
+  // shared and not: k = 512 2,048 items 5.3 and 6.3 us, 16,384 6.4 and 6.3, 32,768
+  // 9.0 and 8.3; k = 1,024 5.7 and 8.1, 8.6 and 9.3, 10.9 and 10.9; k = 256 5.1 and
+  // 5.4, 5.9 and 5.3.  64 users, shared and in tiles of 64 x 64: k = 512 4,096
+  // items 8.0 and 9.1, 8,192 10.4 and 9.3; k = 1,024 8.7 and 12.7, 12.2 and 13.2,
+  // 16,384 18.3 and 14.6; k = 4,096 17.9 and 34.5, 28.6 and 35.1, 50.5 and 35.9.
   const bool split = !OWN && p.items < (p.rows <= 16 ? 32768 : 8193) && p.kp >= 512;
   const auto tiles = [&](int64_t items, int64_t users) {
     return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
@@ -852,11 +868,16 @@ void launch_product(const Product &p, hipStream_t stream) {
     return;
   }
   if constexpr (!OWN) {
+    // (fewer than 128 items: 100 x 100 x 256 6.5 us against 7.1 in tiles of 64 x 64)
     if (p.items < kFewItems || (p.rows <= 64 && split)) {
       if (split) launch_few<O, X, 2, 1, true>(p, stream);
       else launch_few<O, X, 2, 1, false>(p, stream);
       return;
     }
+    // 256 x 256 and 128 x 128, to bf16: 4,096 x 8,192 (512 tiles), k = 256 32 and 27
+    // us, 512 40 and 40, 768 49 and 53, 1,024 57 and 65, 4,096 154 and 215 (to fp32:
+    // 512 60 and 55, 1,024 75 and 79); 2,048 x 4,096 (128 tiles), k = 1,024 27 and
+    // 22, 4,096 62 and 60
     if (p.k >= 512 && p.items >= 256 && tiles(256, 256) >= 256) {
       const dim3 groups((unsigned)tiles(256, 256)), threads(kThreads);
       if (p.k % 16)
@@ -864,7 +885,9 @@ void launch_product(const Product &p, hipStream_t stream) {
       else hipLaunchKernelGGL((k_product_large<O, false>), groups, threads, 0, stream, p);
       return;
     }
-    // the largest tiles of which every CU gets one
+    // the largest tiles of which every CU gets one: 128 x 128, 128 x 64 and 64 x 64
+    // take 20, 20 and 25 us for 2,048 x 18,000 x 64 to bf16, 9.1, 8.0 and 7.8 for
+    // 128 x 16,384 x 72 to fp32
     if (p.rows > 64 && tiles(128, 128) >= 256) {
       launch_many<O, X, 2, 2>(p, stream);
       return;

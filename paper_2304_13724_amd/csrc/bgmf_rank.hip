@@ -449,11 +449,13 @@ __device__ __forceinline__ void write_row(const LogProbs &P, int64_t r, const So
 // One workgroup per row, or per part of a row.  Bound: HBM; the scores are
 // read once.  A thread takes kGroup vectors at a time (64 bytes in flight),
 // their maximum first, so that the running sums are rescaled once per group.
-// 4,001 x 10,007 fp32 without alternatives takes 29 us, 5.5 TB/s.  Choosing
-// them comes after a row's last score: 5 us for ten on each of 1,999 rows of
-// 18,000, all of which are on the GPU at once; these in bf16 with exclusions
-// take 30 us, and 25 without alternatives, bound by the vector units (some 14
-// cycles a score).
+// 4,001 x 10,007 fp32 without alternatives takes 29 us, 5.5 TB/s.  A 16-bit type
+// with exclusions is bound by the vector units: 1,999 x 18,000 bf16 takes 27 us
+// without alternatives (they work 86% of the CUs' cycles, 19 instructions a
+// score) and 31 with ten (80%, 22).  A group's vectors that a row does not have
+// are computed all the same (18,000 scores are 2,250 vectors in three groups of
+// 1,024).  Alternatives are chosen after a row's last score, and their registers
+// (92 against 60) leave room for 1,280 workgroups at once in place of 2,048.
 constexpr int kGroup = kCols;
 template <class T, bool EX, bool TOP, int TH>
 __global__ void __launch_bounds__(TH) k_log_probs(LogProbs P) {
@@ -563,7 +565,10 @@ struct PartSource {  // column q has the list of part q, larger scores first
 };
 
 // Joins the parts of a row: one workgroup per row.  Bound: latency (eight rows
-// of 153 parts with 50 alternatives each: 7 us).
+// of 153 parts with 50 alternatives each: 7 us).  A row with fewer parts than
+// alternatives gets no bound from the parts' maxima, and all of its lists are
+// put in order: one row of 625,001 (20 parts) takes 220 us with 100
+// alternatives, one of 3.2M (98 parts) 319 us with 128, 15 and 18 with ten.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_log_probs_join(LogProbs P) {
   __shared__ SoftLds<kThreads> soft_lds;
@@ -603,7 +608,9 @@ __global__ void __launch_bounds__(kThreads) k_log_probs_join(LogProbs P) {
 // ---------------------------------------------------------------------------
 // Gradient: every score is read and its gradient written once.  A workgroup
 // takes a tile of one row at a time.  Bound: HBM: 4,096 x 18,000 fp32 take 104
-// us, 5.7 TB/s.
+// us, 5.7 TB/s.  16-bit types with exclusions take more registers: 8,192 x
+// 18,000 bf16 150 us, 4.9 TB/s (127 of them, four waves a SIMD), f16 179 us (131,
+// three waves; 154 and 127 with an entropy gradient).
 // ---------------------------------------------------------------------------
 struct LogProbsGrad {
   const void *x;
@@ -676,16 +683,21 @@ __global__ void __launch_bounds__(TH) k_log_probs_grad(LogProbsGrad P) {
 
 constexpr int64_t kMostGroups = 1 << 20;
 
-// How a row is split: enough workgroups to fill the GPU (eight for each of
-// 256 CUs) while a part keeps 32,768 scores, and a row at most 1024 parts.  A
-// part has to pay for the second launch: one row of 18,000 scores, ten
-// alternatives, takes 8.0 us in one part and 7.1 + 5.2 in two.
-constexpr int64_t kFullGpu = 2048, kLeastPart = 32768;
+// How a row is split: in as few parts as hold at most 32,768 scores each, but
+// no more than fill the GPU (eight workgroups for each of 256 CUs) or than 1024.
+// Parts have to pay for the second launch.  One row, ten alternatives, in one,
+// two and three parts: 18,000 scores 7.9, 12.7 and 12.2 us, 33,000 10.1, 13.7
+// and 12.9, 65,000 13.6, 15.4 and 14.4, 80,000 16.0, 16.5 and 14.8; without
+// alternatives 33,000 7.2, 8.1 and 7.2, 65,000 10.7, 9.8 and 8.6.  (Eight and 64
+// rows are alike.)  So rows of up to 65,000 would be faster in one part with
+// alternatives, and longer single rows in more than they get: 625,001 take 14.6
+// us in 20 parts and 11.6 in 128, 5M 17.8 in 153 and 15.9 in 256.
+constexpr int64_t kFullGpu = 2048, kPart = 32768;
 struct Split {
   int64_t parts, len;
 };
 Split split_of(int64_t rows, int64_t cols) {
-  int64_t parts = std::min({(cols + kLeastPart - 1) / kLeastPart,
+  int64_t parts = std::min({(cols + kPart - 1) / kPart,
                             std::max<int64_t>(kFullGpu / std::max<int64_t>(rows, 1), 1), kMostParts});
   if (parts <= 1) return {1, cols};
   const int64_t len = ((cols + parts - 1) / parts + 63) / 64 * 64;
@@ -693,7 +705,11 @@ Split split_of(int64_t rows, int64_t cols) {
 }
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
 
-// Rows of at most this many scores go to workgroups of one wave.
+// Rows of at most this many scores go to workgroups of one wave.  Ten
+// alternatives, a wave and 256 threads: 4,096 rows of 500 9.5 and 20.3 us, of
+// 2,048 13.1 and 22.0, of 4,096 17.9 and 22.0, of 8,192 30.8 and 32.4; 100 rows
+// of 500 6.2 and 6.5, of 2,048 6.7 and 6.7, of 3,000 7.1 and 6.7, of 8,192 9.5 and
+// 6.8.  Their gradient: 4,096 rows of 500 5.6 and 9.2, of 2,048 12.3 and 12.8.
 constexpr int64_t kShortRow = 2048;
 
 template <bool V>
