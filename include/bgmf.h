@@ -431,8 +431,8 @@ int bgmf_chain_stats(bgmf_t *h, int64_t out[4]);
  *     sizes; what it holds before and after is of no meaning.
  *   - An output may share no element with an input or another output, but
  *     where a description allows it (a matrix's rows may interleave with
- *     another's, as columns of one wider matrix do).  For grad_scores, out and
- *     q this is checked.
+ *     another's, as columns of one wider matrix do).  For grad_scores, out, q
+ *     and scale this is checked.
  *   - Sizes of zero are valid and do what the formulas say of empty sums.
  *   - Errors are reported by bgmf_last_error(NULL).  BGMF_E_ARG for what the
  *     descriptions exclude, BGMF_E_BUDGET for a workspace that is too small.
@@ -444,6 +444,7 @@ int bgmf_chain_stats(bgmf_t *h, int64_t out[4]);
 #define BGMF_TYPE_BF16 1
 #define BGMF_TYPE_F16  2
 #define BGMF_TYPE_I8   3
+#define BGMF_TYPE_MX4  4 /* bytes of two 4-bit values (bgmf_quantize_rows_mx) */
 
 /* Largest number of top alternatives, and longest row of a product (its sums
  * are exact in 32-bit integers). */
@@ -520,6 +521,118 @@ int bgmf_quantized_scores(const void *x, int32_t type, int64_t rows, int64_t k,
                           int64_t item_count, int64_t items_stride, const float *item_scale,
                           void *out, int32_t out_type, int64_t out_stride, void *ws,
                           int64_t ws_bytes, void *hip_stream);
+
+/* Rows in 4 bits, in blocks of 32 columns that share a scale (the MXFP4 format of
+ * the OCP Microscaling Formats specification, version 1.0):
+ *   m = max |x| over the block (columns past k count as zeros)
+ *   scale X = 2^e, e = floor(log2 m) - 2, at least -127, kept as the byte e + 127
+ *     (byte 0 for m = 0)
+ *   q = x / X rounded to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ *     negatives, ties to the one whose last bit is 0, larger magnitudes to 6;
+ *     kept as the sign above the three bits that number these values from 0 on
+ * q: rows of 16 bytes a block, the even one of two neighbours in the lower half
+ * of their byte (rows x ceil(k / 32) * 16 bytes, row stride in bytes); scale:
+ * rows of a byte a block.  A block with a NaN or an infinity: scale byte 255 and
+ * q = 0, and it stands for NaN.  x: F32, BF16 or F16.  1 <= k < 2^30. */
+int bgmf_quantize_rows_mx(const void *x, int32_t type, int64_t rows, int64_t k,
+                          int64_t row_stride, uint8_t *q, int64_t q_stride, uint8_t *scale,
+                          int64_t scale_stride, void *hip_stream);
+/* The values that such rows stand for, out[r][c] = q_rc X, c < k, rounded to
+ * out's type (F32, BF16 or F16; exact in F32, and in BF16 down to 2^-126). */
+int bgmf_dequantize_rows_mx(const uint8_t *q, int64_t q_stride, const uint8_t *scale,
+                            int64_t scale_stride, int64_t rows, int64_t k, void *out,
+                            int32_t out_type, int64_t out_stride, void *hip_stream);
+
+/* Scores of users over items, both in 4 bits:
+ *   out[r][j] = sum_c a_rc b_jc, a and b the values that the rows stand for,
+ * with the products exact, summed in fp32, and the sum rounded once to out's
+ * type (F32, BF16 or F16).  A score with a NaN block is NaN.  What is below
+ * 2^-126 in magnitude within a sum may count as zero.
+ *   x: rows x k, BGMF_TYPE_MX4 (bytes, with row_scale; row_stride in bytes), or
+ *     F32, BF16 or F16: then the rows are quantised as by bgmf_quantize_rows_mx
+ *     within the call and row_scale must be NULL;
+ *   items: item_count rows of ceil(k / 32) blocks, strides in bytes.
+ * Rows in 4 bits are whole blocks: their values past k have to be 0, as
+ * bgmf_quantize_rows_mx leaves them.  1 <= k < 2^20; rows, item_count < 2^31. */
+int64_t bgmf_mx_scores_workspace(int64_t rows, int64_t item_count, int64_t k, int32_t type);
+int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t row_stride,
+                   const uint8_t *row_scale, int64_t row_scale_stride, const uint8_t *items,
+                   int64_t item_count, int64_t items_stride, const uint8_t *item_scale,
+                   int64_t item_scale_stride, void *out, int32_t out_type, int64_t out_stride,
+                   void *ws, int64_t ws_bytes, void *hip_stream);
+
+/* Learning from choices that users made among what another policy showed them.
+ * Row r of scores (rows x cols, F32, BF16 or F16) has the shown item g =
+ * given[r], its advantage A = advantage[r] and b = old_log_prob[r], its log
+ * probability when it was shown.  With p = softmax(x / t) over the items that
+ * are not excluded, as in bgmf_log_probs:
+ *   log_prob[r] = ln p_g        rho = exp(log_prob - b)
+ *   loss[r] = -min(rho A, min(max(rho, 1 - clip_low), 1 + clip_high) A)
+ *             + kl_weight kl[r]
+ * and, of a reference policy, one of
+ *   reference (scores of the type and shape of `scores`, excluded alike):
+ *     kl[r] = sum_j p_j ln(p_j / q_j), q = softmax(reference / t)
+ *   reference_log_prob (ln q_g): kl[r] = exp(z) - 1 - z, z = ln q_g - ln p_g,
+ *     its estimate from the shown item
+ *   neither: kl[r] = 0.
+ * kl may come out below 0 by its rounding.  (One pass over the scores and the
+ * reference; terms in fp32, running sums and a row's own numbers in fp64,
+ * results in fp32.)
+ *   given[r] = -1: the row fills the batch up.  Its scores are not looked at;
+ *     loss, log_prob and kl are 0, and so is its gradient.
+ *   A row with nothing left (all items excluded or -inf, or cols = 0): loss and
+ *     kl 0, log_prob -inf, gradient 0.
+ *   given[r] otherwise outside [0, cols): loss, log_prob and the gradient NaN.
+ *   A NaN or +inf among the items that are not excluded makes the row's results
+ *     NaN; in the reference, kl and (with kl_weight not 0) loss and gradient.
+ *   An item with p_j = 0 adds nothing to kl; q_j = 0 < p_j makes it infinite,
+ *     and the gradient is then not finite where kl_weight is not 0.  An excluded
+ *     given item has rho = 0 (and an infinite estimate).
+ * row_state (5 x rows floats, NULL if not wanted): what bgmf_policy_loss_grad needs.
+ *
+ * With grad_scores not NULL the same call gives the gradient of sum_r grad_loss[r]
+ * loss[r] with respect to the scores (grad_loss NULL: ones),
+ *   grad_scores[r][j] = grad_loss[r] / t ( s (1[j = g] - p_j)
+ *     + kl_weight p_j (ln(p_j / q_j) - kl) )     (second line with a reference)
+ *   s = d loss / d log_prob = -rho A where rho A is the smaller one, else 0,
+ *     + kl_weight (1 - exp(z)) with reference_log_prob
+ * rounded once to the type of the scores, 0 for excluded items.  grad_scores may
+ * be the scores or the reference (same pointer and stride).
+ * 0 <= clip_low <= 1, clip_high >= 0 (infinity: no upper bound), kl_weight
+ * finite.  loss, log_prob and kl may be NULL.  rows, cols < 2^31. */
+int64_t bgmf_policy_loss_workspace(int64_t rows, int64_t cols);
+int bgmf_policy_loss(const void *scores, int32_t type, int64_t rows, int64_t cols,
+                     int64_t row_stride, const void *reference, int64_t reference_stride,
+                     const uint8_t *excluded, int64_t excluded_stride, const int32_t *given,
+                     const float *advantage, const float *old_log_prob,
+                     const float *reference_log_prob, float temperature, float clip_low,
+                     float clip_high, float kl_weight, float *loss, float *log_prob, float *kl,
+                     float *row_state, const float *grad_loss, void *grad_scores,
+                     int64_t grad_stride, void *ws, int64_t ws_bytes, void *hip_stream);
+/* The gradient from the forward call's inputs and row_state. */
+int bgmf_policy_loss_grad(const void *scores, int32_t type, int64_t rows, int64_t cols,
+                          int64_t row_stride, const void *reference, int64_t reference_stride,
+                          const uint8_t *excluded, int64_t excluded_stride, const int32_t *given,
+                          float temperature, float kl_weight, const float *row_state,
+                          const float *grad_loss, void *grad_scores, int64_t grad_stride,
+                          void *hip_stream);
+
+/* Dropout (x, out: rows x cols, F32, BF16 or F16): element i = r cols + c is
+ *   out = x / (1 - p), the quotient's factor and the product in fp32, rounded
+ *     once more to the type,         where w_i >= floor(p 2^32)
+ *   out = 0 (also of a NaN)          elsewhere
+ * with w_i word i mod 4 of the generator Philox4x32 with ten rounds (Salmon,
+ * Moraes, Dror and Shaw, "Parallel random numbers: as easy as 1, 2, 3", 2011)
+ * for the key `seed` (its lower word first) and the counter offset +
+ * *offset_on_device + floor(i / 4) (a 64-bit sum, in the counter's two lower
+ * words).  No mask is stored: the gradient is the same call on the gradient.
+ * Calls whose counters are not to meet are ceil(rows cols / 4) apart.
+ * offset_on_device (NULL: 0) is read when the work runs, so that replays of a
+ * captured graph can drop other elements.  out may be x (same pointer and
+ * stride).  0 <= p <= 1; rows < 2^31, cols < 2^40. */
+int bgmf_dropout(const void *x, int32_t type, int64_t rows, int64_t cols, int64_t row_stride,
+                 double p, uint64_t seed, uint64_t offset, const uint64_t *offset_on_device,
+                 void *out, int64_t out_stride, void *hip_stream);
 
 /* One gradient of bgmf_clip_grad_norm: a rows x cols matrix in (row stride
  * in_stride) and the place out of its clipped values (out_stride), which may

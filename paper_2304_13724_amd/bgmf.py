@@ -48,6 +48,7 @@ BGMF_TYPE_F32 = 0
 BGMF_TYPE_BF16 = 1
 BGMF_TYPE_F16 = 2
 BGMF_TYPE_I8 = 3
+BGMF_TYPE_MX4 = 4
 BGMF_TOP_MAX = 128
 BGMF_PRODUCT_K_MAX = 131071
 
@@ -60,6 +61,9 @@ EXPORTED = (
     "bgmf_rmse_coo_dev", "bgmf_reorder_ids", "bgmf_log_probs_workspace", "bgmf_log_probs",
     "bgmf_log_probs_grad", "bgmf_quantize_rows", "bgmf_quantized_scores_workspace",
     "bgmf_quantized_scores", "bgmf_clip_grad_norm_workspace", "bgmf_clip_grad_norm",
+    "bgmf_quantize_rows_mx", "bgmf_dequantize_rows_mx", "bgmf_mx_scores_workspace",
+    "bgmf_mx_scores", "bgmf_policy_loss_workspace", "bgmf_policy_loss", "bgmf_policy_loss_grad",
+    "bgmf_dropout",
 )
 
 
@@ -124,6 +128,18 @@ def _load() -> ctypes.CDLL:
                                    I64, vp], c_int),
         "bgmf_clip_grad_norm_workspace": ([I64], I64),
         "bgmf_clip_grad_norm": ([vp, I64, F32, vp, vp, I64, vp], c_int),
+        "bgmf_quantize_rows_mx": ([vp, I32, I64, I64, I64, vp, I64, vp, I64, vp], c_int),
+        "bgmf_dequantize_rows_mx": ([vp, I64, vp, I64, I64, I64, vp, I32, I64, vp], c_int),
+        "bgmf_mx_scores_workspace": ([I64, I64, I64, I32], I64),
+        "bgmf_mx_scores": ([vp, I32, I64, I64, I64, vp, I64, vp, I64, I64, vp, I64, vp, I32, I64,
+                            vp, I64, vp], c_int),
+        "bgmf_policy_loss_workspace": ([I64, I64], I64),
+        "bgmf_policy_loss": ([vp, I32, I64, I64, I64, vp, I64, vp, I64, vp, vp, vp, vp, F32, F32,
+                              F32, F32, vp, vp, vp, vp, vp, vp, I64, vp, I64, vp], c_int),
+        "bgmf_policy_loss_grad": ([vp, I32, I64, I64, I64, vp, I64, vp, I64, vp, F32, F32, vp, vp,
+                                   vp, I64, vp], c_int),
+        "bgmf_dropout": ([vp, I32, I64, I64, I64, ctypes.c_double, ctypes.c_uint64,
+                          ctypes.c_uint64, vp, vp, I64, vp], c_int),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -395,6 +411,61 @@ def bgmf_clip_grad_norm_workspace(count: int) -> int:
 def bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream) -> None:
     """``grads``: a ctypes array of ``Grad``, or the address of one."""
     _check(None, _lib.bgmf_clip_grad_norm(grads, count, max_norm, norm, ws, ws_bytes, stream))
+
+
+def bgmf_quantize_rows_mx(x, type_, rows, k, row_stride, q, q_stride, scale, scale_stride,
+                          stream) -> None:
+    _check(None, _lib.bgmf_quantize_rows_mx(x, type_, rows, k, row_stride, q, q_stride, scale,
+                                            scale_stride, stream))
+
+
+def bgmf_dequantize_rows_mx(q, q_stride, scale, scale_stride, rows, k, out, out_type, out_stride,
+                            stream) -> None:
+    _check(None, _lib.bgmf_dequantize_rows_mx(q, q_stride, scale, scale_stride, rows, k, out,
+                                              out_type, out_stride, stream))
+
+
+def bgmf_mx_scores_workspace(rows: int, item_count: int, k: int, type_: int) -> int:
+    return _lib.bgmf_mx_scores_workspace(rows, item_count, k, type_)
+
+
+def bgmf_mx_scores(x, type_, rows, k, row_stride, row_scale, row_scale_stride, items, item_count,
+                   items_stride, item_scale, item_scale_stride, out, out_type, out_stride, ws,
+                   ws_bytes, stream) -> None:
+    _check(None, _lib.bgmf_mx_scores(
+        x, type_, rows, k, row_stride, row_scale, row_scale_stride, items, item_count,
+        items_stride, item_scale, item_scale_stride, out, out_type, out_stride, ws, ws_bytes,
+        stream))
+
+
+def bgmf_policy_loss_workspace(rows: int, cols: int) -> int:
+    return _lib.bgmf_policy_loss_workspace(rows, cols)
+
+
+def bgmf_policy_loss(scores, type_, rows, cols, row_stride, reference, reference_stride, excluded,
+                     excluded_stride, given, advantage, old_log_prob, reference_log_prob,
+                     temperature, clip_low, clip_high, kl_weight, loss, log_prob, kl, row_state,
+                     grad_loss, grad_scores, grad_stride, ws, ws_bytes, stream) -> None:
+    _check(None, _lib.bgmf_policy_loss(
+        scores, type_, rows, cols, row_stride, reference, reference_stride, excluded,
+        excluded_stride, given, advantage, old_log_prob, reference_log_prob, temperature, clip_low,
+        clip_high, kl_weight, loss, log_prob, kl, row_state, grad_loss, grad_scores, grad_stride,
+        ws, ws_bytes, stream))
+
+
+def bgmf_policy_loss_grad(scores, type_, rows, cols, row_stride, reference, reference_stride,
+                          excluded, excluded_stride, given, temperature, kl_weight, row_state,
+                          grad_loss, grad_scores, grad_stride, stream) -> None:
+    _check(None, _lib.bgmf_policy_loss_grad(
+        scores, type_, rows, cols, row_stride, reference, reference_stride, excluded,
+        excluded_stride, given, temperature, kl_weight, row_state, grad_loss, grad_scores,
+        grad_stride, stream))
+
+
+def bgmf_dropout(x, type_, rows, cols, row_stride, p, seed, offset, offset_on_device, out,
+                 out_stride, stream) -> None:
+    _check(None, _lib.bgmf_dropout(x, type_, rows, cols, row_stride, p, seed, offset,
+                                   offset_on_device, out, out_stride, stream))
 
 
 # --- convenience wrapper -----------------------------------------------------

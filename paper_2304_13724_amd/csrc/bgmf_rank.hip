@@ -11,91 +11,6 @@ namespace {
 
 // Threads of a workgroup: 256, or one wave for short rows (TH below).
 constexpr int kThreads = 256;
-constexpr float kLog2e = 1.44269504088896341f;
-constexpr double kLn2 = 0.69314718055994530942;
-
-// Reductions over a wave in registers (DPP): four steps within rows of 16
-// lanes, two between rows, the total in lane 63.  A lane without a source adds
-// `none`.
-template <int CTRL, int ROWS>
-__device__ __forceinline__ int32_t dpp(int32_t none, int32_t x) {
-  return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xF, false);
-}
-template <class F>
-__device__ __forceinline__ int32_t wave_reduce(int32_t v, int32_t none, const F &f) {
-  v = f(v, dpp<0x111, 0xF>(none, v));
-  v = f(v, dpp<0x112, 0xF>(none, v));
-  v = f(v, dpp<0x114, 0xF>(none, v));
-  v = f(v, dpp<0x118, 0xF>(none, v));
-  v = f(v, dpp<0x142, 0xA>(none, v));
-  v = f(v, dpp<0x143, 0xC>(none, v));
-  return __builtin_amdgcn_readlane(v, 63);
-}
-__device__ __forceinline__ float wave_max(float v) {
-  return __int_as_float(wave_reduce(__float_as_int(v), __float_as_int(-INFINITY),
-                                    [](int32_t a, int32_t b) {
-                                      return __float_as_int(
-                                          fmaxf(__int_as_float(a), __int_as_float(b)));
-                                    }));
-}
-template <int CTRL, int ROWS>
-__device__ __forceinline__ double dpp_add(double v) {
-  const int32_t lo = dpp<CTRL, ROWS>(0, __double2loint(v)), hi = dpp<CTRL, ROWS>(0, __double2hiint(v));
-  return v + __hiloint2double(hi, lo);
-}
-__device__ __forceinline__ double wave_sum(double v) {
-  v = dpp_add<0x111, 0xF>(v);
-  v = dpp_add<0x112, 0xF>(v);
-  v = dpp_add<0x114, 0xF>(v);
-  v = dpp_add<0x118, 0xF>(v);
-  v = dpp_add<0x142, 0xA>(v);
-  v = dpp_add<0x143, 0xC>(v);
-  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), 63),
-                          __builtin_amdgcn_readlane(__double2loint(v), 63));
-}
-
-// A row, or a part of one, in 16-byte vectors and up to N - 1 single elements
-// at its end.
-template <class T, bool EX>
-struct Row {
-  static constexpr int N = Vec<T>::N;
-  const T *x;
-  const uint8_t *ex;  // with EX
-  int32_t len;
-  __device__ __forceinline__ int32_t vecs() const { return len / N; }
-  __device__ __forceinline__ float one(int32_t i) const {  // -inf where excluded
-    if constexpr (EX)
-      if (ex[i]) return -INFINITY;
-    return to_float(x[i]);
-  }
-  // A vector as it is in memory, and its scores: several are fetched before the
-  // first is looked at.
-  struct Raw {
-    Vec<T> a;
-    uint32_t b[EX ? N / 4 : 1];
-  };
-  __device__ __forceinline__ Raw fetch(int32_t v) const {
-    Raw r;
-    r.a = load_vec(x + (int64_t)v * N);
-    if constexpr (EX) __builtin_memcpy(r.b, ex + (int64_t)v * N, N);
-    return r;
-  }
-  static __device__ __forceinline__ Raw nothing() {  // scores of -inf
-    Raw r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) r.a.v[i] = from_float<T>(-INFINITY);
-    if constexpr (EX)
-      for (int i = 0; i < N / 4; ++i) r.b[i] = 0;
-    return r;
-  }
-  static __device__ __forceinline__ void scores(const Raw &r, float (&out)[N]) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      out[i] = to_float(r.a.v[i]);
-      if constexpr (EX) out[i] = r.b[i / 4] >> (i % 4 * 8) & 0xFF ? -INFINITY : out[i];
-    }
-  }
-};
 
 // Running maximum m, s = sum exp2(d) and w = sum exp2(d) d, d = (x - m) c, of
 // the scores seen so far.  A group's terms are summed in fp32 and added to

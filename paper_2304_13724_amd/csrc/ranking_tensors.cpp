@@ -321,6 +321,246 @@ PyObject *clip_grad_norm(PyObject *const *a) {
   return THPVariable_Wrap(norm);
 }
 
+// A 2-D tensor of bytes on the GPU, the bytes of a row adjacent.
+const at::Tensor &byte_rows(PyObject *o, const char *name) {
+  const at::Tensor &t = tensor(o, name);
+  if (t.dim() != 2 || t.scalar_type() != at::kByte) refuse("%s must be a 2-D tensor of uint8", name);
+  if (!t.is_cuda()) refuse("%s must be on the GPU", name);
+  if (t.size(1) > 1 && t.stride(1) != 1)
+    refuse("%s: the bytes of a row must be adjacent (call .contiguous())", name);
+  return t;
+}
+// Rows in 4 bits with their scales: 16 bytes and one byte for each of their blocks.
+const at::Tensor &blocks_of(PyObject *o, const char *name, PyObject *scales,
+                            const char *scales_name, const at::Tensor **scale) {
+  const at::Tensor &q = byte_rows(o, name), &s = byte_rows(scales, scales_name);
+  if (s.size(0) != q.size(0) || q.size(1) != 16 * s.size(1) || s.device() != q.device())
+    refuse("%s (rows of 16 bytes a block) and %s (rows of one) do not go together", name,
+           scales_name);
+  if (s.size(1) < 1) refuse("%s has rows of no elements", name);
+  *scale = &s;
+  return q;
+}
+const uint8_t *bytes(const at::Tensor &t) {
+  return static_cast<const uint8_t *>(t.const_data_ptr());
+}
+
+// (x, stream) -> (q, scale)
+PyObject *quantize_rows_mx(PyObject *const *a) {
+  int type;
+  const at::Tensor &x = matrix(a[0], "x", kFloats, &type);
+  const int64_t rows = x.size(0), k = x.size(1), blocks = (k + 31) / 32;
+  if (k < 1) refuse("x has rows of no elements");
+  const c10::DeviceGuard guard(x.device());
+  const at::Tensor q = make({rows, blocks * 16}, x, at::kByte),
+                   scale = make({rows, blocks}, x, at::kByte);
+  const int rc = bgmf_quantize_rows_mx(x.const_data_ptr(), type, rows, k, x.stride(0),
+                                       at_<uint8_t>(q), blocks * 16, at_<uint8_t>(scale), blocks,
+                                       stream_of(a[1]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  return Py_BuildValue("(NN)", THPVariable_Wrap(q), THPVariable_Wrap(scale));
+}
+
+// (q, scale, k or None, out type, out, stream) -> out
+PyObject *dequantize_rows_mx(PyObject *const *a) {
+  const at::Tensor *scale;
+  const at::Tensor &q = blocks_of(a[0], "q", a[1], "scale", &scale);
+  const int64_t rows = q.size(0), blocks = scale->size(1);
+  const int64_t k = a[2] == Py_None ? blocks * 32 : integer(a[2], "k");
+  if (k <= (blocks - 1) * 32 || k > blocks * 32)
+    refuse("k must be in (%lld, %lld] for rows of %lld blocks", (long long)(blocks - 1) * 32,
+           (long long)blocks * 32, (long long)blocks);
+  const int out_type = (int)integer(a[3], "out type");
+  const c10::DeviceGuard guard(q.device());
+  const at::Tensor out = output(a[4], "out", q, rows, k, dtype_of(out_type));
+  const int rc = bgmf_dequantize_rows_mx(bytes(q), q.stride(0), bytes(*scale), scale->stride(0),
+                                         rows, k, out.mutable_data_ptr(), out_type, out.stride(0),
+                                         stream_of(a[5]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[4], out);
+  return THPVariable_Wrap(out);
+}
+
+// (rows, items, item_scale, row_scale, out type, out, stream) -> out
+PyObject *mx_scores(PyObject *const *a) {
+  const at::Tensor *item_scale, *row_scale = nullptr;
+  const at::Tensor &items = blocks_of(a[1], "items", a[2], "item_scale", &item_scale);
+  const int64_t blocks = item_scale->size(1), m = items.size(0);
+  int type = BGMF_TYPE_MX4;
+  int64_t k = blocks * 32;
+  const at::Tensor *rows;
+  if (a[3] != Py_None) {
+    rows = &blocks_of(a[0], "rows", a[3], "row_scale", &row_scale);
+    if (row_scale->size(1) != blocks) refuse("rows and items must have equally many blocks");
+  } else {
+    if (THPVariable_Check(a[0]) && THPVariable_Unpack(a[0]).scalar_type() == at::kByte)
+      refuse("row_scale goes with uint8 rows and with no others");
+    rows = &matrix(a[0], "rows", kFloats, &type);
+    k = rows->size(1);
+    if (k < 1 || (k + 31) / 32 != blocks)
+      refuse("rows of %lld columns have %lld blocks, those of items %lld", (long long)k,
+             (long long)(k + 31) / 32, (long long)blocks);
+  }
+  if (rows->device() != items.device()) refuse("rows and items must be on one device");
+  const int64_t n = rows->size(0);
+  const int out_type = (int)integer(a[4], "out type");
+  const c10::DeviceGuard guard(items.device());
+  const at::Tensor out = output(a[5], "out", items, n, m, dtype_of(out_type));
+  const int64_t ws_bytes = bgmf_mx_scores_workspace(n, m, k, type);
+  at::Tensor ws;
+  if (ws_bytes) ws = make({ws_bytes}, items, at::kByte);
+  const int rc = bgmf_mx_scores(
+      rows->const_data_ptr(), type, n, k, rows->stride(0), row_scale ? bytes(*row_scale) : nullptr,
+      row_scale ? row_scale->stride(0) : 0, bytes(items), m, items.stride(0), bytes(*item_scale),
+      item_scale->stride(0), out.mutable_data_ptr(), out_type, out.stride(0),
+      ws_bytes ? ws.mutable_data_ptr() : nullptr, ws_bytes, stream_of(a[6]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[5], out);
+  return THPVariable_Wrap(out);
+}
+
+// The reference's scores, laid out as the policy's are.
+const void *reference_scores(PyObject *o, const at::Tensor &x, int64_t *stride) {
+  *stride = 0;
+  if (o == Py_None) return nullptr;
+  int type;
+  const at::Tensor &t = matrix(o, "reference", kFloats, &type);
+  if (t.sizes() != x.sizes() || t.scalar_type() != x.scalar_type() || t.device() != x.device())
+    refuse("reference must have the shape, the type and the device of the scores");
+  *stride = t.stride(0);
+  return t.const_data_ptr();
+}
+
+// (scores, given, advantage, old_log_prob, reference, reference_log_prob,
+// kl_weight, clip_low, clip_high, temperature, excluded, want, weight, out,
+// stream) -> (loss, log_prob, kl, row_state or None, gradient or None)
+// want: 1 for row_state, 2 for the gradient of the losses times weight.
+PyObject *policy_loss(PyObject *const *a) {
+  int type;
+  const at::Tensor &x = matrix(a[0], "scores", kFloats, &type);
+  const int64_t rows = x.size(0), cols = x.size(1), want = integer(a[11], "want");
+  const auto floats = [&](PyObject *o, const char *name, bool optional) {
+    return static_cast<const float *>(vector(o, name, x, rows, at::kFloat, optional));
+  };
+  const void *given = vector(a[1], "given", x, rows, at::kInt, false);
+  const float *advantage = floats(a[2], "advantage", false),
+              *old_log_prob = floats(a[3], "old_log_prob", false),
+              *ref_log_prob = floats(a[5], "reference_log_prob", true),
+              *weight = floats(a[12], "weight", true);
+  int64_t ex_stride, ref_stride;
+  const void *ref = reference_scores(a[4], x, &ref_stride);
+  if (a[4] != Py_None && a[5] != Py_None) refuse("reference or reference_log_prob, not both");
+  const uint8_t *ex = excluded_items(a[10], x, &ex_stride);
+  const c10::DeviceGuard guard(x.device());
+  const at::Tensor loss = make({rows}, x, at::kFloat), log_prob = make({rows}, x, at::kFloat),
+                   kl = make({rows}, x, at::kFloat);
+  at::Tensor state, grad, ws;
+  if (want & 1) state = make({5, rows}, x, at::kFloat);
+  if (want & 2) grad = output(a[13], "out", x, rows, cols, x.scalar_type());
+  const int64_t ws_bytes = bgmf_policy_loss_workspace(rows, cols);
+  if (ws_bytes) ws = make({ws_bytes}, x, at::kByte);
+  const int rc = bgmf_policy_loss(
+      x.const_data_ptr(), type, rows, cols, x.stride(0), ref, ref_stride, ex, ex_stride,
+      static_cast<const int32_t *>(given), advantage, old_log_prob, ref_log_prob,
+      (float)number(a[9], "temperature"), (float)number(a[7], "clip_low"),
+      (float)number(a[8], "clip_high"), (float)number(a[6], "kl_weight"), at_<float>(loss),
+      at_<float>(log_prob), at_<float>(kl), want & 1 ? at_<float>(state) : nullptr, weight,
+      want & 2 ? grad.mutable_data_ptr() : nullptr, want & 2 ? grad.stride(0) : 0,
+      ws_bytes ? ws.mutable_data_ptr() : nullptr, ws_bytes, stream_of(a[14]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  if (want & 2) written(a[13], grad);
+  const auto or_none = [](const at::Tensor &t) {
+    if (t.defined()) return THPVariable_Wrap(t);
+    Py_INCREF(Py_None);
+    return Py_None;
+  };
+  return Py_BuildValue("(NNNNN)", THPVariable_Wrap(loss), THPVariable_Wrap(log_prob),
+                       THPVariable_Wrap(kl), or_none(state), or_none(grad));
+}
+
+// (scores, given, row_state, weight, reference, kl_weight, temperature,
+// excluded, out, stream) -> out
+PyObject *policy_loss_backward(PyObject *const *a) {
+  int type;
+  const at::Tensor &x = matrix(a[0], "scores", kFloats, &type);
+  const int64_t rows = x.size(0), cols = x.size(1);
+  const void *given = vector(a[1], "given", x, rows, at::kInt, false);
+  const at::Tensor &state = tensor(a[2], "row_state");
+  if (state.dim() != 2 || state.size(0) != 5 || state.size(1) != rows || !state.is_contiguous() ||
+      state.scalar_type() != at::kFloat || state.device() != x.device())
+    refuse("row_state must be a contiguous float32 tensor of shape (5, %lld) on the same GPU",
+           (long long)rows);
+  const float *weight =
+      static_cast<const float *>(vector(a[3], "weight", x, rows, at::kFloat, true));
+  int64_t ex_stride, ref_stride;
+  const void *ref = reference_scores(a[4], x, &ref_stride);
+  const uint8_t *ex = excluded_items(a[7], x, &ex_stride);
+  const c10::DeviceGuard guard(x.device());
+  const at::Tensor out = output(a[8], "out", x, rows, cols, x.scalar_type());
+  const int rc = bgmf_policy_loss_grad(
+      x.const_data_ptr(), type, rows, cols, x.stride(0), ref, ref_stride, ex, ex_stride,
+      static_cast<const int32_t *>(given), (float)number(a[6], "temperature"),
+      (float)number(a[5], "kl_weight"), static_cast<const float *>(state.const_data_ptr()), weight,
+      out.mutable_data_ptr(), out.stride(0), stream_of(a[9]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[8], out);
+  return THPVariable_Wrap(out);
+}
+
+// A Python integer in [0, 2^64).
+uint64_t word(PyObject *o, const char *name) {
+  const unsigned long long v = PyLong_Check(o) ? PyLong_AsUnsignedLongLong(o) : -1ull;
+  if (!PyLong_Check(o) || (v == -1ull && PyErr_Occurred())) {
+    PyErr_Clear();
+    refuse("%s must be an integer in [0, 2^64)", name);
+  }
+  return v;
+}
+
+// (x, p, seed, offset, out, stream) -> out
+PyObject *dropout(PyObject *const *a) {
+  const at::Tensor &x = tensor(a[0], "x");
+  const int type = type_of(x);
+  if (type < 0 || !(kFloats >> type & 1)) refuse("x must be float32, bfloat16 or float16");
+  if (!x.is_cuda()) refuse("x must be on the GPU");
+  if (x.layout() != at::kStrided) refuse("x must be a dense tensor");
+  const double p = number(a[1], "p");
+  const uint64_t seed = word(a[2], "seed");
+  uint64_t offset = 0;
+  const uint64_t *on_device = nullptr;
+  if (THPVariable_Check(a[3])) {
+    const at::Tensor &t = tensor(a[3], "offset");
+    if (t.numel() != 1 || t.scalar_type() != at::kLong || t.device() != x.device())
+      refuse("offset must be an integer or an int64 tensor of one element on the same GPU");
+    on_device = static_cast<const uint64_t *>(t.const_data_ptr());
+  } else {
+    offset = word(a[3], "offset");
+  }
+  int64_t rows = 1, cols = x.numel(), stride = cols, out_stride = cols;
+  const bool as_matrix = !x.is_contiguous() ||
+                         (a[4] != Py_None && !tensor(a[4], "out").is_contiguous());
+  const c10::DeviceGuard guard(x.device());
+  at::Tensor out;
+  if (a[4] == Py_None) {
+    out = make(x.sizes(), x, x.scalar_type());
+  } else {
+    out = tensor(a[4], "out");
+    if (out.sizes() != x.sizes() || out.scalar_type() != x.scalar_type() ||
+        out.device() != x.device())
+      refuse("out must have the shape, the type and the device of x");
+  }
+  if (as_matrix) {
+    if (x.dim() != 2 || (x.size(1) > 1 && (x.stride(1) != 1 || out.stride(1) != 1)))
+      refuse("x and out must be contiguous, or 2-D with adjacent row elements");
+    rows = x.size(0), cols = x.size(1), stride = x.stride(0), out_stride = out.stride(0);
+  }
+  const int rc = bgmf_dropout(x.const_data_ptr(), type, rows, cols, stride, p, seed, offset,
+                              on_device, out.mutable_data_ptr(), out_stride, stream_of(a[5]));
+  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  written(a[4], out);
+  return THPVariable_Wrap(out);
+}
+
 // PyTorch's exception for a full device, which callers catch by its type.
 void set_out_of_memory(const c10::Error &e) {
   PyObject *torch = PyImport_ImportModule("torch");
@@ -361,6 +601,12 @@ PyMethodDef g_methods[] = {
     method<quantize_rows, 2>("quantize_rows"),
     method<quantized_scores, 7>("quantized_scores"),
     method<clip_grad_norm, 4>("clip_grad_norm"),
+    method<quantize_rows_mx, 2>("quantize_rows_mx"),
+    method<dequantize_rows_mx, 6>("dequantize_rows_mx"),
+    method<mx_scores, 7>("mx_scores"),
+    method<policy_loss, 15>("policy_loss"),
+    method<policy_loss_backward, 10>("policy_loss_backward"),
+    method<dropout, 6>("dropout"),
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_ranking", nullptr, -1, g_methods,

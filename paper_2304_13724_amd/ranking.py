@@ -1,9 +1,11 @@
 """Ranking with learned factors, on PyTorch tensors.
 
-Answers: quantise the item factors once (``Catalogue``), score users over the
-whole catalogue, and take log probabilities, entropy and the best items
-(``log_probs``).  Training on choices in place of ratings: ``log_probs`` is
-differentiable, and ``clip_grad_norm`` bounds the gradients' global norm.
+Answers: quantise the item factors once (``Catalogue``, in 8 or 4 bits), score
+users over the whole catalogue, and take log probabilities, entropy and the best
+items (``log_probs``).  Training on choices in place of ratings: ``log_probs`` is
+differentiable, ``dropout`` drops elements of the factors, and ``clip_grad_norm``
+bounds the gradients' global norm.  Training on what users did with the answers:
+``policy_loss``.
 
 Every function checks its tensors (ValueError for those that do not fit,
 BgmfError for what the library refuses), runs the library's kernels
@@ -25,6 +27,13 @@ TOP_MAX = bgmf.BGMF_TOP_MAX
 
 _TYPES = {torch.float32: bgmf.BGMF_TYPE_F32, torch.bfloat16: bgmf.BGMF_TYPE_BF16,
           torch.float16: bgmf.BGMF_TYPE_F16}
+
+
+def _type_code(dtype) -> int:
+    code = _TYPES.get(dtype)
+    if code is None:
+        raise ValueError(f"dtype must be float32, bfloat16 or float16: {dtype}")
+    return code
 
 
 class LogProbs(NamedTuple):
@@ -173,33 +182,197 @@ def quantized_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.
     bfloat16 or float16 without it, quantised in the call as by
     ``quantize_rows``.  ``items``: int8 with ``item_scale``.  Has no
     derivative."""
-    code = _TYPES.get(dtype)
-    if code is None:
-        raise ValueError(f"dtype must be float32, bfloat16 or float16: {dtype}")
+    code = _type_code(dtype)
     return _without_derivative(
         "quantized_scores", lambda: _ranking.quantized_scores(
             rows, items, item_scale, row_scale, code, out, _stream(rows)),
         out, rows, item_scale, row_scale)
 
 
-class Catalogue:
-    """Item factors (m x k, such as a model's V) in 8-bit integers, laid out
-    once, to score and rank them for users."""
+# --- scores in 4 bits -----------------------------------------------------------
 
-    def __init__(self, items: torch.Tensor):
-        self.items, self.scale = quantize_rows(items)
+def quantize_rows_mx4(x: torch.Tensor) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows in 4 bits with a power-of-two scale for each block of 32 columns
+    (the MXFP4 format): (q uint8 [rows, 16 blocks], scale uint8 [rows,
+    blocks]), the last block filled up with zeros.  include/bgmf.h has the
+    rounding and the layout.  The results are bytes, in no graph."""
+    return _checked(_ranking.quantize_rows_mx(x, _stream(x)))
+
+
+def dequantize_rows_mx4(q: torch.Tensor, scale: torch.Tensor, k: Optional[int] = None, *,
+                        dtype: torch.dtype = torch.float32,
+                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that rows in 4 bits stand for, [rows, k] as ``dtype``.
+    ``k``: columns, None for whole blocks."""
+    return _checked(_ranking.dequantize_rows_mx(q, scale, k, _type_code(dtype), out, _stream(q)))
+
+
+def mx4_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.Tensor,
+               row_scale: Optional[torch.Tensor] = None, *, dtype: torch.dtype = torch.float32,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Scores rows . items^T with both in 4 bits, summed in float32, as
+    ``dtype``.  ``rows``: uint8 with ``row_scale``, or float32, bfloat16 or
+    float16 without it, quantised in the call as by ``quantize_rows_mx4``.
+    ``items``: uint8 with ``item_scale``.  Has no derivative."""
+    code = _type_code(dtype)
+    return _without_derivative(
+        "mx4_scores", lambda: _ranking.mx_scores(rows, items, item_scale, row_scale, code, out,
+                                                 _stream(rows)),
+        out, rows)
+
+
+class Catalogue:
+    """Item factors (m x k, such as a model's V) in 8-bit integers, or with
+    ``bits=4`` in 4 bits with block scales (half the memory and the traffic, a
+    coarser score), laid out once, to score and rank them for users."""
+
+    def __init__(self, items: torch.Tensor, bits: int = 8):
+        if bits not in (4, 8):
+            raise ValueError(f"bits must be 8 or 4: {bits}")
+        self.bits = bits
+        self.items, self.scale = quantize_rows(items) if bits == 8 else quantize_rows_mx4(items)
 
     def scores(self, users: torch.Tensor, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """Scores of user factors (rows x k) over all items."""
+        if self.bits == 4:
+            return mx4_scores(users, self.items, self.scale, dtype=dtype)
         return quantized_scores(users, self.items, self.scale, dtype=dtype)
 
     def rank(self, users: torch.Tensor, given: Optional[torch.Tensor] = None, *, top: int = 10,
              temperature: float = 1.0, excluded: Optional[torch.Tensor] = None) -> LogProbs:
         """The best items for each user, with the log probability of a given
         item and the entropy, as by ``log_probs``, but without a derivative
-        with respect to the users: the scores are in 8-bit integers."""
+        with respect to the users: the scores are in 8-bit integers (or 4
+        bits)."""
         return log_probs(self.scores(users), given, top=top, temperature=temperature,
                          excluded=excluded)
+
+
+# --- learning from what users did with the answers ------------------------------
+
+class PolicyLoss(NamedTuple):
+    """Results of ``policy_loss``, one entry per row of scores."""
+    loss: torch.Tensor
+    log_prob: torch.Tensor  # of the shown item
+    kl: torch.Tensor        # divergence from the reference, 0 without one
+
+
+class _PolicyLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, scores, given, advantage, old_log_prob, reference, reference_log_prob,
+                kl_weight, clip_low, clip_high, temperature, excluded):
+        loss, log_prob, kl, state, _ = _checked(_ranking.policy_loss(
+            scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight,
+            clip_low, clip_high, temperature, excluded, 1, None, None, _stream(scores)))
+        ctx.save_for_backward(scores, given, reference, excluded, state)
+        ctx.kl_weight, ctx.temperature = kl_weight, temperature
+        ctx.mark_non_differentiable(log_prob, kl)
+        return loss, log_prob, kl
+
+    @staticmethod
+    def backward(ctx, g_loss, *_):
+        scores, given, reference, excluded, state = ctx.saved_tensors
+        weight = g_loss.resolve_neg().contiguous()
+        grad = _without_derivative(
+            "the gradient of policy_loss", lambda: _ranking.policy_loss_backward(
+                scores, given, state, weight, reference, ctx.kl_weight, ctx.temperature, excluded,
+                None, _stream(scores)),
+            None, scores, g_loss)
+        return (grad,) + (None,) * 10
+
+
+def _only_scores(name, **tensors):
+    for what, t in tensors.items():
+        if _in_graph(t):
+            raise ValueError(f"{name} has a derivative with respect to the scores alone, and "
+                             f"{what} requires grad (call .detach())")
+
+
+def policy_loss(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tensor,
+                old_log_prob: torch.Tensor, *, reference: Optional[torch.Tensor] = None,
+                reference_log_prob: Optional[torch.Tensor] = None, kl_weight: float = 0.0,
+                clip_low: float = 0.2, clip_high: float = 0.2, temperature: float = 1.0,
+                excluded: Optional[torch.Tensor] = None) -> PolicyLoss:
+    """Clipped policy loss of the items that were shown, row by row:
+    -min(rho A, clip(rho, 1 - clip_low, 1 + clip_high) A) + kl_weight kl with
+    rho = exp(log_prob - old_log_prob), without the softmax's probabilities
+    being stored.  ``scores`` (float32, bfloat16 or float16): the policy's, over
+    the catalogue; ``given`` (int32): the shown item, -1 for a row that fills
+    the batch up; ``advantage`` A and ``old_log_prob`` (float32): its log
+    probability when it was shown.  ``reference``: another policy's scores, for
+    the whole divergence, or ``reference_log_prob`` (float32): its log
+    probabilities of the shown items, for an estimate.  Differentiable with
+    respect to the scores through ``loss``.  include/bgmf.h says what empty
+    rows, infinities and NaN give."""
+    _only_scores("policy_loss", advantage=advantage, old_log_prob=old_log_prob,
+                 reference=reference, reference_log_prob=reference_log_prob)
+    if _in_graph(scores):
+        return PolicyLoss(*_PolicyLoss.apply(
+            scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight,
+            clip_low, clip_high, temperature, excluded))
+    return PolicyLoss(*_checked(_ranking.policy_loss(
+        scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight, clip_low,
+        clip_high, temperature, excluded, 0, None, None, _stream(scores)))[:3])
+
+
+def policy_loss_and_grad(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tensor,
+                         old_log_prob: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
+                         reference: Optional[torch.Tensor] = None,
+                         reference_log_prob: Optional[torch.Tensor] = None,
+                         kl_weight: float = 0.0, clip_low: float = 0.2, clip_high: float = 0.2,
+                         temperature: float = 1.0, excluded: Optional[torch.Tensor] = None,
+                         out: Optional[torch.Tensor] = None
+                         ) -> Tuple[PolicyLoss, torch.Tensor]:
+    """The results of ``policy_loss`` and the gradient of sum(weight * loss)
+    with respect to the scores (``weight`` float32, one entry per row; None:
+    ones), which are read once for both where a row fits a workgroup's
+    registers.  ``out`` may be the scores themselves.  For a loop that passes
+    the gradient on itself (``logits.backward(grad)``): the results are in no
+    graph."""
+    _only_scores("policy_loss_and_grad", advantage=advantage, old_log_prob=old_log_prob,
+                 reference=reference, reference_log_prob=reference_log_prob, weight=weight)
+    loss, log_prob, kl, _, grad = _checked(_ranking.policy_loss(
+        scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight, clip_low,
+        clip_high, temperature, excluded, 2, weight, out, _stream(scores)))
+    return PolicyLoss(loss, log_prob, kl), grad
+
+
+# --- dropout --------------------------------------------------------------------
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset):
+        ctx.p, ctx.seed = p, seed
+        ctx.offset = None
+        if isinstance(offset, torch.Tensor):
+            ctx.save_for_backward(offset)
+        else:
+            ctx.offset = offset
+        return _checked(_ranking.dropout(x, p, seed, offset, None, _stream(x)))
+
+    @staticmethod
+    def backward(ctx, g):
+        offset = ctx.saved_tensors[0] if ctx.offset is None else ctx.offset
+        return dropout(g.resolve_neg().contiguous(), ctx.p, ctx.seed, offset), None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, seed: int, offset=0, *,
+            out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Elements of ``x`` (float32, bfloat16 or float16; contiguous, or 2-D with
+    adjacent row elements) set to 0 with probability ``p``, the others times
+    1 / (1 - p).  Which ones depends on ``seed``, ``offset`` (in [0, 2^64)) and
+    the element's place alone (include/bgmf.h has the generator), so no mask is
+    stored: the backward pass draws it again.  A call uses the offsets from
+    ``offset`` up to ``offset + ceil(x.numel() / 4)``.  ``offset`` may be an
+    int64 tensor of one element on the GPU, read when the kernel runs: a
+    captured graph that adds to it drops other elements on each replay (it must
+    not change between a forward and its backward pass, which raises).  ``out``
+    may be ``x`` itself."""
+    if _in_graph(x):
+        if out is not None:
+            raise ValueError("dropout: out takes no part in a graph, and x requires grad")
+        return _Dropout.apply(x, p, seed, offset)
+    return _checked(_ranking.dropout(x, p, seed, offset, out, _stream(x)))
 
 
 # --- clipping -------------------------------------------------------------------
