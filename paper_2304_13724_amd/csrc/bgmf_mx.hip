@@ -197,65 +197,495 @@ struct Product {
 };
 
 // v_mfma_scale_f32_32x32x64_f8f6f4 on 4-bit values: lane l holds block l / 32
-// (of two) of row l % 32 of either side, and its scale.  Register g of a lane
-// is the sum of user 8 (g / 4) + 4 (l / 32) + g % 4 and item l % 32.
+// (of two) of row l % 32 of either side, and in byte SEL of a word its scale.
+// Register g of a lane is the sum of row 8 (g / 4) + 4 (l / 32) + g % 4 of a and
+// row l % 32 of b.
+template <int SEL>
 __device__ __forceinline__ f32x16 multiply(i32x4 a, int a_scale, i32x4 b, int b_scale, f32x16 c) {
   const i32x8 x = {a.x, a.y, a.z, a.w, 0, 0, 0, 0}, y = {b.x, b.y, b.z, b.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, a_scale, 0, b_scale);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, SEL, a_scale, SEL,
+                                                         b_scale);
 }
 
+// 16 bytes at any address.  STREAM: items that the caches cannot keep until the
+// next call are read past them.
+template <bool STREAM = false>
 __device__ __forceinline__ i32x4 block_bytes(const uint8_t *p) {
   typedef int32_t quad __attribute__((ext_vector_type(4), aligned(1)));
-  return *reinterpret_cast<const quad *>(p);
+  const quad *q = reinterpret_cast<const quad *>(p);
+  if constexpr (STREAM) return __builtin_nontemporal_load(q);
+  else return *q;
 }
 
-// A wave takes tiles of 32 items and the 32 users of blockIdx.y.
-template <class O>
-__global__ void __launch_bounds__(kThreads) k_mx_few(Product P) {
+// Few users (32 for each blockIdx.y): every item's bytes go from global memory
+// into a matrix instruction once.  A wave takes ITEMS tiles of 32 items and
+// STEPS pairs of blocks at a time; while it stores their scores, the bytes and
+// scales of its next ones are on their way.  LONG: rows of more than STEPS pairs
+// (with one tile at a time).
+template <class O, int STEPS, int ITEMS, bool LONG, bool STREAM>
+__global__ void __launch_bounds__(kThreads, 4) k_mx_few(Product P) {
+  static_assert(!LONG || ITEMS == 1, "one tile at a time");
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int l32 = lane % 32, half = lane / 32;
-  const int64_t r0 = (int64_t)blockIdx.y * 32, tiles = (P.items + 31) / 32;
+  const int64_t r0 = (int64_t)blockIdx.y * 32, tiles = (P.items + 32 * ITEMS - 1) / (32 * ITEMS);
   const int64_t r = r0 + l32 < P.rows ? r0 + l32 : P.rows - 1;
   const uint8_t *a = P.a + r * P.a_stride, *as = P.a_scale + r * P.as_stride;
-  for (int64_t tile = (int64_t)blockIdx.x * kWaves + wave; tile < tiles;
-       tile += (int64_t)gridDim.x * kWaves) {
-    const int64_t item = tile * 32 + l32, j = item < P.items ? item : P.items - 1;
-    const uint8_t *b = P.b + j * P.b_stride, *bs = P.b_scale + j * P.bs_stride;
-    f32x16 acc = {};
-    for (int32_t s = 0; s < P.blocks; s += 2) {
-      const int32_t at = s + half;
-      i32x4 x = {}, y = {};
-      int xs = 0, ys = 0;
-      if (at < P.blocks) {
-        x = block_bytes(a + (int64_t)at * 16), xs = as[at];
-        y = block_bytes(b + (int64_t)at * 16), ys = bs[at];
-      }
-      acc = multiply(x, xs, y, ys, acc);
-    }
-    if (item >= P.items) continue;
+  int64_t tile = (int64_t)blockIdx.x * kWaves + wave;
+  const int64_t stride = (int64_t)gridDim.x * kWaves;
+  if (tile >= tiles) return;
+  i32x4 x[ITEMS][STEPS], y[STEPS];
+  int xs[ITEMS][STEPS], ys[STEPS];
+  const auto users = [&](int32_t s0) {
 #pragma unroll
-    for (int g = 0; g < 16; ++g) {
-      const int64_t u = r0 + 8 * (g / 4) + 4 * half + g % 4;
-      if (u < P.rows) static_cast<O *>(P.out)[u * P.out_stride + item] = from_float<O>(acc[g]);
+    for (int s = 0; s < STEPS; ++s) {
+      const int32_t at = (s0 + s) * 2 + half;
+      y[s] = i32x4{}, ys[s] = 0;
+      if (at < P.blocks) y[s] = block_bytes(a + (int64_t)at * 16), ys[s] = as[at];
+    }
+  };
+  const auto items = [&](int64_t t, int i, int32_t s0) {
+    int64_t j = t * (32 * ITEMS) + i * 32 + l32;
+    if (j >= P.items) j = P.items - 1;
+    const uint8_t *b = P.b + j * P.b_stride, *bs = P.b_scale + j * P.bs_stride;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) {
+      const int32_t at = (s0 + s) * 2 + half;
+      x[i][s] = i32x4{}, xs[i][s] = 0;
+      if (at < P.blocks) x[i][s] = block_bytes<STREAM>(b + (int64_t)at * 16), xs[i][s] = bs[at];
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < ITEMS; ++i) items(tile, i, 0);
+  if constexpr (!LONG) users(0);
+  for (; tile < tiles; tile += stride) {
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+      f32x16 acc = {};
+      for (int32_t s0 = 0;;) {
+        if constexpr (LONG) users(s0);
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) acc = multiply<0>(y[s], ys[s], x[i][s], xs[i][s], acc);
+        if constexpr (LONG) {
+          s0 += STEPS;
+          if (s0 * 2 < P.blocks) {
+            items(tile, i, s0);
+            continue;
+          }
+        }
+        break;
+      }
+      if (tile + stride < tiles) items(tile + stride, i, 0);
+      const int64_t j = tile * (32 * ITEMS) + i * 32 + l32;
+      if (j >= P.items) continue;
+      O *to = static_cast<O *>(P.out) + j;
+#pragma unroll
+      for (int g = 0; g < 16; ++g) {
+        const int64_t u = r0 + 8 * (g / 4) + 4 * half + g % 4;
+        if (r0 + 8 * (g / 4) + g % 4 >= P.rows) continue;  // of the whole wave
+        if (u < P.rows) to[u * P.out_stride] = from_float<O>(acc[g]);
+      }
     }
   }
 }
 
-// Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
-constexpr int64_t kFullGpu = 2048;
+// Many users: a workgroup of 2 x 2 waves takes tiles of 64 BI items x 64 BU
+// users, each wave a quarter of it in BI x BU blocks of 32 x 32.  STEP bytes of
+// a row (STEP / 16 blocks) at a time pass through LDS, in chunks of a block
+// whose place in a row is swizzled so that 16 lanes that read 16 rows meet all
+// 64 banks, and the row's scales as two words: those of its even blocks, then
+// those of its odd ones.
+constexpr int64_t kUserPad = 256;
+constexpr int64_t kMostStride = 1 << 23;  // bytes from an item to the next (128 rows: 2^30)
+
+template <class O, int BI, int BU, int STEP>
+struct Many {
+  static constexpr int kItems = 64 * BI, kUsers = 64 * BU, kChunks = STEP / 16;
+  static constexpr int kSubs = kChunks / 2;  // pairs of blocks of a step
+  static constexpr int kPass = kThreads / kChunks;  // rows that the workgroup loads at a time
+  // of a thread (where a pass has more rows than there are, some threads' none)
+  static constexpr int kItemLoads = (kItems + kPass - 1) / kPass;
+  static constexpr int kUserLoads = (kUsers + kPass - 1) / kPass;
+  static constexpr int kBuffer = (kItems + kUsers) * kChunks;  // i32x4 of a step
+  static constexpr int kScaleLoads = (kItems + kUsers + kThreads - 1) / kThreads;
+  static constexpr int kScaleWords = kScaleLoads * kThreads * 2;  // of a step
+  static constexpr int kPitch = 32 * BI + 16 / (int)sizeof(O);  // of the scores on their way out
+  static constexpr int kScores = kWaves * 32 * kPitch * (int)sizeof(O) / 16;  // i32x4
+
+  static __device__ __forceinline__ int at(int row, int c) {
+    if constexpr (kChunks == 2) return row * 2 + c;
+    else if constexpr (kChunks == 4) return row * 4 + (c ^ ((row >> 2) & 3));
+    else return row * 8 + (c ^ ((row >> 1) & 7));
+  }
+
+  // Tile t in the order in which workgroups take them: these go to the eight
+  // XCDs in turn, and each XCD gets a part of the tiles of its own, four users'
+  // tiles by one items' after another, so that its L2 serves many of them.  The
+  // last items' tile goes back so far that it is whole.
+  static __device__ __forceinline__ void place(const Product &P, int64_t t, int64_t &j0,
+                                               int64_t &r0) {
+    const int64_t item_tiles = (P.items + kItems - 1) / kItems;
+    const int64_t user_tiles = (P.rows + kUsers - 1) / kUsers, tiles = item_tiles * user_tiles;
+    const int64_t xcd = t % 8, per = tiles / 8, more = tiles % 8;
+    const int64_t i = xcd * per + (xcd < more ? xcd : more) + t / 8;
+    constexpr int64_t kGroup = 4;
+    const int64_t group = i / (kGroup * item_tiles), in = i % (kGroup * item_tiles);
+    const int64_t left = user_tiles - group * kGroup, size = left < kGroup ? left : kGroup;
+    j0 = in / size * kItems;
+    if (j0 > P.items - kItems) j0 = P.items - kItems;
+    r0 = (group * kGroup + in % size) * kUsers;
+  }
+
+  // A thread's blocks of step s of the items from j0 on (kItems of them are
+  // there) and of the users from r0 on (whose rows are laid out up to a multiple
+  // of kUserPad).  A thread's offset within its first row is 32 bits wide (see
+  // kMostStride).  PAD (rows of at least kChunks blocks): without branches; the
+  // users' rows have blocks of zeros up to a multiple of kChunks, and in place of
+  // an item's blocks past its row come its last one with scales of 0, so that
+  // their products are 0.
+  template <bool PAD = false>
+  static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
+                                              i32x4 (&x)[kItemLoads], i32x4 (&y)[kUserLoads]) {
+    const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+    const bool some = PAD || s * kChunks + chunk < P.blocks;
+    const int32_t c = min(s * kChunks + chunk, P.blocks - 1);
+    const uint32_t at_item = (uint32_t)row * (uint32_t)P.b_stride + (uint32_t)c * 16;
+    const uint32_t at_user = (uint32_t)row * (uint32_t)P.a_stride + chunk * 16;
+    const uint8_t *b = P.b + j0 * P.b_stride;
+    const uint8_t *a = P.a + (r0 * P.a_stride + (int64_t)s * STEP);
+#pragma unroll
+    for (int h = 0; h < kItemLoads; ++h) {
+      x[h] = i32x4{};
+      if (some && (kPass <= kItems || row < kItems))
+        x[h] = block_bytes(b + h * kPass * P.b_stride + at_item);
+    }
+#pragma unroll
+    for (int h = 0; h < kUserLoads; ++h) {
+      y[h] = i32x4{};
+      if (some) y[h] = block_bytes(a + h * kPass * P.a_stride + at_user);
+    }
+  }
+  static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kItemLoads],
+                                               const i32x4 (&y)[kUserLoads]) {
+    const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+#pragma unroll
+    for (int h = 0; h < kItemLoads; ++h)
+      if (kPass <= kItems || row < kItems) buffer[at(row + kPass * h, chunk)] = x[h];
+#pragma unroll
+    for (int h = 0; h < kUserLoads; ++h)
+      if (kPass <= kUsers || row < kUsers)
+        buffer[kItems * kChunks + at(row + kPass * h, chunk)] = y[h];
+  }
+  // The scales of a thread's rows (items, then users) in step s, as they are.
+  struct Scales {
+    uint32_t w[kScaleLoads][2];
+  };
+  template <bool PAD = false>
+  static __device__ __forceinline__ void load_scales(const Product &P, int64_t j0, int64_t r0,
+                                                     int s, Scales &scale) {
+    const int32_t c = s * kChunks;
+#pragma unroll
+    for (int h = 0; h < kScaleLoads; ++h) {
+      const int i = threadIdx.x + h * kThreads;
+      scale.w[h][0] = scale.w[h][1] = 0;
+      if (kScaleLoads * kThreads > kItems + kUsers && i >= kItems + kUsers) continue;
+      const bool item = kItems % kThreads == 0 ? h * kThreads < kItems : i < kItems;
+      const uint8_t *p = item ? P.b_scale + (j0 + i) * P.bs_stride
+                              : P.a_scale + (r0 + i - kItems) * P.as_stride;
+      if constexpr (PAD) {
+        const int32_t from = min(c, P.blocks - kChunks), past = c - from;  // below 8
+        uint64_t w;
+        __builtin_memcpy(&w, p + from, 8);
+        w >>= past * 8;
+        scale.w[h][0] = (uint32_t)w, scale.w[h][1] = (uint32_t)(w >> 32);
+        continue;
+      }
+      p += c;
+      if (c + kChunks <= P.blocks) {
+        __builtin_memcpy(scale.w[h], p, kChunks);
+      } else {
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k)
+          if (c + k < P.blocks) scale.w[h][k / 4] |= (uint32_t)p[k] << (k % 4 * 8);
+      }
+    }
+  }
+  static __device__ __forceinline__ void store_scales(uint32_t *words, const Scales &scale) {
+#pragma unroll
+    for (int h = 0; h < kScaleLoads; ++h) {
+      const uint2 w = {__builtin_amdgcn_perm(scale.w[h][1], scale.w[h][0], 0x06040200u),
+                       __builtin_amdgcn_perm(scale.w[h][1], scale.w[h][0], 0x07050301u)};
+      *reinterpret_cast<uint2 *>(words + (threadIdx.x + h * kThreads) * 2) = w;
+    }
+  }
+  // A wave's bytes of a pair of blocks, and its scales of a step.
+  static __device__ __forceinline__ void read(const i32x4 *buffer, int sub, i32x4 (&fi)[BI],
+                                              i32x4 (&fu)[BU]) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int c = sub * 2 + lane / 32;
+#pragma unroll
+    for (int h = 0; h < BI; ++h) fi[h] = buffer[at((wave % 2 * BI + h) * 32 + lane % 32, c)];
+#pragma unroll
+    for (int h = 0; h < BU; ++h)
+      fu[h] = buffer[kItems * kChunks + at((wave / 2 * BU + h) * 32 + lane % 32, c)];
+  }
+  static __device__ __forceinline__ void read_scales(const uint32_t *words, int (&si)[BI],
+                                                     int (&su)[BU]) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+#pragma unroll
+    for (int h = 0; h < BI; ++h)
+      si[h] = (int)words[((wave % 2 * BI + h) * 32 + lane % 32) * 2 + lane / 32];
+#pragma unroll
+    for (int h = 0; h < BU; ++h)
+      su[h] = (int)words[(kItems + (wave / 2 * BU + h) * 32 + lane % 32) * 2 + lane / 32];
+  }
+  template <int SUB>
+  static __device__ __forceinline__ void products(f32x16 (&acc)[BI][BU], const i32x4 (&fi)[BI],
+                                                  const i32x4 (&fu)[BU], const int (&si)[BI],
+                                                  const int (&su)[BU]) {
+#pragma unroll
+    for (int i = 0; i < BI; ++i)
+#pragma unroll
+      for (int u = 0; u < BU; ++u)
+        acc[i][u] = multiply<SUB>(fi[i], si[i], fu[u], su[u], acc[i][u]);
+  }
+
+  // Register g of a lane is the sum of item 8 (g / 4) + 4 (l / 32) + g % 4 and
+  // user l % 32.  The scores of 32 users at a time pass through LDS (lds: the
+  // whole workgroup's), so that a user's 32 BI scores are stored in a row.
+  static __device__ __forceinline__ void store_scores(const Product &P, int64_t j0, int64_t r0,
+                                                      const f32x16 (&acc)[BI][BU], i32x4 *lds) {
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int wi = wave % 2, wu = wave / 2, l32 = lane % 32, half = lane / 32;
+    O *mine = reinterpret_cast<O *>(lds) + wave * (32 * kPitch);
+    constexpr int N = Vec<O>::N, kLanes = 32 * BI / N;  // lanes of a user's row
+#pragma unroll
+    for (int u = 0; u < BU; ++u) {
+#pragma unroll
+      for (int i = 0; i < BI; ++i)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const int ji = i * 32 + g * 8 + half * 4;
+          O v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = from_float<O>(acc[i][u][g * 4 + e]);
+          __builtin_memcpy(__builtin_assume_aligned(mine + l32 * kPitch + ji, 4 * sizeof(O)), v,
+                           4 * sizeof(O));
+        }
+      __builtin_amdgcn_wave_barrier();
+      const int64_t r1 = r0 + (wu * BU + u) * 32 + lane / kLanes;
+      const int ji = lane % kLanes * N;
+      O *to = static_cast<O *>(P.out) + r1 * P.out_stride + (j0 + wi * BI * 32 + ji);
+#pragma unroll
+      for (int q = 0; q < 32 * kLanes / 64; ++q) {
+        const int ru = q * (64 / kLanes);
+        const Vec<O> v =
+            *reinterpret_cast<const Vec<O> *>(mine + (ru + lane / kLanes) * kPitch + ji);
+        if (r1 + ru < P.rows) store_vec(to + ru * P.out_stride, v);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+};
+
+// Tiles of 128 or 64 items x 128 or 64 users: three or four workgroups on a CU
+// overlap their loads, products and stores.  A workgroup's bytes of the next
+// step, or of its next tile, are on their way into registers meanwhile.
+template <class O, int BI, int BU, int STEP>
+__global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4)
+    k_mx_many(Product P, int64_t tiles) {
+  using M = Many<O, BI, BU, STEP>;
+  __shared__ i32x4 lds[M::kBuffer > M::kScores ? M::kBuffer : M::kScores];
+  __shared__ uint32_t s_scale[M::kScaleWords];
+  const int steps = (P.blocks + M::kChunks - 1) / M::kChunks;
+  i32x4 x[M::kItemLoads], y[M::kUserLoads];
+  typename M::Scales scale;
+  const auto load = [&](int64_t j0, int64_t r0, int s) {
+    M::load(P, j0, r0, s, x, y);
+    M::load_scales(P, j0, r0, s, scale);
+  };
+  f32x16 acc[BI][BU] = {};
+  int64_t tile = blockIdx.x, j0, r0;
+  M::place(P, tile, j0, r0);
+  load(j0, r0, 0);
+  for (int s = 0; tile < tiles;) {
+    __syncthreads();
+    M::store(lds, x, y);
+    M::store_scales(s_scale, scale);
+    __syncthreads();
+    const bool last = s + 1 == steps;
+    int64_t jn = j0, rn = r0;
+    const int64_t next = last ? tile + gridDim.x : tile;
+    if (next < tiles) {
+      if (last) M::place(P, next, jn, rn);
+      load(jn, rn, last ? 0 : s + 1);
+    }
+    int si[BI], su[BU];
+    M::read_scales(s_scale, si, su);
+    i32x4 fi[BI], fu[BU];
+    M::read(lds, 0, fi, fu);
+    M::template products<0>(acc, fi, fu, si, su);
+    if constexpr (M::kSubs > 1) {
+      M::read(lds, 1, fi, fu);
+      M::template products<1>(acc, fi, fu, si, su);
+    }
+    ++s;
+    if (last) {
+      __syncthreads();
+      M::store_scores(P, j0, r0, acc, lds);
+#pragma unroll
+      for (int i = 0; i < BI; ++i)
+#pragma unroll
+        for (int u = 0; u < BU; ++u) acc[i][u] = f32x16{};
+      tile = next, j0 = jn, r0 = rn, s = 0;
+    }
+  }
+}
+
+// Long rows: tiles of 256 x 256, eight blocks at a time, which halves the LDS
+// traffic per product.  One workgroup fills a CU, so a wave itself reads its
+// next pair of blocks from LDS while the matrix unit works, and a step's bytes
+// are loaded a whole step before they go to the other LDS buffer.
+// Kinds of instructions that the scheduler is told to place.
+constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
 
 template <class O>
-hipError_t product(Product p, hipStream_t stream) {
-  const int64_t all = (p.items + 32 * kWaves - 1) / (32 * kWaves);
+__global__ void __launch_bounds__(kThreads, 1) k_mx_large(Product P) {
+  using M = Many<O, 4, 4, 128>;
+  __shared__ i32x4 lds[2 * M::kBuffer > M::kScores ? 2 * M::kBuffer : M::kScores];
+  __shared__ uint32_t s_scale[2][M::kScaleWords];
+  const int steps = (P.blocks + 7) / 8;
+  int64_t j0, r0;
+  M::place(P, blockIdx.x, j0, r0);
+  i32x4 x[M::kItemLoads], y[M::kUserLoads];
+  typename M::Scales scale;
+  const auto load = [&](int s) {  // past the last step: it once more, for nothing
+    M::template load<true>(P, j0, r0, min(s, steps - 1), x, y);
+    M::template load_scales<true>(P, j0, r0, min(s, steps - 1), scale);
+  };
+  load(0);
+  M::store(lds, x, y);
+  M::store_scales(s_scale[0], scale);
+  load(1);
+  __syncthreads();
+  f32x16 acc[4][4] = {};
+  i32x4 fi[2][4], fu[2][4];
+  int si[4], su[4], si_next[4], su_next[4];
+  M::read_scales(s_scale[0], si, su);
+  M::read(lds, 0, fi[0], fu[0]);
+  // Between two barriers: 48 products with the reads of the next blocks, the
+  // writes of the next step and the loads of the one after it spread over them.
+  for (int s = 0; s < steps; ++s) {
+    i32x4 *now = lds + s % 2 * M::kBuffer, *other = lds + (s + 1) % 2 * M::kBuffer;
+    M::read(now, 1, fi[1], fu[1]);
+    M::template products<0>(acc, fi[0], fu[0], si, su);
+    M::read(now, 2, fi[0], fu[0]);
+    M::template products<1>(acc, fi[1], fu[1], si, su);
+    M::read(now, 3, fi[1], fu[1]);
+    M::template products<2>(acc, fi[0], fu[0], si, su);
+    M::store(other, x, y);
+    M::store_scales(s_scale[(s + 1) % 2], scale);
+    load(s + 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    }
+    __syncthreads();
+    __builtin_amdgcn_sched_barrier(0);  // the last products cover the next step's first reads
+    M::read_scales(s_scale[(s + 1) % 2], si_next, su_next);
+    M::read(other, 0, fi[0], fu[0]);
+    M::template products<3>(acc, fi[1], fu[1], si, su);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) si[h] = si_next[h], su[h] = su_next[h];
+  }
+  __syncthreads();
+  M::store_scores(P, j0, r0, acc, lds);
+}
+
+// Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
+constexpr int64_t kFullGpu = 2048;
+constexpr int64_t kCached = 192 << 20;  // items that stay in the 256 MB Infinity Cache
+
+template <class O, int STEPS, int ITEMS, bool LONG>
+void launch_few(Product p, hipStream_t stream) {
+  const int64_t all = (p.items + 32 * ITEMS * kWaves - 1) / (32 * ITEMS * kWaves);
+  // equally many tiles for each
+  const int64_t rounds = (all + kFullGpu - 1) / kFullGpu, groups = (all + rounds - 1) / rounds;
+  const bool stream_items = p.rows <= 32 && p.items * (int64_t)p.blocks * 16 > kCached;
   constexpr int64_t kMost = 65535ll * 32;  // users of a launch
   for (int64_t left = p.rows; left > 0; left -= kMost) {
     p.rows = std::min(left, kMost);
-    const int64_t users = (p.rows + 31) / 32;
-    const dim3 grid((unsigned)std::min(all, std::max(kFullGpu / users, (int64_t)1) * 4),
-                    (unsigned)users);
-    hipLaunchKernelGGL(k_mx_few<O>, grid, dim3(kThreads), 0, stream, p);
+    const dim3 grid((unsigned)groups, (unsigned)((p.rows + 31) / 32));
+    if (stream_items)
+      hipLaunchKernelGGL((k_mx_few<O, STEPS, ITEMS, LONG, true>), grid, dim3(kThreads), 0, stream,
+                         p);
+    else
+      hipLaunchKernelGGL((k_mx_few<O, STEPS, ITEMS, LONG, false>), grid, dim3(kThreads), 0, stream,
+                         p);
     p.a += kMost * p.a_stride, p.a_scale += kMost * p.as_stride;
     p.out = static_cast<O *>(p.out) + kMost * p.out_stride;
+  }
+}
+
+template <class O, int BI, int BU, int STEP>
+void launch_many(const Product &p, hipStream_t stream) {
+  const int64_t all =
+      (p.items + 64 * BI - 1) / (64 * BI) * ((p.rows + 64 * BU - 1) / (64 * BU));
+  constexpr int64_t kAtOnce = 256 * (BI * BU == 4 ? 3 : 4);
+  hipLaunchKernelGGL((k_mx_many<O, BI, BU, STEP>), dim3((unsigned)std::min(all, kAtOnce)),
+                     dim3(kThreads), 0, stream, p, all);
+}
+
+constexpr int64_t kLargeBlocks = 32;
+inline bool uses_few(int64_t rows, int64_t items, int64_t items_stride) {
+  return rows <= 32 || items < 128 || items_stride > kMostStride;
+}
+
+template <class O>
+hipError_t product(const Product &p, hipStream_t stream) {
+  const auto tiles = [&](int64_t items, int64_t users) {
+    return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
+  };
+  if (uses_few(p.rows, p.items, p.b_stride)) {
+    const bool small = p.items < 32 * kFullGpu * kWaves;
+    if (p.blocks <= 2) {
+      if (small) launch_few<O, 1, 1, false>(p, stream);
+      else launch_few<O, 1, 8, false>(p, stream);
+    } else if (p.blocks <= 4) {
+      if (small) launch_few<O, 2, 1, false>(p, stream);
+      else launch_few<O, 2, 4, false>(p, stream);
+    } else if (p.blocks <= 8) {
+      if (small) launch_few<O, 4, 1, false>(p, stream);
+      else launch_few<O, 4, 2, false>(p, stream);
+    } else {
+      launch_few<O, 4, 1, true>(p, stream);
+    }
+  } else if (p.blocks >= kLargeBlocks && p.items >= 256 && tiles(256, 256) >= 256) {
+    hipLaunchKernelGGL(k_mx_large<O>, dim3((unsigned)tiles(256, 256)), dim3(kThreads), 0, stream,
+                       p);
+  } else if (p.rows > 64 && tiles(128, 128) >= 256) {
+    if (p.blocks <= 2) launch_many<O, 2, 2, 32>(p, stream);
+    else launch_many<O, 2, 2, 64>(p, stream);
+  } else if (tiles(128, 64) >= 256) {
+    if (p.blocks <= 2) launch_many<O, 2, 1, 32>(p, stream);
+    else launch_many<O, 2, 1, 64>(p, stream);
+  } else {
+    if (p.blocks <= 2) launch_many<O, 1, 1, 32>(p, stream);
+    else launch_many<O, 1, 1, 64>(p, stream);
   }
   return hipGetLastError();
 }
@@ -264,8 +694,32 @@ inline int64_t round_up(int64_t x, int64_t to) { return (x + to - 1) / to * to; 
 inline int64_t blocks_of(int64_t k) { return (k + kBlock - 1) / kBlock; }
 constexpr int64_t kMostK = (1 << 20) - 1;  // of a product
 
-// Workspace: the users' bytes, then their scales.
-int64_t bytes_part(int64_t rows, int64_t k) { return round_up(rows * blocks_of(k) * 16, 256); }
+// Workspace: the users' bytes up to a multiple of kUserPad rows (and of eight
+// blocks, the last ones 0, where k_mx_large may read them), then their scales.
+int64_t padded_rows(int64_t rows) { return rows > 32 ? round_up(rows, kUserPad) : rows; }
+int64_t padded_blocks(int64_t rows, int64_t k) {
+  const int64_t blocks = blocks_of(k);
+  return rows > 32 && blocks >= kLargeBlocks ? round_up(blocks, 8) : blocks;
+}
+int64_t bytes_part(int64_t rows, int64_t k) {
+  return round_up(padded_rows(rows) * padded_blocks(rows, k) * 16, 256);
+}
+
+// Rows given in 4 bits, into the workspace's layout.
+__global__ void __launch_bounds__(kThreads) k_copy_mx(Product P, uint8_t *q, uint8_t *scale,
+                                                      int32_t padded) {
+  const int64_t all = P.rows * padded;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < all;
+       i += (int64_t)gridDim.x * kThreads) {
+    const int64_t r = i / padded, c = i % padded;
+    i32x4 x = {};
+    uint8_t s = 0;
+    if (c < P.blocks)
+      x = block_bytes(P.a + r * P.a_stride + c * 16), s = P.a_scale[r * P.as_stride + c];
+    *reinterpret_cast<i32x4 *>(q + i * 16) = x;
+    scale[i] = s;
+  }
+}
 
 int check_rows(const char *call, int64_t rows, int64_t k, int64_t most_k) {
   if (rows < 0 || rows >= (1ll << 31) || k < 1 || k > most_k)
@@ -345,9 +799,9 @@ int bgmf_dequantize_rows_mx(const uint8_t *q, int64_t q_stride, const uint8_t *s
 
 int64_t bgmf_mx_scores_workspace(int64_t rows, int64_t item_count, int64_t k, int32_t type) {
   if (rows <= 0 || k <= 0 || item_count <= 0 || rows >= (1ll << 31) || k > kMostK ||
-      type == BGMF_TYPE_MX4)
+      (type == BGMF_TYPE_MX4 && (rows <= 32 || item_count < 128)))
     return 0;
-  return bytes_part(rows, k) + round_up(rows * blocks_of(k), 256);
+  return bytes_part(rows, k) + round_up(padded_rows(rows) * padded_blocks(rows, k), 256);
 }
 
 int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t row_stride,
@@ -406,11 +860,19 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
             items, item_scale, item_count, items_stride, item_scale_stride, (int32_t)blocks,
             out, out_stride};
   hipError_t e = hipSuccess;
-  if (own) {
+  if (own || !uses_few(rows, item_count, items_stride)) {
     uint8_t *q = static_cast<uint8_t *>(ws), *scale = q + bytes_part(rows, k);
-    e = quantize_mx(type, Rows{x, rows, row_stride, (int32_t)k, (int32_t)(blocks * 4), q, scale,
-                               bytes, blocks}, stream);
-    p.a = q, p.a_scale = scale, p.a_stride = bytes, p.as_stride = blocks;
+    const int64_t laid = padded_blocks(rows, k);
+    if (own) {
+      e = quantize_mx(type, Rows{x, rows, row_stride, (int32_t)k, (int32_t)(laid * 4), q, scale,
+                                 laid * 16, laid}, stream);
+    } else {
+      const int64_t groups = std::min<int64_t>((rows * laid + kThreads - 1) / kThreads, 4096);
+      hipLaunchKernelGGL(k_copy_mx, dim3((unsigned)groups), dim3(kThreads), 0, stream, p, q, scale,
+                         (int32_t)laid);
+      e = hipGetLastError();
+    }
+    p.a = q, p.a_scale = scale, p.a_stride = laid * 16, p.as_stride = laid;
   }
   if (e == hipSuccess)
     e = out_type == BGMF_TYPE_F32    ? product<float>(p, stream)
