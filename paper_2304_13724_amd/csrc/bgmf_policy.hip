@@ -120,6 +120,37 @@ __device__ __forceinline__ Sums<REF> block_sums(Sums<REF> a, float c, SumsLds<TH
   return r;
 }
 
+// exp(x) - 1 and exp(x) to 6e-10 of themselves, by the series of exp over [-ln 2 /
+// 2, ln 2 / 2] to the eighth power and a power of two; ln S, to as much, from a
+// 32-bit logarithm y and what S exp(-y) is off from 1 (below 1e-5, so that two
+// terms of the series of ln(1 + d) do).  The library's functions would take twice
+// the registers of everything else in these kernels.
+struct Exp {
+  double less1, value;
+  __device__ __forceinline__ explicit Exp(double x) {
+    const double most = x > 1000.0 ? 1000.0 : x < -1100.0 ? -1100.0 : x;  // NaN stays
+    const double k = rint(most * 1.4426950408889634074);
+    double r = fma(-k, 0x1.62e42fefa39efp-1, most);
+    r = fma(-k, 0x1.abc9e3b39803fp-56, r);
+    double p = 1.0 / 40320.0;
+    p = fma(p, r, 1.0 / 5040.0);
+    p = fma(p, r, 1.0 / 720.0);
+    p = fma(p, r, 1.0 / 120.0);
+    p = fma(p, r, 1.0 / 24.0);
+    p = fma(p, r, 1.0 / 6.0);
+    p = fma(p, r, 0.5);
+    p = fma(p * r, r, r);
+    const int e = (int)k;  // (0 for a NaN, whose r is NaN)
+    value = ldexp(1.0 + p, e);
+    less1 = e == 0 ? p : value - 1.0;
+  }
+};
+__device__ __forceinline__ double ln(double s) {  // s > 0, in the range of 32 bits, or NaN
+  const double y = (double)__builtin_amdgcn_logf((float)s) * kLn2;
+  const double d = s * Exp(-y).value - 1.0;
+  return y + fma(-0.5 * d, d, d);
+}
+
 // What the gradient needs of a row: with d and dy as above,
 //   dx_j = g / t (slope (1[j = given] - p_j) + kl_weight p_j ln 2 (d_j - dy_j - mean))
 struct State {
@@ -136,21 +167,21 @@ __device__ __forceinline__ State finish(const Policy &P, int64_t r, const Sums<R
     st.s = 0.0f;
   } else {
     const bool outside = g < 0 || g >= P.cols, none = a.s == 0.0;
-    const double ln_s = none ? 0.0 : log(a.s);
+    const double ln_s = none ? 0.0 : ln(a.s);
     lp = -INFINITY;
     if (outside) lp = NAN;
     else if (!none && !(P.ex && P.ex[r * P.ex_stride + g]))
       lp = ((double)to_float(static_cast<const T *>(P.x)[r * P.stride + g]) - (double)a.m) /
                (double)P.temperature - ln_s;
     if (!none || outside) {
-      const double A = P.advantage[r], rho = exp(lp - (double)P.old_log_prob[r]);
+      const double A = P.advantage[r], rho = Exp(lp - (double)P.old_log_prob[r]).value;
       const double lo = 1.0 - (double)P.clip_low, hi = 1.0 + (double)P.clip_high;
       const double unclipped = rho * A, clipped = (rho < lo ? lo : rho > hi ? hi : rho) * A;
       const bool passes = !(unclipped > clipped);
       loss = -(passes ? unclipped : clipped);
       double slope = passes ? -unclipped : 0.0;
       if (P.ref_log_prob) {
-        const double z = (double)P.ref_log_prob[r] - lp, e = expm1(z);
+        const double z = (double)P.ref_log_prob[r] - lp, e = Exp(z).less1;
         kl = z == INFINITY ? INFINITY : e - z;
         if (P.kl_weight != 0.0f) slope -= (double)P.kl_weight * e;
       }
@@ -160,7 +191,7 @@ __device__ __forceinline__ State finish(const Policy &P, int64_t r, const Sums<R
       if (!none) {
         const double mean = a.w / a.s;
         st.mean = (float)mean;
-        kl = a.sy == 0.0 ? INFINITY : mean * kLn2 - ln_s + log(a.sy);
+        kl = a.sy == 0.0 ? INFINITY : mean * kLn2 - ln_s + ln(a.sy);
       }
     }
     if (P.kl_weight != 0.0f) loss += (double)P.kl_weight * kl;
@@ -180,40 +211,126 @@ struct PartSum {
   float m, my;
 };
 
+// A row's gradient but for its given item's own term: with d, dy and e = exp2(d),
+//   p (gk (d - dy - mean) - gs) = e (slope (d - dy) + level)
+// and 0 for items of probability 0, excluded ones among them.  A row whose level
+// is NaN (bad) has NaN for every item that is not excluded.
+template <bool REF>
+struct Slopes {
+  float c, m, my, slope, level, gs;
+  bool none, bad;
+  __device__ __forceinline__ Slopes(const Policy &P, int64_t r, const State &st) {
+    c = kLog2e / P.temperature;
+    const float w = P.g_loss ? P.g_loss[r] : 1.0f, g = w / P.temperature, inv = 1.0f / st.s;
+    m = st.m, my = Sums<REF>::base_of(st.my);
+    none = st.s == 0.0f || w == 0.0f;
+    gs = none ? 0.0f : g * st.slope;
+    slope = REF ? g * P.kl_weight * (float)kLn2 : 0.0f;
+    level = none ? 0.0f : -(REF ? fmaf(slope, st.mean, gs) : gs) * inv;
+    slope = none ? 0.0f : slope * inv;
+    bad = isnan(level);
+  }
+  __device__ __forceinline__ float operator()(float x, float y) const {
+    // (contracted, d - dy would not be 0 for equal scores)
+#pragma clang fp contract(off)
+    const float d = (x - m) * c, e = __builtin_amdgcn_exp2f(d);
+    float v = level;
+    if constexpr (REF) {
+      const float dy = (y - my) * c;
+      v = fmaf(slope, d - dy, level);
+    }
+    v = e * v;
+    return none || e == 0.0f ? 0.0f : v;
+  }
+};
+
 // Scores as a row's vectors hold them, those of excluded items -inf in both.
 template <class T, bool EX, bool REF>
 struct Pair {
   static constexpr int N = Vec<T>::N;
   Row<T, EX> row;
   const T *y;
+  // Vectors as they are in memory, in 32-bit words (held as 16-bit values, each
+  // would take a register of its own).
   struct Raw {
-    typename Row<T, EX>::Raw x;
-    Vec<T> y;
+    uint32_t x[4], y[REF ? 4 : 1], ex[EX ? N / 4 : 1];
   };
   __device__ __forceinline__ Raw fetch(int32_t v) const {
     Raw r;
-    r.x = row.fetch(v);
-    if constexpr (REF) r.y = load_vec(y + (int64_t)v * N);
+    __builtin_memcpy(r.x, row.x + (int64_t)v * N, 16);
+    if constexpr (REF) __builtin_memcpy(r.y, y + (int64_t)v * N, 16);
+    if constexpr (EX) __builtin_memcpy(r.ex, row.ex + (int64_t)v * N, N);
     return r;
+  }
+  static __device__ __forceinline__ float element(const uint32_t *w, int i) {
+    if constexpr (sizeof(T) == 4) {
+      return __uint_as_float(w[i]);
+    } else if constexpr (std::is_same<T, bf16_t>::value) {
+      return __uint_as_float(i % 2 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    } else {
+      return to_float(__builtin_bit_cast(T, (uint16_t)(w[i / 2] >> (i % 2 * 16))));
+    }
+  }
+  __device__ __forceinline__ float other(int32_t i) const {  // as row.one(i)
+    if constexpr (!REF) return -INFINITY;
+    if constexpr (EX)
+      if (row.ex[i]) return -INFINITY;
+    return to_float(y[i]);
   }
   static __device__ __forceinline__ Raw nothing() {
-    Raw r;
-    r.x = Row<T, EX>::nothing();
-    if constexpr (REF)
+    Raw r = {};
+    const uint32_t low = sizeof(T) == 4 ? 0xFF800000u
+                         : std::is_same<T, bf16_t>::value ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
 #pragma unroll
-      for (int i = 0; i < N; ++i) r.y.v[i] = from_float<T>(-INFINITY);
+    for (int i = 0; i < 4; ++i) {
+      r.x[i] = low;
+      if constexpr (REF) r.y[i] = low;
+    }
     return r;
   }
+  // Between two passes over the same vectors: what the first made of them is not
+  // kept (the scores take two or three times the registers of the vectors).
+  static __device__ __forceinline__ void renew(Raw &r) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      asm volatile("" : "+v"(r.x[i]));
+      if constexpr (REF) asm volatile("" : "+v"(r.y[i]));
+      if constexpr (EX)
+        if (i < N / 4) asm volatile("" : "+v"(r.ex[i]));
+    }
+  }
   static __device__ __forceinline__ void scores(const Raw &r, float (&x)[N], float (&z)[N]) {
-    Row<T, EX>::scores(r.x, x);
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      z[i] = -INFINITY;
-      if constexpr (REF) {
-        z[i] = to_float(r.y.v[i]);
-        if constexpr (EX) z[i] = r.x.b[i / 4] >> (i % 4 * 8) & 0xFF ? -INFINITY : z[i];
+      x[i] = element(r.x, i);
+      z[i] = REF ? element(r.y, i) : -INFINITY;
+      if constexpr (EX) {
+        const bool out = excluded(r, i);
+        x[i] = out ? -INFINITY : x[i];
+        if constexpr (REF) z[i] = out ? -INFINITY : z[i];
       }
     }
+  }
+  // The gradient of a vector, and of one element.
+  static __device__ __forceinline__ bool excluded(const Raw &r, int i) {
+    return EX && r.ex[i / 4] & (0xFFu << (i % 4 * 8));
+  }
+  static __device__ __forceinline__ Vec<T> gradient(const Raw &r, const Slopes<REF> &grad) {
+    Vec<T> v;
+    if (grad.bad) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(excluded(r, i) ? 0.0f : NAN);
+      return v;
+    }
+    float x[N], z[N];
+    scores(r, x, z);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(grad(x[i], z[i]));
+    return v;
+  }
+  __device__ __forceinline__ T gradient(int32_t i, const Slopes<REF> &grad) const {
+    if (grad.bad) return from_float<T>(EX && row.ex[i] ? 0.0f : NAN);
+    return from_float<T>(grad(row.one(i), other(i)));
   }
 };
 
@@ -257,9 +374,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
     if (tid < len - vecs * N) {
       const int32_t i = vecs * N + tid;
       const float x[1] = {two.row.one(i)};
-      float y[1] = {-INFINITY};
-      if constexpr (REF)
-        if (!EX || !two.row.ex[i]) y[0] = to_float(two.y[i]);
+      const float y[1] = {two.other(i)};
       a.add(x, y, x[0], y[0], c);
     }
     const Sums<REF> all = block_sums<TH>(a, c, lds);
@@ -300,79 +415,164 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
 // once.  A workgroup takes a tile of one row at a time.
 // ---------------------------------------------------------------------------
 
-// A row's gradient from its scores.
-template <class T, bool REF>
-struct Slopes {
-  float c, m, my, inv, gs, gk, mean;
-  bool none;
-  int64_t given;
-  __device__ __forceinline__ Slopes(const Policy &P, int64_t r, const State &st) {
-    c = kLog2e / P.temperature;
-    const float g = (P.g_loss ? P.g_loss[r] : 1.0f) / P.temperature;
-    given = P.given[r];
-    m = st.m, my = Sums<REF>::base_of(st.my), mean = st.mean;
-    none = st.s == 0.0f;
-    inv = 1.0f / st.s;
-    gs = g * st.slope;
-    gk = REF && P.kl_weight != 0.0f ? g * P.kl_weight * (float)kLn2 : 0.0f;
-  }
-  __device__ __forceinline__ T operator()(float x, float y, int64_t j, bool excluded) const {
-#pragma clang fp contract(off)
-    const float d = (x - m) * c, p = __builtin_amdgcn_exp2f(d) * inv;
-    float v = -gs * p;
-    if constexpr (REF) {
-      const float dy = (y - my) * c, t = p * (gk * ((d - dy) - mean));
-      v += p == 0.0f || gk == 0.0f ? 0.0f : t;
-    }
-    if (j == given) v += gs;
-    return from_float<T>(excluded || none ? 0.0f : v);
-  }
-};
+// The given item's gradient.
+template <class T, bool EX, bool REF>
+__device__ __forceinline__ T given_gradient(const Policy &P, int64_t r, int64_t g,
+                                            const Slopes<REF> &grad) {
+  if (EX && P.ex[r * P.ex_stride + g]) return from_float<T>(0.0f);
+  if (grad.bad) return from_float<T>(NAN);
+  const float x = to_float(static_cast<const T *>(P.x)[r * P.stride + g]);
+  float y = 0.0f;
+  if constexpr (REF) y = to_float(static_cast<const T *>(P.y)[r * P.y_stride + g]);
+  return from_float<T>(grad(x, y) + grad.gs);
+}
 
 constexpr int kGradGroup = 2;
 template <class T, bool EX, bool REF, int TH>
 __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
+  using Two = Pair<T, EX, REF>;
   constexpr int N = Vec<T>::N;
   constexpr int64_t kTile = (int64_t)TH * kGradGroup * N;
   const int tid = threadIdx.x;
   for (int64_t u = blockIdx.x; u < P.rows * P.tiles; u += gridDim.x) {
     const int64_t r = u / P.tiles, first = u % P.tiles * kTile, left = P.cols - first;
     const int32_t len = (int32_t)(left < kTile ? left : kTile);
-    const T *x = static_cast<const T *>(P.x) + (r * P.stride + first);
-    const T *y = REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr;
-    const uint8_t *ex = EX ? P.ex + (r * P.ex_stride + first) : nullptr;
+    const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
+                   EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
+                  REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
     T *out = static_cast<T *>(P.out) + (r * P.out_stride + first);
+    typename Two::Raw raw[kGradGroup];
+#pragma unroll
+    for (int q = 0; q < kGradGroup; ++q)
+      if ((tid + q * TH) * N + N <= len) raw[q] = two.fetch(tid + q * TH);
     const State st{P.state[r], P.state[P.rows + r], P.state[2 * P.rows + r],
                    P.state[3 * P.rows + r], P.state[4 * P.rows + r]};
-    const Slopes<T, REF> grad(P, r, st);
-    Vec<T> a[kGradGroup], b[kGradGroup];
-    uint8_t e[kGradGroup][N];
+    const Slopes<REF> grad(P, r, st);
+    // the thread whose vector has the given item writes it once more
+    const int64_t g = P.given[r] - first;
+    const bool own = g >= 0 && g < len && g / N % TH == tid;
+    T given;
+    if (own) given = given_gradient<T, EX, REF>(P, r, first + g, grad);
 #pragma unroll
     for (int q = 0; q < kGradGroup; ++q) {
       const int32_t i = (tid + q * TH) * N;
       if (i + N <= len) {
-        a[q] = load_vec(x + i);
-        if constexpr (REF) b[q] = load_vec(y + i);
-        if constexpr (EX) __builtin_memcpy(e[q], ex + i, N);
-      }
-    }
-#pragma unroll
-    for (int q = 0; q < kGradGroup; ++q) {
-      const int32_t i = (tid + q * TH) * N;
-      if (i + N <= len) {
-        Vec<T> v;
-#pragma unroll
-        for (int k = 0; k < N; ++k)
-          v.v[k] = grad(to_float(a[q].v[k]), REF ? to_float(b[q].v[k]) : 0.0f, first + i + k,
-                        EX && e[q][k]);
-        store_vec(out + i, v);
+        store_vec(out + i, two.gradient(raw[q], grad));
       } else {
         for (int k = 0; k < N; ++k)
-          if (i + k < len)
-            out[i + k] = grad(to_float(x[i + k]), REF ? to_float(y[i + k]) : 0.0f, first + i + k,
-                              EX && ex[i + k]);
+          if (i + k < len) out[i + k] = two.gradient(i + k, grad);
       }
     }
+    if (own) out[g] = given;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Both at once, for rows that fit the registers of a workgroup (H vectors a
+// thread): the scores and the reference are read and the gradient is written
+// once.
+// ---------------------------------------------------------------------------
+template <int TH>
+struct StepLds {
+  float m[TH / 64], my[TH / 64];
+  double s[TH / 64], w[TH / 64], sy[TH / 64];
+  State st;
+};
+template <class T, bool EX, bool REF, int TH, int H>
+__global__ void __launch_bounds__(TH, 4) k_policy_step(Policy P) {
+  __shared__ StepLds<TH> lds;
+  using Two = Pair<T, EX, REF>;
+  constexpr int N = Two::N, W = TH / 64;
+  const int tid = threadIdx.x, wave = tid / 64;
+  const float c = kLog2e / P.temperature;
+  const int32_t len = (int32_t)P.cols, vecs = len / N;
+  for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x) {
+    const int64_t g = P.given[r];
+    T *out = static_cast<T *>(P.out) + r * P.out_stride;
+    const Two two{{static_cast<const T *>(P.x) + r * P.stride,
+                   EX ? P.ex + r * P.ex_stride : nullptr, len},
+                  REF ? static_cast<const T *>(P.y) + r * P.y_stride : nullptr};
+    const bool tail = tid < len - vecs * N;
+    Sums<REF> a;
+    typename Two::Raw raw[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) raw[h] = Two::nothing();
+    float x1 = -INFINITY, y1 = -INFINITY;
+    if (g != -1) {  // of all threads
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
+      if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
+      // the largest
+      a.m = x1, a.my = y1;
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (h * TH + tid < vecs) {
+          float x[N], y[N];
+          Two::scores(raw[h], x, y);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            a.m = fmaxf(a.m, x[i]);
+            if constexpr (REF) a.my = fmaxf(a.my, y[i]);
+          }
+        }
+      a.m = wave_max(a.m);
+      if constexpr (REF) a.my = wave_max(a.my);
+      if constexpr (W > 1) {
+        if (tid % 64 == 0) lds.m[wave] = a.m, lds.my[wave] = a.my;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          a.m = fmaxf(a.m, lds.m[i]);
+          if constexpr (REF) a.my = fmaxf(a.my, lds.my[i]);
+        }
+      }
+      // the sums
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (h * TH + tid < vecs) {
+          float x[N], y[N];
+          Two::renew(raw[h]);
+          Two::scores(raw[h], x, y);
+          a.add(x, y, a.m, a.my, c);
+        }
+      if (tail) {
+        const float x[1] = {x1}, y[1] = {y1};
+        a.add(x, y, a.m, a.my, c);
+      }
+      a.s = wave_sum(a.s);
+      if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
+      if constexpr (W > 1) {
+        if (tid % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
+        __syncthreads();
+      }
+    }
+    if (tid == 0) {
+      if (W > 1 && g != -1) {
+        a.s = a.w = a.sy = 0.0;
+        for (int i = 0; i < W; ++i) {
+          a.s += lds.s[i];
+          if constexpr (REF) a.w += lds.w[i], a.sy += lds.sy[i];
+        }
+      }
+      lds.st = finish<T>(P, r, a);
+    }
+    __syncthreads();
+    const Slopes<REF> grad(P, r, lds.st);
+    const bool own = g >= 0 && g < len && (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
+    T given;
+    if (own) given = given_gradient<T, EX, REF>(P, r, g, grad);
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int32_t v = h * TH + tid;
+      if (v < vecs) {
+        Two::renew(raw[h]);
+        store_vec(out + (int64_t)v * N, two.gradient(raw[h], grad));
+      }
+    }
+    if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
+    if (own) out[g] = given;
+    __syncthreads();  // before the next row uses LDS
   }
 }
 
@@ -407,7 +607,7 @@ void with_flags(bool a, bool b, const F &f) {
 
 template <class T>
 void policy_grad(Policy p, hipStream_t stream) {
-  with_flags(p.ex, p.y, [&](auto ex, auto ref) {
+  with_flags(p.ex, p.y && p.kl_weight != 0.0f, [&](auto ex, auto ref) {
     constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
     const auto go = [&](auto threads) {
       constexpr int TH = decltype(threads)::value;
@@ -422,8 +622,34 @@ void policy_grad(Policy p, hipStream_t stream) {
   });
 }
 
+// Whether the call that gives both goes through the scores once.
+template <class T>
+bool in_registers(const Policy &p) {
+  return p.out && p.cols && p.cols <= 5 * 1024 * Vec<T>::N && !(p.y && p.kl_weight == 0.0f);
+}
+
+template <class T>
+hipError_t policy_step(const Policy &p, hipStream_t stream) {
+  const int64_t vecs = p.cols / Vec<T>::N;
+  with_flags(p.ex, p.y, [&](auto ex, auto ref) {
+    constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
+    const auto go = [&](auto threads, auto held) {
+      constexpr int TH = decltype(threads)::value, H = decltype(held)::value;
+      hipLaunchKernelGGL((k_policy_step<T, EX, REF, TH, H>),
+                         dim3((unsigned)std::min(p.rows, kMostGroups)), dim3(TH), 0, stream, p);
+    };
+    using std::integral_constant;
+    if (vecs <= 4 * 64) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
+    else if (vecs <= 4 * 256) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
+    else if (vecs <= 5 * 512) go(integral_constant<int, 512>{}, integral_constant<int, 5>{});
+    else go(integral_constant<int, 1024>{}, integral_constant<int, 5>{});
+  });
+  return hipGetLastError();
+}
+
 template <class T>
 hipError_t policy(const Policy &p, hipStream_t stream) {
+  if (in_registers<T>(p)) return policy_step<T>(p, stream);
   with_flags(p.ex, p.y, [&](auto ex, auto ref) {
     constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
     const dim3 groups((unsigned)std::min(p.rows * p.parts, kMostGroups));
