@@ -20,6 +20,7 @@ struct Policy {
   int64_t rows, cols, stride, y_stride, ex_stride;
   float temperature, clip_low, clip_high, kl_weight;
   float *loss, *log_prob, *kl;
+  int64_t first;  // a launch's first row (or part): workgroups have one each
   float *state;  // [5][rows]: row_max, row_sum, the reference's row_max, slope, mean
   // rows split in `parts` of part_len scores: where the parts' sums go
   int64_t parts, part_len;
@@ -29,6 +30,11 @@ struct Policy {
   void *out;
   int64_t out_stride, tiles;  // tiles of a row
 };
+
+// a b, but 0 where either is 0, whatever the other is (v_mul_legacy_f32; the
+// compiler has no builtin for it).
+extern "C" __device__ float bgmf_mul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
+__device__ __forceinline__ float times_or_0(float a, float b) { return bgmf_mul_legacy(a, b); }
 
 // Running sums of a row's scores x and of the reference's y, m and my the
 // largest of each so far, d = (x - m) c and dy = (y - my) c:
@@ -71,9 +77,9 @@ struct Sums {
       const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
       gs += e;
       if constexpr (REF) {
-        const float dy = (y[i] - by) * c, t = e * (d - dy);
+        const float dy = (y[i] - by) * c;
         gy += __builtin_amdgcn_exp2f(dy);
-        gw += e > 0.0f ? t : 0.0f;  // (e may be 0 where d - dy is not finite)
+        gw += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
       }
     }
     s += gs;
@@ -213,22 +219,23 @@ struct PartSum {
 
 // A row's gradient but for its given item's own term: with d, dy and e = exp2(d),
 //   p (gk (d - dy - mean) - gs) = e (slope (d - dy) + level)
-// and 0 for items of probability 0, excluded ones among them.  A row whose level
-// is NaN (bad) has NaN for every item that is not excluded.
+// and 0 for items of probability 0, excluded ones among them.  In an odd row every
+// item that is not excluded has the same: 0 where the row takes no part, NaN where
+// its level is.
 template <bool REF>
 struct Slopes {
   float c, m, my, slope, level, gs;
-  bool none, bad;
+  bool odd;
   __device__ __forceinline__ Slopes(const Policy &P, int64_t r, const State &st) {
     c = kLog2e / P.temperature;
     const float w = P.g_loss ? P.g_loss[r] : 1.0f, g = w / P.temperature, inv = 1.0f / st.s;
     m = st.m, my = Sums<REF>::base_of(st.my);
-    none = st.s == 0.0f || w == 0.0f;
+    const bool none = st.s == 0.0f || w == 0.0f;
     gs = none ? 0.0f : g * st.slope;
     slope = REF ? g * P.kl_weight * (float)kLn2 : 0.0f;
     level = none ? 0.0f : -(REF ? fmaf(slope, st.mean, gs) : gs) * inv;
-    slope = none ? 0.0f : slope * inv;
-    bad = isnan(level);
+    slope *= inv;
+    odd = none || isnan(level);
   }
   __device__ __forceinline__ float operator()(float x, float y) const {
     // (contracted, d - dy would not be 0 for equal scores)
@@ -239,8 +246,7 @@ struct Slopes {
       const float dy = (y - my) * c;
       v = fmaf(slope, d - dy, level);
     }
-    v = e * v;
-    return none || e == 0.0f ? 0.0f : v;
+    return times_or_0(e, v);
   }
 };
 
@@ -255,12 +261,33 @@ struct Pair {
   struct Raw {
     uint32_t x[4], y[REF ? 4 : 1], ex[EX ? N / 4 : 1];
   };
+  static constexpr uint32_t kLow = sizeof(T) == 4 ? 0xFF800000u
+                                   : std::is_same<T, bf16_t>::value ? 0xFF80FF80u
+                                                                    : 0xFC00FC00u;  // -inf
   __device__ __forceinline__ Raw fetch(int32_t v) const {
     Raw r;
     __builtin_memcpy(r.x, row.x + (int64_t)v * N, 16);
     if constexpr (REF) __builtin_memcpy(r.y, y + (int64_t)v * N, 16);
     if constexpr (EX) __builtin_memcpy(r.ex, row.ex + (int64_t)v * N, N);
     return r;
+  }
+  // Once fetched: -inf in place of excluded scores, by words.
+  static __device__ __forceinline__ void exclude(Raw &r) {
+    if constexpr (EX) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t b = r.ex[k * (N / 4) / 4];
+        const uint32_t some = ((b & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | b;  // bit 7 of each byte
+        uint32_t mask;
+        if constexpr (N == 4)
+          mask = (uint32_t)((int32_t)(some << (24 - 8 * k)) >> 31);
+        else  // (8 to 11 repeat bits 15, 31, 47 and 63 of both words)
+          mask = __builtin_amdgcn_perm(some << 8, some, k % 2 ? 0x09090B0Bu : 0x08080A0Au);
+        r.x[k] = (mask & kLow) | (~mask & r.x[k]);
+        if constexpr (REF) r.y[k] = (mask & kLow) | (~mask & r.y[k]);
+      }
+      renew(r);  // (the compiler would mask each element by itself)
+    }
   }
   static __device__ __forceinline__ float element(const uint32_t *w, int i) {
     if constexpr (sizeof(T) == 4) {
@@ -279,12 +306,10 @@ struct Pair {
   }
   static __device__ __forceinline__ Raw nothing() {
     Raw r = {};
-    const uint32_t low = sizeof(T) == 4 ? 0xFF800000u
-                         : std::is_same<T, bf16_t>::value ? 0xFF80FF80u : 0xFC00FC00u;  // -inf
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      r.x[i] = low;
-      if constexpr (REF) r.y[i] = low;
+      r.x[i] = kLow;
+      if constexpr (REF) r.y[i] = kLow;
     }
     return r;
   }
@@ -295,8 +320,6 @@ struct Pair {
     for (int i = 0; i < 4; ++i) {
       asm volatile("" : "+v"(r.x[i]));
       if constexpr (REF) asm volatile("" : "+v"(r.y[i]));
-      if constexpr (EX)
-        if (i < N / 4) asm volatile("" : "+v"(r.ex[i]));
     }
   }
   static __device__ __forceinline__ void scores(const Raw &r, float (&x)[N], float (&z)[N]) {
@@ -304,32 +327,24 @@ struct Pair {
     for (int i = 0; i < N; ++i) {
       x[i] = element(r.x, i);
       z[i] = REF ? element(r.y, i) : -INFINITY;
-      if constexpr (EX) {
-        const bool out = excluded(r, i);
-        x[i] = out ? -INFINITY : x[i];
-        if constexpr (REF) z[i] = out ? -INFINITY : z[i];
-      }
     }
   }
-  // The gradient of a vector, and of one element.
-  static __device__ __forceinline__ bool excluded(const Raw &r, int i) {
-    return EX && r.ex[i / 4] & (0xFFu << (i % 4 * 8));
-  }
-  static __device__ __forceinline__ Vec<T> gradient(const Raw &r, const Slopes<REF> &grad) {
-    Vec<T> v;
-    if (grad.bad) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(excluded(r, i) ? 0.0f : NAN);
-      return v;
+  // The gradient of vector v, and of one element.
+  __device__ __forceinline__ Vec<T> gradient(int32_t v, const Raw &r,
+                                             const Slopes<REF> &grad) const {
+    Vec<T> to;
+    if (grad.odd) {
+      for (int i = 0; i < N; ++i) to.v[i] = gradient(v * N + i, grad);
+      return to;
     }
     float x[N], z[N];
     scores(r, x, z);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v.v[i] = from_float<T>(grad(x[i], z[i]));
-    return v;
+    for (int i = 0; i < N; ++i) to.v[i] = from_float<T>(grad(x[i], z[i]));
+    return to;
   }
   __device__ __forceinline__ T gradient(int32_t i, const Slopes<REF> &grad) const {
-    if (grad.bad) return from_float<T>(EX && row.ex[i] ? 0.0f : NAN);
+    if (grad.odd) return from_float<T>(EX && row.ex[i] ? 0.0f : grad.level);
     return from_float<T>(grad(row.one(i), other(i)));
   }
 };
@@ -344,45 +359,43 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
   constexpr int N = Two::N;
   const int tid = threadIdx.x;
   const float c = kLog2e / P.temperature;
-  const int64_t units = P.rows * P.parts;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int64_t r = P.parts == 1 ? u : u / P.parts, part = P.parts == 1 ? 0 : u % P.parts;
-    const int64_t first = part * P.part_len;
-    const int64_t left = P.cols - first;
-    const int32_t len = P.given[r] == -1 ? 0 : (int32_t)(left < P.part_len ? left : P.part_len);
-    const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
-                   EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
-                  REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
-    Sums<REF> a;
-    const int32_t vecs = two.row.vecs();
-    for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
-      typename Two::Raw raw[kGroup];
+  const int64_t u = P.first + blockIdx.x;
+  const int64_t r = P.parts == 1 ? u : u / P.parts, part = P.parts == 1 ? 0 : u % P.parts;
+  const int64_t first = part * P.part_len;
+  const int64_t left = P.cols - first;
+  const int32_t len = P.given[r] == -1 ? 0 : (int32_t)(left < P.part_len ? left : P.part_len);
+  const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
+                 EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
+                REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
+  Sums<REF> a;
+  const int32_t vecs = two.row.vecs();
+  for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
+    typename Two::Raw raw[kGroup];
 #pragma unroll
-      for (int g = 0; g < kGroup; ++g) {
-        raw[g] = Two::nothing();
-        if (v0 + g * TH + tid < vecs) raw[g] = two.fetch(v0 + g * TH + tid);
-      }
+    for (int g = 0; g < kGroup; ++g) {
+      raw[g] = Two::nothing();
+      if (v0 + g * TH + tid < vecs) raw[g] = two.fetch(v0 + g * TH + tid);
+    }
 #pragma unroll
-      for (int g = 0; g < kGroup; ++g) {
-        float x[N], y[N], gm = -INFINITY, gmy = -INFINITY;
-        Two::scores(raw[g], x, y);
+    for (int g = 0; g < kGroup; ++g) {
+      float x[N], y[N], gm = -INFINITY, gmy = -INFINITY;
+      Two::exclude(raw[g]);
+      Two::scores(raw[g], x, y);
 #pragma unroll
-        for (int i = 0; i < N; ++i) gm = fmaxf(gm, x[i]), gmy = fmaxf(gmy, y[i]);
-        a.add(x, y, gm, gmy, c);
-      }
+      for (int i = 0; i < N; ++i) gm = fmaxf(gm, x[i]), gmy = fmaxf(gmy, y[i]);
+      a.add(x, y, gm, gmy, c);
     }
-    if (tid < len - vecs * N) {
-      const int32_t i = vecs * N + tid;
-      const float x[1] = {two.row.one(i)};
-      const float y[1] = {two.other(i)};
-      a.add(x, y, x[0], y[0], c);
-    }
-    const Sums<REF> all = block_sums<TH>(a, c, lds);
-    if (tid == 0) {
-      if (P.parts == 1) finish<T>(P, r, all);
-      else P.part_sum[u] = PartSum{all.s, all.w, all.sy, all.m, all.my};
-    }
-    __syncthreads();  // before the next row uses LDS
+  }
+  if (tid < len - vecs * N) {
+    const int32_t i = vecs * N + tid;
+    const float x[1] = {two.row.one(i)};
+    const float y[1] = {two.other(i)};
+    a.add(x, y, x[0], y[0], c);
+  }
+  const Sums<REF> all = block_sums<TH>(a, c, lds);
+  if (tid == 0) {
+    if (P.parts == 1) finish<T>(P, r, all);
+    else P.part_sum[u] = PartSum{all.s, all.w, all.sy, all.m, all.my};
   }
 }
 
@@ -420,7 +433,7 @@ template <class T, bool EX, bool REF>
 __device__ __forceinline__ T given_gradient(const Policy &P, int64_t r, int64_t g,
                                             const Slopes<REF> &grad) {
   if (EX && P.ex[r * P.ex_stride + g]) return from_float<T>(0.0f);
-  if (grad.bad) return from_float<T>(NAN);
+  if (grad.odd) return from_float<T>(grad.level);
   const float x = to_float(static_cast<const T *>(P.x)[r * P.stride + g]);
   float y = 0.0f;
   if constexpr (REF) y = to_float(static_cast<const T *>(P.y)[r * P.y_stride + g]);
@@ -457,7 +470,8 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
     for (int q = 0; q < kGradGroup; ++q) {
       const int32_t i = (tid + q * TH) * N;
       if (i + N <= len) {
-        store_vec(out + i, two.gradient(raw[q], grad));
+        Two::exclude(raw[q]);
+        store_vec(out + i, two.gradient(tid + q * TH, raw[q], grad));
       } else {
         for (int k = 0; k < N; ++k)
           if (i + k < len) out[i + k] = two.gradient(i + k, grad);
@@ -479,101 +493,98 @@ struct StepLds {
   State st;
 };
 template <class T, bool EX, bool REF, int TH, int H>
-__global__ void __launch_bounds__(TH, 4) k_policy_step(Policy P) {
+__global__ void __launch_bounds__(TH, TH > 512 ? 4 : 6) k_policy_step(Policy P) {
   __shared__ StepLds<TH> lds;
   using Two = Pair<T, EX, REF>;
   constexpr int N = Two::N, W = TH / 64;
   const int tid = threadIdx.x, wave = tid / 64;
   const float c = kLog2e / P.temperature;
   const int32_t len = (int32_t)P.cols, vecs = len / N;
-  for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x) {
-    const int64_t g = P.given[r];
-    T *out = static_cast<T *>(P.out) + r * P.out_stride;
-    const Two two{{static_cast<const T *>(P.x) + r * P.stride,
-                   EX ? P.ex + r * P.ex_stride : nullptr, len},
-                  REF ? static_cast<const T *>(P.y) + r * P.y_stride : nullptr};
-    const bool tail = tid < len - vecs * N;
-    Sums<REF> a;
-    typename Two::Raw raw[H];
+  const int64_t r = P.first + blockIdx.x;
+  const int64_t g = P.given[r];
+  T *out = static_cast<T *>(P.out) + r * P.out_stride;
+  const Two two{{static_cast<const T *>(P.x) + r * P.stride,
+                 EX ? P.ex + r * P.ex_stride : nullptr, len},
+                REF ? static_cast<const T *>(P.y) + r * P.y_stride : nullptr};
+  const bool tail = tid < len - vecs * N;
+  Sums<REF> a;
+  typename Two::Raw raw[H];
+  float x1 = -INFINITY, y1 = -INFINITY;
+  if (g != -1) {  // of all threads
 #pragma unroll
-    for (int h = 0; h < H; ++h) raw[h] = Two::nothing();
-    float x1 = -INFINITY, y1 = -INFINITY;
-    if (g != -1) {  // of all threads
+    for (int h = 0; h < H; ++h)
+      if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
+    if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
+    // the largest
+    a.m = x1, a.my = y1;
 #pragma unroll
-      for (int h = 0; h < H; ++h)
-        if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
-      if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
-      // the largest
-      a.m = x1, a.my = y1;
+    for (int h = 0; h < H; ++h)
+      if (h * TH + tid < vecs) {
+        float x[N], y[N];
+        Two::exclude(raw[h]);
+        Two::scores(raw[h], x, y);
 #pragma unroll
-      for (int h = 0; h < H; ++h)
-        if (h * TH + tid < vecs) {
-          float x[N], y[N];
-          Two::scores(raw[h], x, y);
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            a.m = fmaxf(a.m, x[i]);
-            if constexpr (REF) a.my = fmaxf(a.my, y[i]);
-          }
-        }
-      a.m = wave_max(a.m);
-      if constexpr (REF) a.my = wave_max(a.my);
-      if constexpr (W > 1) {
-        if (tid % 64 == 0) lds.m[wave] = a.m, lds.my[wave] = a.my;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-          a.m = fmaxf(a.m, lds.m[i]);
-          if constexpr (REF) a.my = fmaxf(a.my, lds.my[i]);
+        for (int i = 0; i < N; ++i) {
+          a.m = fmaxf(a.m, x[i]);
+          if constexpr (REF) a.my = fmaxf(a.my, y[i]);
         }
       }
-      // the sums
+    a.m = wave_max(a.m);
+    if constexpr (REF) a.my = wave_max(a.my);
+    if constexpr (W > 1) {
+      if (tid % 64 == 0) lds.m[wave] = a.m, lds.my[wave] = a.my;
+      __syncthreads();
 #pragma unroll
-      for (int h = 0; h < H; ++h)
-        if (h * TH + tid < vecs) {
-          float x[N], y[N];
-          Two::renew(raw[h]);
-          Two::scores(raw[h], x, y);
-          a.add(x, y, a.m, a.my, c);
-        }
-      if (tail) {
-        const float x[1] = {x1}, y[1] = {y1};
+      for (int i = 0; i < W; ++i) {
+        a.m = fmaxf(a.m, lds.m[i]);
+        if constexpr (REF) a.my = fmaxf(a.my, lds.my[i]);
+      }
+    }
+    // the sums
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      if (h * TH + tid < vecs) {
+        float x[N], y[N];
+        Two::renew(raw[h]);
+        Two::scores(raw[h], x, y);
         a.add(x, y, a.m, a.my, c);
       }
-      a.s = wave_sum(a.s);
-      if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
-      if constexpr (W > 1) {
-        if (tid % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
-        __syncthreads();
-      }
+    if (tail) {
+      const float x[1] = {x1}, y[1] = {y1};
+      a.add(x, y, a.m, a.my, c);
     }
-    if (tid == 0) {
-      if (W > 1 && g != -1) {
-        a.s = a.w = a.sy = 0.0;
-        for (int i = 0; i < W; ++i) {
-          a.s += lds.s[i];
-          if constexpr (REF) a.w += lds.w[i], a.sy += lds.sy[i];
-        }
-      }
-      lds.st = finish<T>(P, r, a);
+    a.s = wave_sum(a.s);
+    if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
+    if constexpr (W > 1) {
+      if (tid % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
+      __syncthreads();
     }
-    __syncthreads();
-    const Slopes<REF> grad(P, r, lds.st);
-    const bool own = g >= 0 && g < len && (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
-    T given;
-    if (own) given = given_gradient<T, EX, REF>(P, r, g, grad);
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      const int32_t v = h * TH + tid;
-      if (v < vecs) {
-        Two::renew(raw[h]);
-        store_vec(out + (int64_t)v * N, two.gradient(raw[h], grad));
-      }
-    }
-    if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
-    if (own) out[g] = given;
-    __syncthreads();  // before the next row uses LDS
   }
+  if (tid == 0) {
+    if (W > 1 && g != -1) {
+      a.s = a.w = a.sy = 0.0;
+      for (int i = 0; i < W; ++i) {
+        a.s += lds.s[i];
+        if constexpr (REF) a.w += lds.w[i], a.sy += lds.sy[i];
+      }
+    }
+    lds.st = finish<T>(P, r, a);
+  }
+  __syncthreads();
+  const Slopes<REF> grad(P, r, lds.st);
+  const bool own = g >= 0 && g < len && (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
+  T given;
+  if (own) given = given_gradient<T, EX, REF>(P, r, g, grad);
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    const int32_t v = h * TH + tid;
+    if (v < vecs) {
+      Two::renew(raw[h]);
+      store_vec(out + (int64_t)v * N, two.gradient(v, raw[h], grad));
+    }
+  }
+  if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
+  if (own) out[g] = given;
 }
 
 constexpr int64_t kMostGroups = 1 << 20;
@@ -629,14 +640,16 @@ bool in_registers(const Policy &p) {
 }
 
 template <class T>
-hipError_t policy_step(const Policy &p, hipStream_t stream) {
+hipError_t policy_step(Policy p, hipStream_t stream) {
   const int64_t vecs = p.cols / Vec<T>::N;
   with_flags(p.ex, p.y, [&](auto ex, auto ref) {
     constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
     const auto go = [&](auto threads, auto held) {
       constexpr int TH = decltype(threads)::value, H = decltype(held)::value;
-      hipLaunchKernelGGL((k_policy_step<T, EX, REF, TH, H>),
-                         dim3((unsigned)std::min(p.rows, kMostGroups)), dim3(TH), 0, stream, p);
+      for (p.first = 0; p.first < p.rows; p.first += kMostGroups)
+        hipLaunchKernelGGL((k_policy_step<T, EX, REF, TH, H>),
+                           dim3((unsigned)std::min(p.rows - p.first, kMostGroups)), dim3(TH), 0,
+                           stream, p);
     };
     using std::integral_constant;
     if (vecs <= 4 * 64) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
@@ -648,15 +661,18 @@ hipError_t policy_step(const Policy &p, hipStream_t stream) {
 }
 
 template <class T>
-hipError_t policy(const Policy &p, hipStream_t stream) {
+hipError_t policy(Policy p, hipStream_t stream) {
   if (in_registers<T>(p)) return policy_step<T>(p, stream);
   with_flags(p.ex, p.y, [&](auto ex, auto ref) {
     constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
-    const dim3 groups((unsigned)std::min(p.rows * p.parts, kMostGroups));
-    if (p.cols <= kShortRow)
-      hipLaunchKernelGGL((k_policy<T, EX, REF, 64>), groups, dim3(64), 0, stream, p);
-    else
-      hipLaunchKernelGGL((k_policy<T, EX, REF, kThreads>), groups, dim3(kThreads), 0, stream, p);
+    const int64_t units = p.rows * p.parts;
+    for (p.first = 0; p.first < units; p.first += kMostGroups) {
+      const dim3 groups((unsigned)std::min(units - p.first, kMostGroups));
+      if (p.cols <= kShortRow)
+        hipLaunchKernelGGL((k_policy<T, EX, REF, 64>), groups, dim3(64), 0, stream, p);
+      else
+        hipLaunchKernelGGL((k_policy<T, EX, REF, kThreads>), groups, dim3(kThreads), 0, stream, p);
+    }
     if (p.parts > 1)
       hipLaunchKernelGGL((k_policy_join<T, REF>), dim3((unsigned)std::min(p.rows, kMostGroups)),
                          dim3(kThreads), 0, stream, p);
