@@ -64,26 +64,37 @@ struct Sums {
       if (my != -INFINITY) sy *= __builtin_amdgcn_exp2f((my - My) * c);
     m = M, my = My;
   }
+  // A group's sums, with m and my not below its scores.
+  struct Group {
+    float s = 0.0f, w = 0.0f, sy = 0.0f;
+    template <int COUNT>
+    __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float bx,
+                                        float by, float c) {
+      // d and dy are rounded alike, so that equal scores leave exactly 0
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) {
+        const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        if constexpr (REF) {
+          const float dy = (y[i] - by) * c;
+          sy += __builtin_amdgcn_exp2f(dy);
+          w += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
+        }
+      }
+    }
+  };
+  __device__ __forceinline__ void add(const Group &g) {
+    s += g.s;
+    if constexpr (REF) w += g.w, sy += g.sy;
+  }
   template <int COUNT>
   __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float gm,
                                       float gmy, float c) {  // the largest of x and of y
-    // d and dy are rounded alike, so that equal scores leave exactly 0
-#pragma clang fp contract(off)
     if (gm > m || (REF && gmy > my)) rescale(fmaxf(m, gm), REF ? fmaxf(my, gmy) : my, c);
-    const float bx = base_of(m), by = base_of(my);
-    float gs = 0.0f, gw = 0.0f, gy = 0.0f;
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-      const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
-      gs += e;
-      if constexpr (REF) {
-        const float dy = (y[i] - by) * c;
-        gy += __builtin_amdgcn_exp2f(dy);
-        gw += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
-      }
-    }
-    s += gs;
-    if constexpr (REF) w += gw, sy += gy;
+    Group g;
+    g.add(x, y, base_of(m), base_of(my), c);
+    add(g);
   }
 };
 
@@ -304,15 +315,6 @@ struct Pair {
       if (row.ex[i]) return -INFINITY;
     return to_float(y[i]);
   }
-  static __device__ __forceinline__ Raw nothing() {
-    Raw r = {};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      r.x[i] = kLow;
-      if constexpr (REF) r.y[i] = kLow;
-    }
-    return r;
-  }
   // Between two passes over the same vectors: what the first made of them is not
   // kept (the scores take two or three times the registers of the vectors).
   static __device__ __forceinline__ void renew(Raw &r) {
@@ -369,15 +371,22 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
                 REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
   Sums<REF> a;
   const int32_t vecs = two.row.vecs();
+  // the vectors of the next group are on their way while this one's are summed
+  typename Two::Raw next[kGroup];
+  const auto fetch = [&](int32_t v0) {
+#pragma unroll
+    for (int g = 0; g < kGroup; ++g)
+      if (v0 + g * TH + tid < vecs) next[g] = two.fetch(v0 + g * TH + tid);
+  };
+  fetch(0);
   for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
     typename Two::Raw raw[kGroup];
 #pragma unroll
-    for (int g = 0; g < kGroup; ++g) {
-      raw[g] = Two::nothing();
-      if (v0 + g * TH + tid < vecs) raw[g] = two.fetch(v0 + g * TH + tid);
-    }
+    for (int g = 0; g < kGroup; ++g) raw[g] = next[g];
+    fetch(v0 + TH * kGroup);
 #pragma unroll
     for (int g = 0; g < kGroup; ++g) {
+      if (v0 + g * TH + tid >= vecs) break;
       float x[N], y[N], gm = -INFINITY, gmy = -INFINITY;
       Two::exclude(raw[g]);
       Two::scores(raw[g], x, y);
@@ -493,7 +502,7 @@ struct StepLds {
   State st;
 };
 template <class T, bool EX, bool REF, int TH, int H>
-__global__ void __launch_bounds__(TH, TH > 512 ? 4 : 6) k_policy_step(Policy P) {
+__global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(Policy P) {
   __shared__ StepLds<TH> lds;
   using Two = Pair<T, EX, REF>;
   constexpr int N = Two::N, W = TH / 64;
@@ -540,18 +549,26 @@ __global__ void __launch_bounds__(TH, TH > 512 ? 4 : 6) k_policy_step(Policy P) 
         if constexpr (REF) a.my = fmaxf(a.my, lds.my[i]);
       }
     }
-    // the sums
+    // the sums, of 16 scores in 32 bits
+    const float bx = Sums<REF>::base_of(a.m), by = Sums<REF>::base_of(a.my);
+    typename Sums<REF>::Group group;
 #pragma unroll
-    for (int h = 0; h < H; ++h)
+    for (int h = 0; h < H; ++h) {
       if (h * TH + tid < vecs) {
         float x[N], y[N];
         Two::renew(raw[h]);
         Two::scores(raw[h], x, y);
-        a.add(x, y, a.m, a.my, c);
+        group.add(x, y, bx, by, c);
       }
+      if ((h + 1) * N % 16 == 0 || h == H - 1) {
+        a.add(group);
+        group = {};
+      }
+    }
     if (tail) {
       const float x[1] = {x1}, y[1] = {y1};
-      a.add(x, y, a.m, a.my, c);
+      group.add(x, y, bx, by, c);
+      a.add(group);
     }
     a.s = wave_sum(a.s);
     if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
@@ -591,7 +608,7 @@ constexpr int64_t kMostGroups = 1 << 20;
 
 // How a row is split: in as few parts as hold at most kPart scores each, but no
 // more than fill the GPU or than kMostParts.
-constexpr int64_t kFullGpu = 2048, kPart = 16384;
+constexpr int64_t kFullGpu = 2048, kPart = 8192;
 struct Split {
   int64_t parts, len;
 };
@@ -634,9 +651,11 @@ void policy_grad(Policy p, hipStream_t stream) {
 }
 
 // Whether the call that gives both goes through the scores once.
+constexpr int kMostHeld = 9;
 template <class T>
 bool in_registers(const Policy &p) {
-  return p.out && p.cols && p.cols <= 5 * 1024 * Vec<T>::N && !(p.y && p.kl_weight == 0.0f);
+  return p.out && p.cols && p.cols <= kMostHeld * 1024 * Vec<T>::N &&
+         !(p.y && p.kl_weight == 0.0f);
 }
 
 template <class T>
@@ -652,10 +671,16 @@ hipError_t policy_step(Policy p, hipStream_t stream) {
                            stream, p);
     };
     using std::integral_constant;
+    using Few = integral_constant<int, 5>;
+    using Most = integral_constant<int, kMostHeld>;
+    const bool many = p.rows > 512;
     if (vecs <= 4 * 64) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
-    else if (vecs <= 4 * 256) go(integral_constant<int, 256>{}, integral_constant<int, 4>{});
-    else if (vecs <= 5 * 512) go(integral_constant<int, 512>{}, integral_constant<int, 5>{});
-    else go(integral_constant<int, 1024>{}, integral_constant<int, 5>{});
+    else if (vecs <= 5 * 256) go(integral_constant<int, 256>{}, Few{});
+    else if (many && vecs <= 9 * 256) go(integral_constant<int, 256>{}, Most{});
+    else if (vecs <= 5 * 512) go(integral_constant<int, 512>{}, Few{});
+    else if (many && vecs <= 9 * 512) go(integral_constant<int, 512>{}, Most{});
+    else if (vecs <= 5 * 1024) go(integral_constant<int, 1024>{}, Few{});
+    else go(integral_constant<int, 1024>{}, Most{});
   });
   return hipGetLastError();
 }
