@@ -187,6 +187,9 @@ hipError_t dequantize_mx(const Rows &p, void *out, int64_t out_stride, hipStream
 // The product.
 // ---------------------------------------------------------------------------
 struct Product {
+  const void *x;  // users' values, rows of k, where the product itself quantises them
+  int64_t x_stride;
+  int32_t k;
   const uint8_t *a, *a_scale;  // users: rows of `blocks` blocks
   int64_t rows, a_stride, as_stride;
   const uint8_t *b, *b_scale;  // items
@@ -218,72 +221,100 @@ __device__ __forceinline__ i32x4 block_bytes(const uint8_t *p) {
 }
 
 // Few users (32 for each blockIdx.y): every item's bytes go from global memory
-// into a matrix instruction once.  A wave takes ITEMS tiles of 32 items and
-// STEPS pairs of blocks at a time; while it stores their scores, the bytes and
-// scales of its next ones are on their way.  LONG: rows of more than STEPS pairs
-// (with one tile at a time).
-template <class O, int STEPS, int ITEMS, bool LONG, bool STREAM>
+// into a matrix instruction once.  A wave takes a tile of 32 items and STEPS pairs
+// of blocks at a time; while it stores their scores, the bytes and scales of its
+// next ones are on their way.  LONG: rows of more than STEPS pairs.
+//
+// X: uint8_t, users' bytes in P.a; or the type of their values in P.x (rows of at
+// most kOwnBlocks blocks), which every workgroup then quantises into LDS, a block
+// to a thread, while its first items are on their way: a launch less.
+constexpr int kOwnBlocks = 16;
+template <class O, class X, int STEPS, bool LONG, bool STREAM>
 __global__ void __launch_bounds__(kThreads, 4) k_mx_few(Product P) {
-  static_assert(!LONG || ITEMS == 1, "one tile at a time");
+  constexpr bool OWN = !std::is_same<X, uint8_t>::value;
+  __shared__ i32x4 own_bytes[OWN ? 32 * kOwnBlocks : 1];
+  __shared__ uint8_t own_scales[OWN ? 32 * kOwnBlocks : 1];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
   const int l32 = lane % 32, half = lane / 32;
-  const int64_t r0 = (int64_t)blockIdx.y * 32, tiles = (P.items + 32 * ITEMS - 1) / (32 * ITEMS);
-  const int64_t r = r0 + l32 < P.rows ? r0 + l32 : P.rows - 1;
-  const uint8_t *a = P.a + r * P.a_stride, *as = P.a_scale + r * P.as_stride;
+  const int64_t r0 = (int64_t)blockIdx.y * 32, tiles = (P.items + 31) / 32;
+  const int rows = P.rows - r0 < 32 ? (int)(P.rows - r0) : 32;
+  const int row = l32 < rows ? l32 : rows - 1;
+  const uint8_t *a = P.a + (r0 + row) * P.a_stride, *as = P.a_scale + (r0 + row) * P.as_stride;
   int64_t tile = (int64_t)blockIdx.x * kWaves + wave;
   const int64_t stride = (int64_t)gridDim.x * kWaves;
-  if (tile >= tiles) return;
-  i32x4 x[ITEMS][STEPS], y[STEPS];
-  int xs[ITEMS][STEPS], ys[STEPS];
+  i32x4 x[STEPS], y[STEPS];
+  int xs[STEPS], ys[STEPS];
   const auto users = [&](int32_t s0) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       const int32_t at = (s0 + s) * 2 + half;
       y[s] = i32x4{}, ys[s] = 0;
-      if (at < P.blocks) y[s] = block_bytes(a + (int64_t)at * 16), ys[s] = as[at];
+      if (at < P.blocks) {
+        if constexpr (OWN) {
+          y[s] = own_bytes[row * P.blocks + at], ys[s] = own_scales[row * P.blocks + at];
+        } else {
+          y[s] = block_bytes(a + (int64_t)at * 16), ys[s] = as[at];
+        }
+      }
     }
   };
-  const auto items = [&](int64_t t, int i, int32_t s0) {
-    int64_t j = t * (32 * ITEMS) + i * 32 + l32;
+  const auto items = [&](int64_t t, int32_t s0) {
+    int64_t j = t * 32 + l32;
     if (j >= P.items) j = P.items - 1;
     const uint8_t *b = P.b + j * P.b_stride, *bs = P.b_scale + j * P.bs_stride;
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
       const int32_t at = (s0 + s) * 2 + half;
-      x[i][s] = i32x4{}, xs[i][s] = 0;
-      if (at < P.blocks) x[i][s] = block_bytes<STREAM>(b + (int64_t)at * 16), xs[i][s] = bs[at];
+      x[s] = i32x4{}, xs[s] = 0;
+      if (at < P.blocks) x[s] = block_bytes<STREAM>(b + (int64_t)at * 16), xs[s] = bs[at];
     }
   };
+  if (tile < tiles) items(tile, 0);
+  if constexpr (OWN) {
+    for (int i = threadIdx.x; i < rows * P.blocks; i += kThreads) {
+      const X *v = static_cast<const X *>(P.x) + (r0 + i / P.blocks) * P.x_stride;
+      float eight[4][8];
+      uint32_t most = 0, bits[4];
 #pragma unroll
-  for (int i = 0; i < ITEMS; ++i) items(tile, i, 0);
+      for (int q = 0; q < 4; ++q) {
+        load_eight(v, i % P.blocks * kBlock + q * 8, P.k, eight[q]);
+        most = max(most, largest_bits(eight[q]));
+      }
+      const int code = scale_byte(most);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) bits[q] = eight_to_bits(eight[q], code);
+      own_bytes[i] = i32x4{(int)bits[0], (int)bits[1], (int)bits[2], (int)bits[3]};
+      own_scales[i] = (uint8_t)code;
+    }
+    __syncthreads();
+  }
   if constexpr (!LONG) users(0);
   for (; tile < tiles; tile += stride) {
+    f32x16 acc = {};
+    for (int32_t s0 = 0;;) {
+      if constexpr (LONG) users(s0);
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-      f32x16 acc = {};
-      for (int32_t s0 = 0;;) {
-        if constexpr (LONG) users(s0);
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) acc = multiply<0>(y[s], ys[s], x[i][s], xs[i][s], acc);
-        if constexpr (LONG) {
-          s0 += STEPS;
-          if (s0 * 2 < P.blocks) {
-            items(tile, i, s0);
-            continue;
-          }
+      for (int s = 0; s < STEPS; ++s) acc = multiply<0>(y[s], ys[s], x[s], xs[s], acc);
+      if constexpr (LONG) {
+        s0 += STEPS;
+        if (s0 * 2 < P.blocks) {
+          items(tile, s0);
+          continue;
         }
-        break;
       }
-      if (tile + stride < tiles) items(tile + stride, i, 0);
-      const int64_t j = tile * (32 * ITEMS) + i * 32 + l32;
-      if (j >= P.items) continue;
-      O *to = static_cast<O *>(P.out) + j;
+      break;
+    }
+    if (tile + stride < tiles) items(tile + stride, 0);
+    const int64_t j = tile * 32 + l32;
+    if (j >= P.items) continue;
+    O *to = static_cast<O *>(P.out) + ((r0 + 4 * half) * P.out_stride + j);
 #pragma unroll
-      for (int g = 0; g < 16; ++g) {
-        const int64_t u = r0 + 8 * (g / 4) + 4 * half + g % 4;
-        if (r0 + 8 * (g / 4) + g % 4 >= P.rows) continue;  // of the whole wave
-        if (u < P.rows) to[u * P.out_stride] = from_float<O>(acc[g]);
-      }
+    for (int g = 0; g < 16; ++g) {
+      const int u = 8 * (g / 4) + g % 4;
+      if (u >= rows) break;  // of the whole wave
+      if (u + 4 * half < rows) *to = from_float<O>(acc[g]);
+      to += g % 4 == 3 ? 5 * P.out_stride : P.out_stride;
+      asm volatile("" : "+v"(to));  // (16 addresses would be kept)
     }
   }
 }
@@ -620,9 +651,9 @@ __global__ void __launch_bounds__(kThreads, 1) k_mx_large(Product P) {
 constexpr int64_t kFullGpu = 2048;
 constexpr int64_t kCached = 192 << 20;  // items that stay in the 256 MB Infinity Cache
 
-template <class O, int STEPS, int ITEMS, bool LONG>
+template <class O, class X, int STEPS, bool LONG>
 void launch_few(Product p, hipStream_t stream) {
-  const int64_t all = (p.items + 32 * ITEMS * kWaves - 1) / (32 * ITEMS * kWaves);
+  const int64_t all = (p.items + 32 * kWaves - 1) / (32 * kWaves);
   // equally many tiles for each
   const int64_t rounds = (all + kFullGpu - 1) / kFullGpu, groups = (all + rounds - 1) / rounds;
   const bool stream_items = p.rows <= 32 && p.items * (int64_t)p.blocks * 16 > kCached;
@@ -631,14 +662,23 @@ void launch_few(Product p, hipStream_t stream) {
     p.rows = std::min(left, kMost);
     const dim3 grid((unsigned)groups, (unsigned)((p.rows + 31) / 32));
     if (stream_items)
-      hipLaunchKernelGGL((k_mx_few<O, STEPS, ITEMS, LONG, true>), grid, dim3(kThreads), 0, stream,
-                         p);
+      hipLaunchKernelGGL((k_mx_few<O, X, STEPS, LONG, true>), grid, dim3(kThreads), 0,
+                         stream, p);
     else
-      hipLaunchKernelGGL((k_mx_few<O, STEPS, ITEMS, LONG, false>), grid, dim3(kThreads), 0, stream,
-                         p);
+      hipLaunchKernelGGL((k_mx_few<O, X, STEPS, LONG, false>), grid, dim3(kThreads), 0,
+                         stream, p);
+    if (p.x) p.x = static_cast<const X *>(p.x) + kMost * p.x_stride;
     p.a += kMost * p.a_stride, p.a_scale += kMost * p.as_stride;
     p.out = static_cast<O *>(p.out) + kMost * p.out_stride;
   }
+}
+
+template <class O, class X>
+void product_few(const Product &p, hipStream_t stream) {
+  if (p.blocks <= 2) launch_few<O, X, 1, false>(p, stream);
+  else if (p.blocks <= 4) launch_few<O, X, 2, false>(p, stream);
+  else if (p.blocks <= 8) launch_few<O, X, 4, false>(p, stream);
+  else launch_few<O, X, 4, true>(p, stream);
 }
 
 template <class O, int BI, int BU, int STEP>
@@ -650,31 +690,39 @@ void launch_many(const Product &p, hipStream_t stream) {
                      dim3(kThreads), 0, stream, p, all);
 }
 
-constexpr int64_t kLargeBlocks = 32;
+// Whether the product itself quantises the users' values (few users, or so few
+// scores that the other kernels' launch for it costs more): fp32, k = 64, own and
+// in the faster of the other kernels, 18,000 items 48 users 4.4 and 5.7 us, 64 5.0
+// and 5.7, 128 6.3 and 6.1, 100,003 items 48 users 8.8 and 8.7, 64 10.3 and 9.3; k =
+// 200, 18,000 items 48 users 5.8 and 6.7, 128 8.7 and 8.2, 100,003 items 48 users
+// 14.3 and 10.7.  Up to 32 users own and with a launch: k = 64 18,000 items 4.1 and
+// 5.5 us, 1M 30.3 and 31.6; k = 512 18,000 items 8.4 and 8.3, 100,003 19.9 and 18.1,
+// 1M 135 and 140.
+inline bool takes_values(int64_t rows, int64_t items, int64_t blocks) {
+  return rows <= 32 ? blocks <= kOwnBlocks : blocks <= 8 && rows * items <= (1 << 22) / blocks;
+}
 inline bool uses_few(int64_t rows, int64_t items, int64_t items_stride) {
   return rows <= 32 || items < 128 || items_stride > kMostStride;
 }
+// Tiles of 256 x 256 for rows of at least this many blocks and at least 128 tiles.
+// Against 128 x 128, to bf16: 4,096 x 8,192 (512 tiles), k = 512 24 and 19 us, 1,024
+// 29 and 30, 2,048 42 and 56, 4,096 71 and 129; 2,048 x 18,000 (568), k = 1,024 39
+// and 34, 2,048 58 and 63; 512 x 18,000 (142), k = 1,024 14.7 and 13.8, 2,048 20.8 and
+// 22.2; 2,048 x 4,096 (128), k = 2,048 19.9 and 18.1, 4,096 35.2 and 36.6 (all with
+// bytes of one value, which the GPU multiplies at a higher clock).
+constexpr int64_t kLargeBlocks = 64;
 
 template <class O>
-hipError_t product(const Product &p, hipStream_t stream) {
+hipError_t product(const Product &p, int32_t type, hipStream_t stream) {
   const auto tiles = [&](int64_t items, int64_t users) {
     return (p.items + items - 1) / items * ((p.rows + users - 1) / users);
   };
-  if (uses_few(p.rows, p.items, p.b_stride)) {
-    const bool small = p.items < 32 * kFullGpu * kWaves;
-    if (p.blocks <= 2) {
-      if (small) launch_few<O, 1, 1, false>(p, stream);
-      else launch_few<O, 1, 8, false>(p, stream);
-    } else if (p.blocks <= 4) {
-      if (small) launch_few<O, 2, 1, false>(p, stream);
-      else launch_few<O, 2, 4, false>(p, stream);
-    } else if (p.blocks <= 8) {
-      if (small) launch_few<O, 4, 1, false>(p, stream);
-      else launch_few<O, 4, 2, false>(p, stream);
-    } else {
-      launch_few<O, 4, 1, true>(p, stream);
-    }
-  } else if (p.blocks >= kLargeBlocks && p.items >= 256 && tiles(256, 256) >= 256) {
+  if (p.x || uses_few(p.rows, p.items, p.b_stride)) {
+    if (!p.x) product_few<O, uint8_t>(p, stream);
+    else if (type == BGMF_TYPE_F32) product_few<O, float>(p, stream);
+    else if (type == BGMF_TYPE_BF16) product_few<O, bf16_t>(p, stream);
+    else product_few<O, f16_t>(p, stream);
+  } else if (p.blocks >= kLargeBlocks && p.items >= 256 && tiles(256, 256) >= 128) {
     hipLaunchKernelGGL(k_mx_large<O>, dim3((unsigned)tiles(256, 256)), dim3(kThreads), 0, stream,
                        p);
   } else if (p.rows > 64 && tiles(128, 128) >= 256) {
@@ -856,11 +904,13 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
       shares(item_scale, BGMF_TYPE_I8, item_count, blocks, item_scale_stride))
     return fail_call(BGMF_E_ARG, "%s: out shares memory with an input", call);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  Product p{static_cast<const uint8_t *>(x), row_scale, rows, row_stride, row_scale_stride,
+  Product p{nullptr, row_stride, (int32_t)k, static_cast<const uint8_t *>(x), row_scale, rows, row_stride, row_scale_stride,
             items, item_scale, item_count, items_stride, item_scale_stride, (int32_t)blocks,
             out, out_stride};
   hipError_t e = hipSuccess;
-  if (own || !uses_few(rows, item_count, items_stride)) {
+  if (own && takes_values(rows, item_count, blocks)) {
+    p.x = x, p.a = nullptr;
+  } else if (own || !uses_few(rows, item_count, items_stride)) {
     uint8_t *q = static_cast<uint8_t *>(ws), *scale = q + bytes_part(rows, k);
     const int64_t laid = padded_blocks(rows, k);
     if (own) {
@@ -875,9 +925,9 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
     p.a = q, p.a_scale = scale, p.a_stride = laid * 16, p.as_stride = laid;
   }
   if (e == hipSuccess)
-    e = out_type == BGMF_TYPE_F32    ? product<float>(p, stream)
-        : out_type == BGMF_TYPE_BF16 ? product<bf16_t>(p, stream)
-                                     : product<f16_t>(p, stream);
+    e = out_type == BGMF_TYPE_F32    ? product<float>(p, type, stream)
+        : out_type == BGMF_TYPE_BF16 ? product<bf16_t>(p, type, stream)
+                                     : product<f16_t>(p, type, stream);
   if (e != hipSuccess) return fail_call(BGMF_E_HIP, "%s: %s", call, hipGetErrorString(e));
   return BGMF_OK;
 }

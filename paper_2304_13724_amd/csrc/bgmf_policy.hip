@@ -174,31 +174,50 @@ struct State {
   float m, s, my, slope, mean;  // s = 0: the row's gradient is 0
 };
 
+// What a row's results need of its given item, fetched before its sums are there.
+// Every thread of the row has the same.
+template <class T, bool REF>
+struct Given {
+  int64_t item;
+  bool inside, excluded;
+  float x = 0.0f, y = 0.0f, advantage, old_log_prob, ref_log_prob = 0.0f;
+  __device__ __forceinline__ Given(const Policy &P, int64_t r) {
+    item = P.given[r];
+    inside = item >= 0 && item < P.cols;
+    excluded = inside && P.ex && P.ex[r * P.ex_stride + item];
+    if (inside) {
+      x = to_float(static_cast<const T *>(P.x)[r * P.stride + item]);
+      if constexpr (REF) y = to_float(static_cast<const T *>(P.y)[r * P.y_stride + item]);
+    }
+    advantage = P.advantage[r], old_log_prob = P.old_log_prob[r];
+    if (P.ref_log_prob) ref_log_prob = P.ref_log_prob[r];
+  }
+};
+
 // The row's results, by one thread, in 64 bits.
 template <class T, bool REF>
-__device__ __forceinline__ State finish(const Policy &P, int64_t r, const Sums<REF> &a) {
+__device__ __forceinline__ State finish(const Policy &P, int64_t r, const Given<T, REF> &g,
+                                        const Sums<REF> &a) {
   State st{a.m, (float)a.s, a.my, 0.0f, 0.0f};
   double loss = 0.0, lp = 0.0, kl = 0.0;
-  const int64_t g = P.given[r];
-  if (g == -1) {
+  if (g.item == -1) {
     st.s = 0.0f;
   } else {
-    const bool outside = g < 0 || g >= P.cols, none = a.s == 0.0;
+    const bool none = a.s == 0.0;
     const double ln_s = none ? 0.0 : ln(a.s);
     lp = -INFINITY;
-    if (outside) lp = NAN;
-    else if (!none && !(P.ex && P.ex[r * P.ex_stride + g]))
-      lp = ((double)to_float(static_cast<const T *>(P.x)[r * P.stride + g]) - (double)a.m) /
-               (double)P.temperature - ln_s;
-    if (!none || outside) {
-      const double A = P.advantage[r], rho = Exp(lp - (double)P.old_log_prob[r]).value;
+    if (!g.inside) lp = NAN;
+    else if (!none && !g.excluded)
+      lp = ((double)g.x - (double)a.m) / (double)P.temperature - ln_s;
+    if (!none || !g.inside) {
+      const double A = g.advantage, rho = Exp(lp - (double)g.old_log_prob).value;
       const double lo = 1.0 - (double)P.clip_low, hi = 1.0 + (double)P.clip_high;
       const double unclipped = rho * A, clipped = (rho < lo ? lo : rho > hi ? hi : rho) * A;
       const bool passes = !(unclipped > clipped);
       loss = -(passes ? unclipped : clipped);
       double slope = passes ? -unclipped : 0.0;
       if (P.ref_log_prob) {
-        const double z = (double)P.ref_log_prob[r] - lp, e = Exp(z).less1;
+        const double z = (double)g.ref_log_prob - lp, e = Exp(z).less1;
         kl = z == INFINITY ? INFINITY : e - z;
         if (P.kl_weight != 0.0f) slope -= (double)P.kl_weight * e;
       }
@@ -365,12 +384,13 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
   const int64_t r = P.parts == 1 ? u : u / P.parts, part = P.parts == 1 ? 0 : u % P.parts;
   const int64_t first = part * P.part_len;
   const int64_t left = P.cols - first;
-  const int32_t len = P.given[r] == -1 ? 0 : (int32_t)(left < P.part_len ? left : P.part_len);
+  const int32_t len = (int32_t)(left < P.part_len ? left : P.part_len);
   const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
                  EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
                 REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
   Sums<REF> a;
-  const int32_t vecs = two.row.vecs();
+  int32_t vecs = two.row.vecs();
+  bool tail = tid < len - vecs * N;
   // the vectors of the next group are on their way while this one's are summed
   typename Two::Raw next[kGroup];
   const auto fetch = [&](int32_t v0) {
@@ -379,6 +399,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
       if (v0 + g * TH + tid < vecs) next[g] = two.fetch(v0 + g * TH + tid);
   };
   fetch(0);
+  if (P.given[r] == -1) vecs = 0, tail = false;
   for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
     typename Two::Raw raw[kGroup];
 #pragma unroll
@@ -395,7 +416,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
       a.add(x, y, gm, gmy, c);
     }
   }
-  if (tid < len - vecs * N) {
+  if (tail) {
     const int32_t i = vecs * N + tid;
     const float x[1] = {two.row.one(i)};
     const float y[1] = {two.other(i)};
@@ -403,7 +424,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
   }
   const Sums<REF> all = block_sums<TH>(a, c, lds);
   if (tid == 0) {
-    if (P.parts == 1) finish<T>(P, r, all);
+    if (P.parts == 1) finish(P, r, Given<T, REF>(P, r), all);
     else P.part_sum[u] = PartSum{all.s, all.w, all.sy, all.m, all.my};
   }
 }
@@ -416,6 +437,7 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
   const float c = kLog2e / P.temperature;
   for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x) {
     const PartSum *sums = P.part_sum + r * P.parts;
+    const Given<T, REF> given(P, r);
     Sums<REF> a;
     for (int64_t i = threadIdx.x; i < P.parts; i += kThreads) {
       Sums<REF> b;
@@ -427,7 +449,7 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
       a.s += b.s, a.w += b.w, a.sy += b.sy;
     }
     const Sums<REF> all = block_sums<kThreads>(a, c, lds);
-    if (threadIdx.x == 0) finish<T>(P, r, all);
+    if (threadIdx.x == 0) finish(P, r, given, all);
     __syncthreads();
   }
 }
@@ -438,15 +460,11 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
 // ---------------------------------------------------------------------------
 
 // The given item's gradient.
-template <class T, bool EX, bool REF>
-__device__ __forceinline__ T given_gradient(const Policy &P, int64_t r, int64_t g,
+template <class T, bool REF>
+__device__ __forceinline__ T given_gradient(float x, float y, bool excluded,
                                             const Slopes<REF> &grad) {
-  if (EX && P.ex[r * P.ex_stride + g]) return from_float<T>(0.0f);
-  if (grad.odd) return from_float<T>(grad.level);
-  const float x = to_float(static_cast<const T *>(P.x)[r * P.stride + g]);
-  float y = 0.0f;
-  if constexpr (REF) y = to_float(static_cast<const T *>(P.y)[r * P.y_stride + g]);
-  return from_float<T>(grad(x, y) + grad.gs);
+  const float v = grad.odd ? grad.level : grad(x, y) + grad.gs;
+  return from_float<T>(excluded ? 0.0f : v);
 }
 
 constexpr int kGradGroup = 2;
@@ -474,7 +492,9 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
     const int64_t g = P.given[r] - first;
     const bool own = g >= 0 && g < len && g / N % TH == tid;
     T given;
-    if (own) given = given_gradient<T, EX, REF>(P, r, first + g, grad);
+    if (own)
+      given = given_gradient<T>(to_float(two.row.x[g]), REF ? to_float(two.y[g]) : 0.0f,
+                                EX && two.row.ex[g], grad);
 #pragma unroll
     for (int q = 0; q < kGradGroup; ++q) {
       const int32_t i = (tid + q * TH) * N;
@@ -510,7 +530,6 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(P
   const float c = kLog2e / P.temperature;
   const int32_t len = (int32_t)P.cols, vecs = len / N;
   const int64_t r = P.first + blockIdx.x;
-  const int64_t g = P.given[r];
   T *out = static_cast<T *>(P.out) + r * P.out_stride;
   const Two two{{static_cast<const T *>(P.x) + r * P.stride,
                  EX ? P.ex + r * P.ex_stride : nullptr, len},
@@ -519,11 +538,13 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(P
   Sums<REF> a;
   typename Two::Raw raw[H];
   float x1 = -INFINITY, y1 = -INFINITY;
-  if (g != -1) {  // of all threads
 #pragma unroll
-    for (int h = 0; h < H; ++h)
-      if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
-    if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
+  for (int h = 0; h < H; ++h)
+    if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
+  if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
+  const Given<T, REF> given(P, r);
+  const int64_t g = given.item;
+  if (g != -1) {  // of all threads
     // the largest
     a.m = x1, a.my = y1;
 #pragma unroll
@@ -585,13 +606,13 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(P
         if constexpr (REF) a.w += lds.w[i], a.sy += lds.sy[i];
       }
     }
-    lds.st = finish<T>(P, r, a);
+    lds.st = finish(P, r, given, a);
   }
   __syncthreads();
   const Slopes<REF> grad(P, r, lds.st);
-  const bool own = g >= 0 && g < len && (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
-  T given;
-  if (own) given = given_gradient<T, EX, REF>(P, r, g, grad);
+  // the thread whose vector has the given item writes it once more
+  const bool own = given.inside &&
+                   (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
 #pragma unroll
   for (int h = 0; h < H; ++h) {
     const int32_t v = h * TH + tid;
@@ -601,7 +622,7 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(P
     }
   }
   if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
-  if (own) out[g] = given;
+  if (own) out[g] = given_gradient<T>(given.x, given.y, given.excluded, grad);
 }
 
 constexpr int64_t kMostGroups = 1 << 20;
