@@ -191,6 +191,12 @@ struct Given {
     }
     advantage = P.advantage[r], old_log_prob = P.old_log_prob[r];
     if (P.ref_log_prob) ref_log_prob = P.ref_log_prob[r];
+    x = scalar(x), y = scalar(y), advantage = scalar(advantage);
+    old_log_prob = scalar(old_log_prob), ref_log_prob = scalar(ref_log_prob);
+    excluded = __builtin_amdgcn_readfirstlane(excluded);
+  }
+  static __device__ __forceinline__ float scalar(float v) {  // out of the vector registers
+    return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
   }
 };
 
@@ -254,7 +260,7 @@ struct PartSum {
 // its level is.
 template <bool REF>
 struct Slopes {
-  float c, m, my, slope, level, gs;
+  float c, m, my, slope, level, gs;  // slope 0: the reference plays no part
   bool odd;
   __device__ __forceinline__ Slopes(const Policy &P, int64_t r, const State &st) {
     c = kLog2e / P.temperature;
@@ -262,8 +268,9 @@ struct Slopes {
     m = st.m, my = Sums<REF>::base_of(st.my);
     const bool none = st.s == 0.0f || w == 0.0f;
     gs = none ? 0.0f : g * st.slope;
-    slope = REF ? g * P.kl_weight * (float)kLn2 : 0.0f;
-    level = none ? 0.0f : -(REF ? fmaf(slope, st.mean, gs) : gs) * inv;
+    const bool flat = !REF || P.kl_weight == 0.0f;
+    slope = flat ? 0.0f : g * P.kl_weight * (float)kLn2;
+    level = none ? 0.0f : -(flat ? gs : fmaf(slope, st.mean, gs)) * inv;
     slope *= inv;
     odd = none || isnan(level);
   }
@@ -274,7 +281,7 @@ struct Slopes {
     float v = level;
     if constexpr (REF) {
       const float dy = (y - my) * c;
-      v = fmaf(slope, d - dy, level);
+      v = times_or_0(slope, d - dy) + level;
     }
     return times_or_0(e, v);
   }
@@ -522,7 +529,7 @@ struct StepLds {
   State st;
 };
 template <class T, bool EX, bool REF, int TH, int H>
-__global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 6) k_policy_step(Policy P) {
+__global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(Policy P) {
   __shared__ StepLds<TH> lds;
   using Two = Pair<T, EX, REF>;
   constexpr int N = Two::N, W = TH / 64;
@@ -641,6 +648,10 @@ Split split_of(int64_t rows, int64_t cols) {
   return {(cols + len - 1) / len, len};
 }
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
+int64_t parts_bytes(int64_t rows, int64_t cols) {
+  const int64_t parts = split_of(rows, cols).parts;
+  return parts == 1 ? 0 : padded(rows * parts * (int64_t)sizeof(PartSum));
+}
 
 constexpr int64_t kShortRow = 2048;  // rows for workgroups of one wave
 
@@ -675,8 +686,7 @@ void policy_grad(Policy p, hipStream_t stream) {
 constexpr int kMostHeld = 9;
 template <class T>
 bool in_registers(const Policy &p) {
-  return p.out && p.cols && p.cols <= kMostHeld * 1024 * Vec<T>::N &&
-         !(p.y && p.kl_weight == 0.0f);
+  return p.out && p.cols && p.cols <= kMostHeld * 1024 * Vec<T>::N;
 }
 
 template <class T>
@@ -783,12 +793,12 @@ using namespace bgmfk;
 
 extern "C" {
 
-// Workspace: the parts' sums, then row_state where the caller wants none.
+// Workspace: the parts' sums, then row_state where the caller wants none and rows
+// of some type do not fit registers.
 int64_t bgmf_policy_loss_workspace(int64_t rows, int64_t cols) {
   if (rows <= 0 || cols <= 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
-  const int64_t parts = split_of(rows, cols).parts;
-  return (parts == 1 ? 0 : padded(rows * parts * (int64_t)sizeof(PartSum))) +
-         padded(5 * rows * (int64_t)sizeof(float));
+  return parts_bytes(rows, cols) +
+         (cols > kMostHeld * 1024 * 4 ? padded(5 * rows * (int64_t)sizeof(float)) : 0);
 }
 
 int bgmf_policy_loss(const void *scores, int32_t type, int64_t rows, int64_t cols,
@@ -826,10 +836,8 @@ int bgmf_policy_loss(const void *scores, int32_t type, int64_t rows, int64_t col
   const Split split = split_of(rows, cols);
   p.parts = split.parts, p.part_len = split.len;
   p.part_sum = static_cast<PartSum *>(ws);
-  if (grad_scores && cols && !row_state)
-    p.state = reinterpret_cast<float *>(
-        static_cast<char *>(ws) +
-        (split.parts == 1 ? 0 : padded(rows * split.parts * (int64_t)sizeof(PartSum))));
+  if (grad_scores && !row_state && cols > kMostHeld * 1024 * 4)
+    p.state = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(rows, cols));
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = type == BGMF_TYPE_F32    ? policy<float>(p, stream)
                        : type == BGMF_TYPE_BF16 ? policy<bf16_t>(p, stream)

@@ -281,11 +281,10 @@ class _PolicyLoss(torch.autograd.Function):
         return (grad,) + (None,) * 10
 
 
-def _only_scores(name, **tensors):
-    for what, t in tensors.items():
-        if _in_graph(t):
-            raise ValueError(f"{name} has a derivative with respect to the scores alone, and "
-                             f"{what} requires grad (call .detach())")
+def _only_scores(name, *tensors):
+    if _in_graph(*tensors):
+        raise ValueError(f"{name} has a derivative with respect to the scores alone, and another "
+                         "of its tensors requires grad (call .detach())")
 
 
 def policy_loss(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tensor,
@@ -304,8 +303,7 @@ def policy_loss(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tens
     probabilities of the shown items, for an estimate.  Differentiable with
     respect to the scores through ``loss``.  include/bgmf.h says what empty
     rows, infinities and NaN give."""
-    _only_scores("policy_loss", advantage=advantage, old_log_prob=old_log_prob,
-                 reference=reference, reference_log_prob=reference_log_prob)
+    _only_scores("policy_loss", advantage, old_log_prob, reference, reference_log_prob)
     if _in_graph(scores):
         return PolicyLoss(*_PolicyLoss.apply(
             scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight,
@@ -329,8 +327,8 @@ def policy_loss_and_grad(scores: torch.Tensor, given: torch.Tensor, advantage: t
     registers.  ``out`` may be the scores themselves.  For a loop that passes
     the gradient on itself (``logits.backward(grad)``): the results are in no
     graph."""
-    _only_scores("policy_loss_and_grad", advantage=advantage, old_log_prob=old_log_prob,
-                 reference=reference, reference_log_prob=reference_log_prob, weight=weight)
+    _only_scores("policy_loss_and_grad", advantage, old_log_prob, reference, reference_log_prob,
+                 weight)
     loss, log_prob, kl, _, grad = _checked(_ranking.policy_loss(
         scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight, clip_low,
         clip_high, temperature, excluded, 2, weight, out, _stream(scores)))
@@ -353,7 +351,9 @@ class _Dropout(torch.autograd.Function):
     @staticmethod
     def backward(ctx, g):
         offset = ctx.saved_tensors[0] if ctx.offset is None else ctx.offset
-        return dropout(g.resolve_neg().contiguous(), ctx.p, ctx.seed, offset), None, None, None
+        if g.is_neg() or not g.is_contiguous():
+            g = g.resolve_neg().contiguous()
+        return dropout(g, ctx.p, ctx.seed, offset), None, None, None
 
 
 def dropout(x: torch.Tensor, p: float, seed: int, offset=0, *,

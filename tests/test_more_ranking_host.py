@@ -81,10 +81,17 @@ def policy_args():
     dict(out=9 * A + 2), dict(out_stride=99), dict(out=A, out_stride=101),
     dict(out=2 * A, out_stride=101), dict(out=A + 4), dict(out=3 * A), dict(out=4 * A),
     dict(out=5 * A), dict(out=6 * A), dict(out=7 * A), dict(out=8 * A),
-    dict(out=11 * A, state=11 * A + 64), dict(out=11 * A, g_loss=11 * A), dict(ws=0),
-    dict(ws=A + 8)])
+    dict(out=11 * A, state=11 * A + 64), dict(out=11 * A, g_loss=11 * A)])
 def test_policy_loss(change):
     refused(bgmf.bgmf_policy_loss, policy_args(), POLICY, change)
+
+
+@pytest.mark.parametrize("change", [dict(ws=0), dict(ws=A + 8)])
+def test_policy_loss_of_rows_that_need_a_workspace(change):
+    args = {**dict(zip(POLICY, policy_args())), "cols": 100_000, "stride": 100_000,
+            "reference_stride": 100_000, "out": 1 << 40, "out_stride": 100_000, "scores": 1 << 41,
+            "reference": 1 << 42}
+    refused(bgmf.bgmf_policy_loss, args.values(), POLICY, change)
 
 
 @pytest.mark.parametrize("change", [
