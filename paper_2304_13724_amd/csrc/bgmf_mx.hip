@@ -366,22 +366,39 @@ struct Many {
     r0 = (group * kGroup + in % size) * kUsers;
   }
 
+  // PAD (rows of at least kChunks blocks): without branches; the users' rows have
+  // blocks of zeros up to a multiple of kChunks, and in place of an item's blocks
+  // past its row come its last one with scales of 0, so that their products are 0.
+  // Block q of a thread's blocks of a step (the items', then the users'), with PAD:
+  static __device__ __forceinline__ i32x4 load_one(const Product &P, int64_t j0, int64_t r0, int s,
+                                                   int q) {
+    const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+    if (q < kItemLoads) {
+      const int32_t c = min(s * kChunks + chunk, P.blocks - 1);
+      const uint32_t at = (uint32_t)row * (uint32_t)P.b_stride + (uint32_t)c * 16;
+      return block_bytes(P.b + (j0 + q * kPass) * P.b_stride + at);
+    }
+    const uint32_t at = (uint32_t)row * (uint32_t)P.a_stride + chunk * 16;
+    const uint8_t *a = P.a + (r0 + (q - kItemLoads) * kPass) * P.a_stride + (int64_t)s * STEP;
+    return block_bytes(a + at);
+  }
+  static __device__ __forceinline__ void store_one(i32x4 *buffer, int q, i32x4 x) {
+    const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
+    if (q < kItemLoads) buffer[at(row + kPass * q, chunk)] = x;
+    else buffer[kItems * kChunks + at(row + kPass * (q - kItemLoads), chunk)] = x;
+  }
+
   // A thread's blocks of step s of the items from j0 on (kItems of them are
   // there) and of the users from r0 on (whose rows are laid out up to a multiple
   // of kUserPad).  A thread's offset within its first row is 32 bits wide (see
-  // kMostStride).  PAD (rows of at least kChunks blocks): without branches; the
-  // users' rows have blocks of zeros up to a multiple of kChunks, and in place of
-  // an item's blocks past its row come its last one with scales of 0, so that
-  // their products are 0.
-  template <bool PAD = false>
+  // kMostStride).
   static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
                                               i32x4 (&x)[kItemLoads], i32x4 (&y)[kUserLoads]) {
     const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
-    const bool some = PAD || s * kChunks + chunk < P.blocks;
-    const int32_t c = min(s * kChunks + chunk, P.blocks - 1);
-    const uint32_t at_item = (uint32_t)row * (uint32_t)P.b_stride + (uint32_t)c * 16;
+    const bool some = s * kChunks + chunk < P.blocks;
+    const uint32_t at_item = (uint32_t)row * (uint32_t)P.b_stride + chunk * 16;
     const uint32_t at_user = (uint32_t)row * (uint32_t)P.a_stride + chunk * 16;
-    const uint8_t *b = P.b + j0 * P.b_stride;
+    const uint8_t *b = P.b + (j0 * P.b_stride + (int64_t)s * STEP);
     const uint8_t *a = P.a + (r0 * P.a_stride + (int64_t)s * STEP);
 #pragma unroll
     for (int h = 0; h < kItemLoads; ++h) {
@@ -582,58 +599,79 @@ constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
 template <class O>
 __global__ void __launch_bounds__(kThreads, 1) k_mx_large(Product P) {
   using M = Many<O, 4, 4, 128>;
+  constexpr int kLoads = M::kItemLoads + M::kUserLoads;
   __shared__ i32x4 lds[2 * M::kBuffer > M::kScores ? 2 * M::kBuffer : M::kScores];
   __shared__ uint32_t s_scale[2][M::kScaleWords];
   const int steps = (P.blocks + 7) / 8;
   int64_t j0, r0;
   M::place(P, blockIdx.x, j0, r0);
-  i32x4 x[M::kItemLoads], y[M::kUserLoads];
+  i32x4 x[kLoads];
   typename M::Scales scale;
-  const auto load = [&](int s) {  // past the last step: it once more, for nothing
-    M::template load<true>(P, j0, r0, min(s, steps - 1), x, y);
-    M::template load_scales<true>(P, j0, r0, min(s, steps - 1), scale);
-  };
-  load(0);
-  M::store(lds, x, y);
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) x[q] = M::load_one(P, j0, r0, 0, q);
+  M::template load_scales<true>(P, j0, r0, 0, scale);
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) M::store_one(lds, q, x[q]);
   M::store_scales(s_scale[0], scale);
-  load(1);
+  // past the last step: it once more, for nothing
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) x[q] = M::load_one(P, j0, r0, min(1, steps - 1), q);
+  M::template load_scales<true>(P, j0, r0, min(1, steps - 1), scale);
   __syncthreads();
   f32x16 acc[4][4] = {};
   i32x4 fi[2][4], fu[2][4];
   int si[4], su[4], si_next[4], su_next[4];
   M::read_scales(s_scale[0], si, su);
   M::read(lds, 0, fi[0], fu[0]);
-  // Between two barriers: 48 products with the reads of the next blocks, the
-  // writes of the next step and the loads of the one after it spread over them.
+  // A step has four pairs of blocks, 16 products each.  During the products of the
+  // first three the next pair is read, a third of the next step is written to the
+  // other buffer, and the same third of the step after it is fetched; the last
+  // one's cover the next step's first reads.
+  // keeps products among the reads and writes that they are to cover (they have no
+  // order of their own)
+  const auto hold = [&] {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) asm volatile("" : "+a"(acc[i][u]));
+  };
   for (int s = 0; s < steps; ++s) {
     i32x4 *now = lds + s % 2 * M::kBuffer, *other = lds + (s + 1) % 2 * M::kBuffer;
-    M::read(now, 1, fi[1], fu[1]);
-    M::template products<0>(acc, fi[0], fu[0], si, su);
-    M::read(now, 2, fi[0], fu[0]);
-    M::template products<1>(acc, fi[1], fu[1], si, su);
-    M::read(now, 3, fi[1], fu[1]);
-    M::template products<2>(acc, fi[0], fu[0], si, su);
-    M::store(other, x, y);
-    M::store_scales(s_scale[(s + 1) % 2], scale);
-    load(s + 2);
+    const int ahead = min(s + 2, steps - 1);
+    const auto third = [&](auto part) {
+      constexpr int R = decltype(part)::value, kFrom = (kLoads * R + 2) / 3,
+                    kTo = (kLoads * (R + 1) + 2) / 3;
+      __builtin_amdgcn_sched_barrier(0);
+      M::read(now, R + 1, fi[(R + 1) % 2], fu[(R + 1) % 2]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kMfma, 2, 0);
-    }
+      for (int q = kFrom; q < kTo; ++q) {
+        M::store_one(other, q, x[q]);
+        x[q] = M::load_one(P, j0, r0, ahead, q);
+      }
+      if constexpr (R == 2) {
+        M::store_scales(s_scale[(s + 1) % 2], scale);
+        M::template load_scales<true>(P, j0, r0, ahead, scale);
+      }
+      M::template products<R>(acc, fi[R % 2], fu[R % 2], si, su);
+      hold();
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      if (i % 2 == 0) __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
-      __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-    }
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+        if (i < kTo - kFrom) __builtin_amdgcn_sched_group_barrier(kDsWrite, 1, 0);
+        if (i < kTo - kFrom) __builtin_amdgcn_sched_group_barrier(kVmemRead, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      }
+    };
+    third(std::integral_constant<int, 0>{});
+    third(std::integral_constant<int, 1>{});
+    third(std::integral_constant<int, 2>{});
     __syncthreads();
-    __builtin_amdgcn_sched_barrier(0);  // the last products cover the next step's first reads
+    __builtin_amdgcn_sched_barrier(0);
     M::read_scales(s_scale[(s + 1) % 2], si_next, su_next);
     M::read(other, 0, fi[0], fu[0]);
     M::template products<3>(acc, fi[1], fu[1], si, su);
+    hold();
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       __builtin_amdgcn_sched_group_barrier(kDsRead, 2, 0);
