@@ -575,14 +575,15 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
  *   reference_log_prob (ln q_g): kl[r] = exp(z) - 1 - z, z = ln q_g - ln p_g,
  *     its estimate from the shown item
  *   neither: kl[r] = 0.
- * kl may come out below 0 by its rounding.  (One pass over the scores and the
- * reference; terms in fp32, running sums and a row's own numbers in fp64,
- * results in fp32.)
+ * kl may come out below 0 by its rounding (some 1e-8; equal scores give 0).  (One
+ * pass over the scores and the reference; terms in fp32, running sums and a
+ * row's own numbers in fp64, results in fp32.)
  *   given[r] = -1: the row fills the batch up.  Its scores are not looked at;
  *     loss, log_prob and kl are 0, and so is its gradient.
  *   A row with nothing left (all items excluded or -inf, or cols = 0): loss and
  *     kl 0, log_prob -inf, gradient 0.
- *   given[r] otherwise outside [0, cols): loss, log_prob and the gradient NaN.
+ *   given[r] otherwise outside [0, cols): loss and log_prob NaN (in a row with
+ *     nothing left too), and the gradient but in such rows.
  *   A NaN or +inf among the items that are not excluded makes the row's results
  *     NaN; in the reference, kl and (with kl_weight not 0) loss and gradient.
  *   An item with p_j = 0 adds nothing to kl; q_j = 0 < p_j makes it infinite,
@@ -596,8 +597,9 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
  *     + kl_weight p_j (ln(p_j / q_j) - kl) )     (second line with a reference)
  *   s = d loss / d log_prob = -rho A where rho A is the smaller one, else 0,
  *     + kl_weight (1 - exp(z)) with reference_log_prob
- * rounded once to the type of the scores, 0 for excluded items.  grad_scores may
- * be the scores or the reference (same pointer and stride).
+ * rounded once to the type of the scores; 0 for excluded items, where grad_loss[r]
+ * is 0, and in rows that take no part.  grad_scores may be the scores or the
+ * reference (same pointer and stride).
  * 0 <= clip_low <= 1, clip_high >= 0 (infinity: no upper bound), kl_weight
  * finite.  loss, log_prob and kl may be NULL.  rows, cols < 2^31. */
 int64_t bgmf_policy_loss_workspace(int64_t rows, int64_t cols);

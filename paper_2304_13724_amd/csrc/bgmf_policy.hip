@@ -378,7 +378,10 @@ struct Pair {
 };
 
 // One workgroup per row, or per part of a row; the scores and the reference are
-// read once.
+// read once.  Bound: HBM: 4,001 x 10,007 f32 with a reference take 59 us, 5.4 TB/s.  A
+// workgroup has one row and no loop over rows: the compiler would keep the 64-bit
+// functions' constants in registers through it (87 in place of 39, so that fewer
+// waves' loads are in flight).
 constexpr int kGroup = 2;
 template <class T, bool EX, bool REF, int TH>
 __global__ void __launch_bounds__(TH) k_policy(Policy P) {
@@ -436,7 +439,8 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
   }
 }
 
-// Joins the parts of a row: one workgroup per row.
+// Joins the parts of a row: one workgroup per row.  Bound: latency (33 rows of 62
+// parts: 4.4 us).
 constexpr int64_t kMostParts = 4 * kThreads;
 template <class T, bool REF>
 __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
@@ -463,7 +467,9 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
 
 // ---------------------------------------------------------------------------
 // Gradient: the scores and the reference are read and the gradient is written
-// once.  A workgroup takes a tile of one row at a time.
+// once.  A workgroup takes a tile of one row at a time.  Bound: HBM: 33 x 625,001 f32
+// with a reference take 37 us, 6.6 TB/s (the Infinity Cache has some of what the
+// forward pass read).
 // ---------------------------------------------------------------------------
 
 // The given item's gradient.
@@ -520,7 +526,11 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
 // ---------------------------------------------------------------------------
 // Both at once, for rows that fit the registers of a workgroup (H vectors a
 // thread): the scores and the reference are read and the gradient is written
-// once.
+// once.  Three passes over the registers: the maxima, the sums with them, the
+// gradient.  Bound: 2,047 x 18,000 bf16 with a reference and exclusions take 54 us:
+// HBM, 4.8 TB/s, and the vector units (75% of the CUs' cycles, 37 instructions a
+// score, three exponentials among them); 16 x 18,000 f32 6.2 us: latency (a row's
+// loads, three reductions, the 64-bit functions of one thread).
 // ---------------------------------------------------------------------------
 template <int TH>
 struct StepLds {
@@ -634,16 +644,20 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
 
 constexpr int64_t kMostGroups = 1 << 20;
 
-// How a row is split: in as few parts as hold at most kPart scores each, but no
-// more than fill the GPU or than kMostParts.
-constexpr int64_t kFullGpu = 2048, kPart = 8192;
+// How a row is split: rows of up to kWhole scores not at all, others in as few
+// parts as hold at most kPart each, but in no more than fill the GPU (eight
+// workgroups for each of 256 CUs) or than kMostParts.  The join costs some 2.5 us:
+// one row and its reference in one part and in two, bf16 8,000 scores 5.2 us and
+// 10,000 7.8, f32 6.1 and 8.1, and a part takes 1 to 1.4 us more for each 4,000.  33
+// rows of 625,001 f32 in 39 parts of 16,384 take 46 us, in 62 41.
+constexpr int64_t kFullGpu = 2048, kWhole = 16384, kPart = 8192;
 struct Split {
   int64_t parts, len;
 };
 Split split_of(int64_t rows, int64_t cols) {
   int64_t parts = std::min({(cols + kPart - 1) / kPart,
                             std::max<int64_t>(kFullGpu / std::max<int64_t>(rows, 1), 1), kMostParts});
-  if (parts <= 1) return {1, cols};
+  if (cols <= kWhole || parts <= 1) return {1, cols};
   const int64_t len = ((cols + parts - 1) / parts + 63) / 64 * 64;
   return {(cols + len - 1) / len, len};
 }
@@ -653,7 +667,9 @@ int64_t parts_bytes(int64_t rows, int64_t cols) {
   return parts == 1 ? 0 : padded(rows * parts * (int64_t)sizeof(PartSum));
 }
 
-constexpr int64_t kShortRow = 2048;  // rows for workgroups of one wave
+// Rows of at most this many scores go to workgroups of one wave (as in log_probs,
+// whose figures are at its constant).
+constexpr int64_t kShortRow = 2048;
 
 template <bool V>
 using Flag = std::integral_constant<bool, V>;
@@ -682,7 +698,10 @@ void policy_grad(Policy p, hipStream_t stream) {
   });
 }
 
-// Whether the call that gives both goes through the scores once.
+// Whether the call that gives both goes through the scores once.  With exclusions and
+// a reference, once and twice: f32 4,096 x 18,000 183 and 301 us, 4,096 x 36,000 418
+// and 577, 16 x 18,000 8.6 and 12.4, 1 x 36,000 14.3 and 12.0 (one workgroup has all of
+// it); bf16 4,096 x 18,000 101 and 172.
 constexpr int kMostHeld = 9;
 template <class T>
 bool in_registers(const Policy &p) {
@@ -704,7 +723,12 @@ hipError_t policy_step(Policy p, hipStream_t stream) {
     using std::integral_constant;
     using Few = integral_constant<int, 5>;
     using Most = integral_constant<int, kMostHeld>;
-    const bool many = p.rows > 512;
+    // the fewest threads that hold a row, but for few rows no more than five vectors
+    // each.  With exclusions and a reference: bf16 4,096 x 2,000 by 64 x 4 and 256 x 5
+    // 18.0 and 21.1 us, 16 x 2,000 5.7 and 4.7; 4,096 x 18,000 by 256 x 9 and 512 x 5 101
+    // and 107, 256 x 18,000 10.6 and 10.2; f32 4,096 x 18,000 by 512 x 9 and 1,024 x 5
+    // 183 and 208, 512 rows 21.7 and 28.0, 256 rows 14.7 and 14.3
+    const bool many = p.rows >= 512;
     if (vecs <= 4 * 64) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (vecs <= 5 * 256) go(integral_constant<int, 256>{}, Few{});
     else if (many && vecs <= 9 * 256) go(integral_constant<int, 256>{}, Most{});

@@ -507,10 +507,12 @@ PyObject *policy_loss_backward(PyObject *const *a) {
   return THPVariable_Wrap(out);
 }
 
-// A Python integer in [0, 2^64).
+// A Python (or numpy) integer in [0, 2^64).
 uint64_t word(PyObject *o, const char *name) {
-  const unsigned long long v = PyLong_Check(o) ? PyLong_AsUnsignedLongLong(o) : -1ull;
-  if (!PyLong_Check(o) || (v == -1ull && PyErr_Occurred())) {
+  PyObject *i = THPVariable_Check(o) ? nullptr : PyNumber_Index(o);
+  const unsigned long long v = i ? PyLong_AsUnsignedLongLong(i) : 0;
+  Py_XDECREF(i);
+  if (!i || PyErr_Occurred()) {
     PyErr_Clear();
     refuse("%s must be an integer in [0, 2^64)", name);
   }
