@@ -14,13 +14,16 @@
 #include <ATen/ops/empty.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/util/Exception.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/forward_grad.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdarg>
 #include <cstdio>
 #include <new>
+#include <optional>
 #include <stdexcept>
+#include <string>
 #include <vector>
 
 #include "../../include/bgmf.h"
@@ -30,6 +33,14 @@ namespace {
 struct Refused : std::runtime_error {
   using std::runtime_error::runtime_error;
 };
+// What the library refused, with its message.
+struct Failed : std::runtime_error {
+  int code;
+  explicit Failed(int rc) : std::runtime_error(bgmf_last_error(nullptr)), code(rc) {}
+};
+void check(int rc) {
+  if (rc != BGMF_OK) throw Failed(rc);
+}
 
 [[noreturn]] void refuse(const char *fmt, ...) __attribute__((format(printf, 1, 2)));
 void refuse(const char *fmt, ...) {
@@ -431,80 +442,171 @@ const void *reference_scores(PyObject *o, const at::Tensor &x, int64_t *stride) 
   return t.const_data_ptr();
 }
 
-// (scores, given, advantage, old_log_prob, reference, reference_log_prob,
-// kl_weight, clip_low, clip_high, temperature, excluded, want, weight, out,
-// stream) -> (loss, log_prob, kl, row_state or None, gradient or None)
-// want: 1 for row_state, 2 for the gradient of the losses times weight.
-PyObject *policy_loss(PyObject *const *a) {
-  int type;
-  const at::Tensor &x = matrix(a[0], "scores", kFloats, &type);
-  const int64_t rows = x.size(0), cols = x.size(1), want = integer(a[11], "want");
-  const auto floats = [&](PyObject *o, const char *name, bool optional) {
-    return static_cast<const float *>(vector(o, name, x, rows, at::kFloat, optional));
-  };
-  const void *given = vector(a[1], "given", x, rows, at::kInt, false);
-  const float *advantage = floats(a[2], "advantage", false),
-              *old_log_prob = floats(a[3], "old_log_prob", false),
-              *ref_log_prob = floats(a[5], "reference_log_prob", true),
-              *weight = floats(a[12], "weight", true);
-  int64_t ex_stride, ref_stride;
-  const void *ref = reference_scores(a[4], x, &ref_stride);
-  if (a[4] != Py_None && a[5] != Py_None) refuse("reference or reference_log_prob, not both");
-  const uint8_t *ex = excluded_items(a[10], x, &ex_stride);
-  const c10::DeviceGuard guard(x.device());
-  const at::Tensor loss = make({rows}, x, at::kFloat), log_prob = make({rows}, x, at::kFloat),
-                   kl = make({rows}, x, at::kFloat);
-  at::Tensor state, grad, ws;
-  if (want & 1) state = make({5, rows}, x, at::kFloat);
-  if (want & 2) grad = output(a[13], "out", x, rows, cols, x.scalar_type());
-  const int64_t ws_bytes = bgmf_policy_loss_workspace(rows, cols);
-  if (ws_bytes) ws = make({ws_bytes}, x, at::kByte);
-  const int rc = bgmf_policy_loss(
-      x.const_data_ptr(), type, rows, cols, x.stride(0), ref, ref_stride, ex, ex_stride,
-      static_cast<const int32_t *>(given), advantage, old_log_prob, ref_log_prob,
-      (float)number(a[9], "temperature"), (float)number(a[7], "clip_low"),
-      (float)number(a[8], "clip_high"), (float)number(a[6], "kl_weight"), at_<float>(loss),
-      at_<float>(log_prob), at_<float>(kl), want & 1 ? at_<float>(state) : nullptr, weight,
-      want & 2 ? grad.mutable_data_ptr() : nullptr, want & 2 ? grad.stride(0) : 0,
-      ws_bytes ? ws.mutable_data_ptr() : nullptr, ws_bytes, stream_of(a[14]));
-  if (rc != BGMF_OK) return PyLong_FromLong(rc);
-  if (want & 2) written(a[13], grad);
-  const auto or_none = [](const at::Tensor &t) {
-    if (t.defined()) return THPVariable_Wrap(t);
-    Py_INCREF(Py_None);
-    return Py_None;
-  };
-  return Py_BuildValue("(NNNNN)", THPVariable_Wrap(loss), THPVariable_Wrap(log_prob),
-                       THPVariable_Wrap(kl), or_none(state), or_none(grad));
+// The current stream of a device, from the function that ranking.py gave
+// (set_stream_function): a backward pass runs on a thread and, it may be, on a
+// stream of PyTorch's choice.
+PyObject *g_stream_function = nullptr;
+void *current_stream(const at::Device &device) {
+  const PyGILState_STATE gil = PyGILState_Ensure();
+  PyObject *r = PyObject_CallFunction(g_stream_function, "i", (int)device.index());
+  void *stream = r ? PyLong_AsVoidPtr(r) : nullptr;
+  const bool failed = !r || PyErr_Occurred();
+  PyErr_Clear();
+  Py_XDECREF(r);
+  PyGILState_Release(gil);
+  if (failed) throw std::runtime_error("no current stream");
+  return stream;
+}
+PyObject *set_stream_function(PyObject *const *a) {
+  Py_XDECREF(g_stream_function);
+  Py_INCREF(a[0]);
+  g_stream_function = a[0];
+  Py_INCREF(Py_None);
+  return Py_None;
 }
 
-// (scores, given, row_state, weight, reference, kl_weight, temperature,
-// excluded, out, stream) -> out
-PyObject *policy_loss_backward(PyObject *const *a) {
-  int type;
-  const at::Tensor &x = matrix(a[0], "scores", kFloats, &type);
-  const int64_t rows = x.size(0), cols = x.size(1);
-  const void *given = vector(a[1], "given", x, rows, at::kInt, false);
-  const at::Tensor &state = tensor(a[2], "row_state");
-  if (state.dim() != 2 || state.size(0) != 5 || state.size(1) != rows || !state.is_contiguous() ||
-      state.scalar_type() != at::kFloat || state.device() != x.device())
-    refuse("row_state must be a contiguous float32 tensor of shape (5, %lld) on the same GPU",
-           (long long)rows);
-  const float *weight =
-      static_cast<const float *>(vector(a[3], "weight", x, rows, at::kFloat, true));
-  int64_t ex_stride, ref_stride;
-  const void *ref = reference_scores(a[4], x, &ref_stride);
-  const uint8_t *ex = excluded_items(a[7], x, &ex_stride);
+using torch::autograd::AutogradContext;
+using torch::autograd::Variable;
+using torch::autograd::variable_list;
+
+// Results that have no derivative: a backward pass that reaches them raises.
+struct NoDerivative : torch::autograd::Function<NoDerivative> {
+  static Variable forward(AutogradContext *ctx, const Variable &result, const Variable &of,
+                          const Variable &and_of, std::string name) {
+    ctx->saved_data["name"] = name;
+    return result.view(result.sizes());
+  }
+  static variable_list backward(AutogradContext *ctx, variable_list) {
+    throw std::runtime_error(ctx->saved_data["name"].toStringRef() +
+                             " has no derivative: call it under torch.no_grad(), or on detached "
+                             "tensors");
+  }
+};
+bool in_graph(const Variable &t) {
+  return at::GradMode::is_enabled() && t.defined() && t.requires_grad();
+}
+
+at::Tensor policy_gradient(const at::Tensor &x, const at::Tensor &given, const at::Tensor &ref,
+                           const at::Tensor &ex, const float *state, const float *weight,
+                           double kl_weight, double temperature, const at::Tensor &out,
+                           void *stream) {
   const c10::DeviceGuard guard(x.device());
-  const at::Tensor out = output(a[8], "out", x, rows, cols, x.scalar_type());
-  const int rc = bgmf_policy_loss_grad(
-      x.const_data_ptr(), type, rows, cols, x.stride(0), ref, ref_stride, ex, ex_stride,
-      static_cast<const int32_t *>(given), (float)number(a[6], "temperature"),
-      (float)number(a[5], "kl_weight"), static_cast<const float *>(state.const_data_ptr()), weight,
-      out.mutable_data_ptr(), out.stride(0), stream_of(a[9]));
-  if (rc != BGMF_OK) return PyLong_FromLong(rc);
-  written(a[8], out);
-  return THPVariable_Wrap(out);
+  check(bgmf_policy_loss_grad(
+      x.const_data_ptr(), type_of(x), x.size(0), x.size(1), x.stride(0),
+      ref.defined() ? ref.const_data_ptr() : nullptr, ref.defined() ? ref.stride(0) : 0,
+      ex.defined() ? static_cast<const uint8_t *>(ex.const_data_ptr()) : nullptr,
+      ex.defined() ? ex.stride(0) : 0, static_cast<const int32_t *>(given.const_data_ptr()),
+      (float)temperature, (float)kl_weight, state, weight, out.mutable_data_ptr(), out.stride(0),
+      stream));
+  return out;
+}
+
+// (scores, given, advantage, old_log_prob, reference, reference_log_prob,
+// kl_weight, clip_low, clip_high, temperature, excluded, weight, out, stream),
+// checked; the three results, with row_state or the gradient where wanted.
+struct PolicyCall {
+  const at::Tensor &x;
+  int type;
+  int64_t rows, cols, ex_stride, ref_stride;
+  const void *given, *ref;
+  const float *advantage, *old_log_prob, *ref_log_prob, *weight;
+  const uint8_t *ex;
+  double kl_weight, clip_low, clip_high, temperature;
+  void *stream;
+  at::Tensor loss, log_prob, kl, state, grad;
+
+  explicit PolicyCall(PyObject *const *a) : x(matrix(a[0], "scores", kFloats, &type)) {
+    rows = x.size(0), cols = x.size(1);
+    const auto floats = [&](PyObject *o, const char *name, bool optional) {
+      return static_cast<const float *>(vector(o, name, x, rows, at::kFloat, optional));
+    };
+    given = vector(a[1], "given", x, rows, at::kInt, false);
+    advantage = floats(a[2], "advantage", false);
+    old_log_prob = floats(a[3], "old_log_prob", false);
+    ref_log_prob = floats(a[5], "reference_log_prob", true);
+    weight = floats(a[11], "weight", true);
+    ref = reference_scores(a[4], x, &ref_stride);
+    if (a[4] != Py_None && a[5] != Py_None)
+      refuse("reference or reference_log_prob, not both");
+    ex = excluded_items(a[10], x, &ex_stride);
+    kl_weight = number(a[6], "kl_weight"), clip_low = number(a[7], "clip_low");
+    clip_high = number(a[8], "clip_high"), temperature = number(a[9], "temperature");
+    stream = stream_of(a[13]);
+  }
+  void run(bool want_state, PyObject *out) {  // out: null for no gradient
+    const c10::DeviceGuard guard(x.device());
+    loss = make({rows}, x, at::kFloat), log_prob = make({rows}, x, at::kFloat);
+    kl = make({rows}, x, at::kFloat);
+    if (want_state) state = make({5, rows}, x, at::kFloat);
+    if (out) grad = output(out, "out", x, rows, cols, x.scalar_type());
+    at::Tensor ws;
+    const int64_t ws_bytes = bgmf_policy_loss_workspace(rows, cols);
+    if (ws_bytes) ws = make({ws_bytes}, x, at::kByte);
+    check(bgmf_policy_loss(
+        x.const_data_ptr(), type, rows, cols, x.stride(0), ref, ref_stride, ex, ex_stride,
+        static_cast<const int32_t *>(given), advantage, old_log_prob, ref_log_prob,
+        (float)temperature, (float)clip_low, (float)clip_high, (float)kl_weight, at_<float>(loss),
+        at_<float>(log_prob), at_<float>(kl), want_state ? at_<float>(state) : nullptr, weight,
+        out ? grad.mutable_data_ptr() : nullptr, out ? grad.stride(0) : 0,
+        ws_bytes ? ws.mutable_data_ptr() : nullptr, ws_bytes, stream));
+    if (out) written(out, grad);
+  }
+};
+
+at::Tensor or_undefined(PyObject *o) {
+  return o == Py_None ? at::Tensor() : THPVariable_Unpack(o);
+}
+
+// The loss in a graph: its derivative with respect to the scores.
+struct PolicyLoss : torch::autograd::Function<PolicyLoss> {
+  static variable_list forward(AutogradContext *ctx, const Variable &scores, PolicyCall *call,
+                               PyObject *const *a) {
+    call->run(true, nullptr);
+    ctx->save_for_backward({scores, THPVariable_Unpack(a[1]), or_undefined(a[4]),
+                            or_undefined(a[10]), call->state});
+    ctx->saved_data["kl_weight"] = call->kl_weight;
+    ctx->saved_data["temperature"] = call->temperature;
+    ctx->mark_non_differentiable({call->log_prob, call->kl});
+    return {call->loss, call->log_prob, call->kl};
+  }
+  static variable_list backward(AutogradContext *ctx, variable_list grads) {
+    const variable_list saved = ctx->get_saved_variables();
+    const Variable &x = saved[0], weight = grads[0].resolve_neg().contiguous();
+    Variable grad;
+    {
+      const at::NoGradGuard no_grad;
+      grad = policy_gradient(x, saved[1], saved[2], saved[3],
+                             static_cast<const float *>(saved[4].const_data_ptr()),
+                             static_cast<const float *>(weight.const_data_ptr()),
+                             ctx->saved_data["kl_weight"].toDouble(),
+                             ctx->saved_data["temperature"].toDouble(),
+                             make(x.sizes(), x, x.scalar_type()), current_stream(x.device()));
+    }
+    if (in_graph(x) || in_graph(grads[0]))
+      grad = NoDerivative::apply(grad, x, grads[0], std::string("the gradient of policy_loss"));
+    return {grad, Variable(), Variable()};
+  }
+};
+
+// PolicyCall's arguments -> (loss, log_prob, kl)
+PyObject *policy_loss(PyObject *const *a) {
+  PolicyCall call(a);
+  if (in_graph(call.x)) {
+    const variable_list r = PolicyLoss::apply(call.x, &call, a);
+    return Py_BuildValue("(NNN)", THPVariable_Wrap(r[0]), THPVariable_Wrap(r[1]),
+                         THPVariable_Wrap(r[2]));
+  }
+  call.run(false, nullptr);
+  return Py_BuildValue("(NNN)", THPVariable_Wrap(call.loss), THPVariable_Wrap(call.log_prob),
+                       THPVariable_Wrap(call.kl));
+}
+
+// The same -> (loss, log_prob, kl, the gradient of the losses times weight)
+PyObject *policy_loss_and_grad(PyObject *const *a) {
+  PolicyCall call(a);
+  call.run(false, a[12]);
+  return Py_BuildValue("(NNNN)", THPVariable_Wrap(call.loss), THPVariable_Wrap(call.log_prob),
+                       THPVariable_Wrap(call.kl), THPVariable_Wrap(call.grad));
 }
 
 // A Python (or numpy) integer in [0, 2^64).
@@ -519,6 +621,56 @@ uint64_t word(PyObject *o, const char *name) {
   return v;
 }
 
+// x dropped into out (undefined: a new tensor).
+at::Tensor dropped(const at::Tensor &x, double p, uint64_t seed, uint64_t offset,
+                   const at::Tensor &on_device, at::Tensor out, void *stream) {
+  int64_t rows = 1, cols = x.numel(), stride = cols, out_stride = cols;
+  const bool as_matrix = !x.is_contiguous() || (out.defined() && !out.is_contiguous());
+  const c10::DeviceGuard guard(x.device());
+  if (!out.defined()) {
+    out = make(x.sizes(), x, x.scalar_type());
+  } else if (out.sizes() != x.sizes() || out.scalar_type() != x.scalar_type() ||
+             out.device() != x.device()) {
+    refuse("out must have the shape, the type and the device of x");
+  }
+  if (as_matrix) {
+    if (x.dim() != 2 || (x.size(1) > 1 && (x.stride(1) != 1 || out.stride(1) != 1)))
+      refuse("x and out must be contiguous, or 2-D with adjacent row elements");
+    rows = x.size(0), cols = x.size(1), stride = x.stride(0), out_stride = out.stride(0);
+  }
+  check(bgmf_dropout(
+      x.const_data_ptr(), type_of(x), rows, cols, stride, p, seed, offset,
+      on_device.defined() ? static_cast<const uint64_t *>(on_device.const_data_ptr()) : nullptr,
+      out.mutable_data_ptr(), out_stride, stream));
+  return out;
+}
+
+// Dropout in a graph.  Its derivative drops the gradient alike, and has the same
+// derivative itself.
+struct Dropout : torch::autograd::Function<Dropout> {
+  static std::optional<at::Tensor> optional(const at::Tensor &t) {
+    return t.defined() ? std::optional<at::Tensor>(t) : std::nullopt;
+  }
+  static Variable forward(AutogradContext *ctx, const Variable &x, double p, int64_t seed,
+                          int64_t offset, const std::optional<at::Tensor> &more, void *stream) {
+    const Variable on_device = more ? *more : Variable();
+    ctx->save_for_backward({on_device});
+    ctx->saved_data["p"] = p, ctx->saved_data["seed"] = seed, ctx->saved_data["offset"] = offset;
+    return dropped(x, p, (uint64_t)seed, (uint64_t)offset, on_device, at::Tensor(), stream);
+  }
+  static variable_list backward(AutogradContext *ctx, variable_list grads) {
+    const Variable on_device = ctx->get_saved_variables()[0];
+    const Variable g = grads[0].resolve_neg().contiguous();
+    const double p = ctx->saved_data["p"].toDouble();
+    const int64_t seed = ctx->saved_data["seed"].toInt(), offset = ctx->saved_data["offset"].toInt();
+    void *stream = current_stream(g.device());
+    const Variable grad = in_graph(g) ? apply(g, p, seed, offset, optional(on_device), stream)
+                                      : dropped(g, p, (uint64_t)seed, (uint64_t)offset, on_device,
+                                                at::Tensor(), stream);
+    return {grad, Variable(), Variable(), Variable(), Variable(), Variable()};
+  }
+};
+
 // (x, p, seed, offset, out, stream) -> out
 PyObject *dropout(PyObject *const *a) {
   const at::Tensor &x = tensor(a[0], "x");
@@ -529,36 +681,24 @@ PyObject *dropout(PyObject *const *a) {
   const double p = number(a[1], "p");
   const uint64_t seed = word(a[2], "seed");
   uint64_t offset = 0;
-  const uint64_t *on_device = nullptr;
+  at::Tensor on_device;
   if (THPVariable_Check(a[3])) {
-    const at::Tensor &t = tensor(a[3], "offset");
-    if (t.numel() != 1 || t.scalar_type() != at::kLong || t.device() != x.device())
+    on_device = tensor(a[3], "offset");
+    if (on_device.numel() != 1 || on_device.scalar_type() != at::kLong ||
+        on_device.device() != x.device())
       refuse("offset must be an integer or an int64 tensor of one element on the same GPU");
-    on_device = static_cast<const uint64_t *>(t.const_data_ptr());
   } else {
     offset = word(a[3], "offset");
   }
-  int64_t rows = 1, cols = x.numel(), stride = cols, out_stride = cols;
-  const bool as_matrix = !x.is_contiguous() ||
-                         (a[4] != Py_None && !tensor(a[4], "out").is_contiguous());
-  const c10::DeviceGuard guard(x.device());
-  at::Tensor out;
-  if (a[4] == Py_None) {
-    out = make(x.sizes(), x, x.scalar_type());
-  } else {
-    out = tensor(a[4], "out");
-    if (out.sizes() != x.sizes() || out.scalar_type() != x.scalar_type() ||
-        out.device() != x.device())
-      refuse("out must have the shape, the type and the device of x");
+  if (in_graph(x)) {
+    if (a[4] != Py_None) refuse("dropout: out takes no part in a graph, and x requires grad");
+    return THPVariable_Wrap(
+        Dropout::apply(x, p, (int64_t)seed, (int64_t)offset, Dropout::optional(on_device),
+                       stream_of(a[5])));
   }
-  if (as_matrix) {
-    if (x.dim() != 2 || (x.size(1) > 1 && (x.stride(1) != 1 || out.stride(1) != 1)))
-      refuse("x and out must be contiguous, or 2-D with adjacent row elements");
-    rows = x.size(0), cols = x.size(1), stride = x.stride(0), out_stride = out.stride(0);
-  }
-  const int rc = bgmf_dropout(x.const_data_ptr(), type, rows, cols, stride, p, seed, offset,
-                              on_device, out.mutable_data_ptr(), out_stride, stream_of(a[5]));
-  if (rc != BGMF_OK) return PyLong_FromLong(rc);
+  const at::Tensor out = dropped(x, p, seed, offset, on_device,
+                                 a[4] == Py_None ? at::Tensor() : tensor(a[4], "out"),
+                                 stream_of(a[5]));
   written(a[4], out);
   return THPVariable_Wrap(out);
 }
@@ -581,6 +721,8 @@ PyObject *call(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return F(args);
   } catch (const Refused &e) {
     PyErr_SetString(PyExc_ValueError, e.what());
+  } catch (const Failed &e) {
+    return PyLong_FromLong(e.code);
   } catch (const c10::OutOfMemoryError &e) {
     set_out_of_memory(e);
   } catch (const std::bad_alloc &) {
@@ -606,8 +748,9 @@ PyMethodDef g_methods[] = {
     method<quantize_rows_mx, 2>("quantize_rows_mx"),
     method<dequantize_rows_mx, 6>("dequantize_rows_mx"),
     method<mx_scores, 7>("mx_scores"),
-    method<policy_loss, 15>("policy_loss"),
-    method<policy_loss_backward, 10>("policy_loss_backward"),
+    method<policy_loss, 14>("policy_loss"),
+    method<policy_loss_and_grad, 14>("policy_loss_and_grad"),
+    method<set_stream_function, 1>("set_stream_function"),
     method<dropout, 6>("dropout"),
     {nullptr, nullptr, 0, nullptr},
 };

@@ -48,6 +48,8 @@ class LogProbs(NamedTuple):
 
 # the current stream's address without a Stream object, where PyTorch offers it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_ranking.set_stream_function(
+    _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream))
 
 
 def _stream(t) -> int:
@@ -257,30 +259,6 @@ class PolicyLoss(NamedTuple):
     kl: torch.Tensor        # divergence from the reference, 0 without one
 
 
-class _PolicyLoss(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, scores, given, advantage, old_log_prob, reference, reference_log_prob,
-                kl_weight, clip_low, clip_high, temperature, excluded):
-        loss, log_prob, kl, state, _ = _checked(_ranking.policy_loss(
-            scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight,
-            clip_low, clip_high, temperature, excluded, 1, None, None, _stream(scores)))
-        ctx.save_for_backward(scores, given, reference, excluded, state)
-        ctx.kl_weight, ctx.temperature = kl_weight, temperature
-        ctx.mark_non_differentiable(log_prob, kl)
-        return loss, log_prob, kl
-
-    @staticmethod
-    def backward(ctx, g_loss, *_):
-        scores, given, reference, excluded, state = ctx.saved_tensors
-        weight = g_loss.resolve_neg().contiguous()
-        grad = _without_derivative(
-            "the gradient of policy_loss", lambda: _ranking.policy_loss_backward(
-                scores, given, state, weight, reference, ctx.kl_weight, ctx.temperature, excluded,
-                None, _stream(scores)),
-            None, scores, g_loss)
-        return (grad,) + (None,) * 10
-
-
 def _only_scores(name, *tensors):
     if _in_graph(*tensors):
         raise ValueError(f"{name} has a derivative with respect to the scores alone, and another "
@@ -304,13 +282,9 @@ def policy_loss(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tens
     respect to the scores through ``loss``.  include/bgmf.h says what empty
     rows, infinities and NaN give."""
     _only_scores("policy_loss", advantage, old_log_prob, reference, reference_log_prob)
-    if _in_graph(scores):
-        return PolicyLoss(*_PolicyLoss.apply(
-            scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight,
-            clip_low, clip_high, temperature, excluded))
     return PolicyLoss(*_checked(_ranking.policy_loss(
         scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight, clip_low,
-        clip_high, temperature, excluded, 0, None, None, _stream(scores)))[:3])
+        clip_high, temperature, excluded, None, None, _stream(scores))))
 
 
 def policy_loss_and_grad(scores: torch.Tensor, given: torch.Tensor, advantage: torch.Tensor,
@@ -329,32 +303,13 @@ def policy_loss_and_grad(scores: torch.Tensor, given: torch.Tensor, advantage: t
     graph."""
     _only_scores("policy_loss_and_grad", advantage, old_log_prob, reference, reference_log_prob,
                  weight)
-    loss, log_prob, kl, _, grad = _checked(_ranking.policy_loss(
+    loss, log_prob, kl, grad = _checked(_ranking.policy_loss_and_grad(
         scores, given, advantage, old_log_prob, reference, reference_log_prob, kl_weight, clip_low,
-        clip_high, temperature, excluded, 2, weight, out, _stream(scores)))
+        clip_high, temperature, excluded, weight, out, _stream(scores)))
     return PolicyLoss(loss, log_prob, kl), grad
 
 
 # --- dropout --------------------------------------------------------------------
-
-class _Dropout(torch.autograd.Function):
-    @staticmethod
-    def forward(ctx, x, p, seed, offset):
-        ctx.p, ctx.seed = p, seed
-        ctx.offset = None
-        if isinstance(offset, torch.Tensor):
-            ctx.save_for_backward(offset)
-        else:
-            ctx.offset = offset
-        return _checked(_ranking.dropout(x, p, seed, offset, None, _stream(x)))
-
-    @staticmethod
-    def backward(ctx, g):
-        offset = ctx.saved_tensors[0] if ctx.offset is None else ctx.offset
-        if g.is_neg() or not g.is_contiguous():
-            g = g.resolve_neg().contiguous()
-        return dropout(g, ctx.p, ctx.seed, offset), None, None, None
-
 
 def dropout(x: torch.Tensor, p: float, seed: int, offset=0, *,
             out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -368,10 +323,6 @@ def dropout(x: torch.Tensor, p: float, seed: int, offset=0, *,
     captured graph that adds to it drops other elements on each replay (it must
     not change between a forward and its backward pass, which raises).  ``out``
     may be ``x`` itself."""
-    if _in_graph(x):
-        if out is not None:
-            raise ValueError("dropout: out takes no part in a graph, and x requires grad")
-        return _Dropout.apply(x, p, seed, offset)
     return _checked(_ranking.dropout(x, p, seed, offset, out, _stream(x)))
 
 
