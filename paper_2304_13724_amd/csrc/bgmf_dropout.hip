@@ -48,7 +48,10 @@ __device__ __forceinline__ T dropped(const Dropout &P, uint32_t word, T x) {
 }
 
 // Elements in one row (a dense tensor): a thread takes 16-byte vectors, one or
-// two counters each.
+// two counters each.  Bound: 480,000 x 64 bf16 take 24.5 us: HBM, 5.0 TB/s, a large
+// copy's rate, and the vector units, at work 92% of the cycles (23 instructions an
+// element, 15 of them a quarter of a counter's ten rounds).  4,096 x 64 fp32 2.4 us:
+// latency.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_dropout(Dropout P) {
   constexpr int N = Vec<T>::N;
@@ -80,7 +83,7 @@ __global__ void __launch_bounds__(kThreads) k_dropout(Dropout P) {
 }
 
 // Rows that are apart: a thread takes a counter's four elements, which may lie
-// in several rows.
+// in several rows (element by element, with two 64-bit divisions a counter).
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_dropout_rows(Dropout P) {
   const uint64_t offset = P.offset + (P.more ? *P.more : 0);

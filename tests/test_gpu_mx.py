@@ -151,6 +151,44 @@ def test_product(out, rows, items, k):
         assert (both | edge).all()
 
 
+# more tiles than workgroups at a time, of 128 x 128 and of 128 x 64, in one and in
+# several steps, and long rows in tiles of 256 x 256 with rows, items and blocks left over
+LARGE = [(3000, 5003, 64), (2999, 5000, 40), (3001, 4999, 200), (2100, 6001, 300),
+         (60, 140_003, 64), (64, 140_000, 200), (2900, 2801, 2048), (2817, 2900, 2100),
+         (3000, 3001, 2300), (300, 18_000, 4090), (257, 16_500, 2049)]
+
+
+@pytest.mark.parametrize("rows,items,k", LARGE)
+def test_product_exact_large(rows, items, k):
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    grid = torch.from_numpy(GRID).float().cuda()
+
+    def draw_exact(n):
+        x = grid[torch.randint(0, 8, (n, k), generator=g, device="cuda")]
+        x = x * (torch.randint(0, 2, (n, k), generator=g, device="cuda") * 2 - 1)
+        x[:, ::32] = 4.0
+        return x * 2.0 ** (torch.arange(n, device="cuda") % 3)[:, None]  # scales of its own
+
+    x, v = draw_exact(rows), draw_exact(items)
+    want = (x.double() @ v.double().t()).float()
+    w, b = ranking.quantize_rows_mx4(v)
+    q, a = ranking.quantize_rows_mx4(x)
+    assert torch.equal(ranking.mx4_scores(x, w, b), want)
+    assert torch.equal(ranking.mx4_scores(q, w, b, a), want)
+    # items apart, with NaN scales and other bytes between them
+    blocks = blocks_of(k)
+    wide = torch.full((items, 17 * blocks + 11), 255, dtype=torch.uint8, device="cuda")
+    wide[:, 3:3 + 16 * blocks], wide[:, 7 + 16 * blocks:7 + 17 * blocks] = w, b
+    got = ranking.mx4_scores(x.bfloat16(), wide[:, 3:3 + 16 * blocks],
+                             wide[:, 7 + 16 * blocks:7 + 17 * blocks], dtype=torch.bfloat16)
+    assert torch.equal(got, want.bfloat16())
+    # NaN blocks at the ends: their own rows and items alone
+    x[rows - 1, k - 1], v[0, 0], v[items - 1, k - 1] = float("nan"), float("inf"), float("nan")
+    got = ranking.mx4_scores(x, *ranking.quantize_rows_mx4(v))
+    want[rows - 1], want[:, 0], want[:, items - 1] = float("nan"), float("nan"), float("nan")
+    assert torch.equal(got.nan_to_num(7.5), want.nan_to_num(7.5))
+
+
 @pytest.mark.parametrize("rows,items,k", [(1, 70, 64), (3, 300, 96), (40, 500, 70), (200, 300, 64),
                                           (300, 600, 600), (5, 9000, 128)])
 def test_product_blocks_that_stand_for_nan(rows, items, k):
