@@ -548,7 +548,7 @@ struct Many {
 // overlap their loads, products and stores.  A workgroup's bytes of the next
 // step, or of its next tile, are on their way into registers meanwhile.  Bound:
 // HBM (the scores) up to k of some hundred: 2,048 users x 18,000 items, k = 64, to bf16
-// takes 15.8 us, 4.7 TB/s.
+// takes 15.7 us, 4.7 TB/s.
 template <class O, int BI, int BU, int STEP>
 __global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4)
     k_mx_many(Product P, int64_t tiles) {
@@ -600,17 +600,17 @@ __global__ void __launch_bounds__(kThreads, BI * BU == 4 ? 3 : 4)
   }
 }
 
+// Kinds of instructions that the scheduler is told to place.
+constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
+
 // Long rows: tiles of 256 x 256, eight blocks at a time, which halves the LDS
 // traffic per product.  One workgroup fills a CU, so a wave itself reads its
 // next pair of blocks from LDS while the matrix unit works, and a step's bytes
 // are loaded a whole step before they go to the other LDS buffer.  Bound: the
-// instructions' issue and the clock: 4,096 x 8,192 x 4,096 to bf16 takes 81 us, 3.4e15
-// operations a second (matrix instructions alone reach 5.2e15 to 6.2e15 on this card,
-// on values that are not all alike); the matrix units work 40% of the cycles, and some
-// 15 us go into the first loads and the stores of the two tiles that each CU has.
-// Kinds of instructions that the scheduler is told to place.
-constexpr int kMfma = 0x8, kVmemRead = 0x20, kDsRead = 0x100, kDsWrite = 0x200;
-
+// instructions' issue and the clock: 4,096 x 8,192 x 4,096 to bf16 takes 81 to 85 us,
+// 3.3e15 operations a second (matrix instructions alone reach 5.2e15 to 6.2e15 on this
+// card, on values that are not all alike); the matrix units work 45% of the cycles, and
+// some 15 us go into the first loads and the stores of the two tiles that each CU has.
 template <class O>
 __global__ void __launch_bounds__(kThreads, 1) k_mx_large(Product P) {
   using M = Many<O, 4, 4, 128>;
@@ -961,9 +961,9 @@ int bgmf_mx_scores(const void *x, int32_t type, int64_t rows, int64_t k, int64_t
       shares(item_scale, BGMF_TYPE_I8, item_count, blocks, item_scale_stride))
     return fail_call(BGMF_E_ARG, "%s: out shares memory with an input", call);
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  Product p{nullptr, row_stride, (int32_t)k, static_cast<const uint8_t *>(x), row_scale, rows, row_stride, row_scale_stride,
-            items, item_scale, item_count, items_stride, item_scale_stride, (int32_t)blocks,
-            out, out_stride};
+  Product p{nullptr, row_stride, (int32_t)k, static_cast<const uint8_t *>(x), row_scale, rows,
+            row_stride, row_scale_stride, items, item_scale, item_count, items_stride,
+            item_scale_stride, (int32_t)blocks, out, out_stride};
   hipError_t e = hipSuccess;
   if (own && takes_values(rows, item_count, blocks)) {
     p.x = x, p.a = nullptr;

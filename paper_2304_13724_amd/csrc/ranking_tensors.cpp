@@ -486,18 +486,51 @@ bool in_graph(const Variable &t) {
   return at::GradMode::is_enabled() && t.defined() && t.requires_grad();
 }
 
-at::Tensor policy_gradient(const at::Tensor &x, const at::Tensor &given, const at::Tensor &ref,
-                           const at::Tensor &ex, const float *state, const float *weight,
-                           double kl_weight, double temperature, const at::Tensor &out,
-                           void *stream) {
+// A gradient as autograd passes it, in memory of its own kind: a view that negates
+// is resolved, a tensor of zeros without memory gets some.  One whose derivative
+// would be lost is refused.
+at::Tensor passed(const Variable &g) {
+  if (g._fw_grad(0).defined())
+    throw Refused("a gradient has a tangent: forward-mode derivatives are not supported");
+  if (!g.has_storage()) throw Refused("a gradient has no memory of its own (vmap?)");
+  return (g._is_zerotensor() ? make(g.sizes(), g, g.scalar_type()).zero_() : g.resolve_neg())
+      .contiguous();
+}
+
+// Saved tensors come back as they were, unless a hook of the caller's changes them.
+void same_as(bool same, const char *name) {
+  if (!same) throw Refused(std::string("the saved ") + name + " came back changed");
+}
+
+// The gradient from what the forward pass saved.
+at::Tensor policy_gradient(const variable_list &saved, const at::Tensor &weight, double kl_weight,
+                           double temperature) {
+  const at::Tensor &x = saved[0], &given = saved[1], &ref = saved[2], &ex = saved[3],
+                   &state = saved[4];
+  const int64_t rows = x.size(0), cols = x.size(1);
+  const auto adjacent = [&](const at::Tensor &t) {
+    return t.is_cuda() && t.device() == x.device() && t.sizes() == x.sizes() &&
+           (cols < 2 || t.stride(1) == 1);
+  };
+  const auto dense = [&](const at::Tensor &t, at::ScalarType type, int64_t count) {
+    return t.device() == x.device() && t.scalar_type() == type && t.numel() == count &&
+           t.is_contiguous();
+  };
+  same_as(adjacent(x), "scores");
+  same_as(dense(given, at::kInt, rows), "given");
+  same_as(!ref.defined() || (adjacent(ref) && ref.scalar_type() == x.scalar_type()), "reference");
+  same_as(!ex.defined() || (adjacent(ex) && ex.element_size() == 1), "excluded");
+  same_as(dense(state, at::kFloat, 5 * rows) && dense(weight, at::kFloat, rows), "state");
   const c10::DeviceGuard guard(x.device());
+  const at::Tensor out = make(x.sizes(), x, x.scalar_type());
   check(bgmf_policy_loss_grad(
-      x.const_data_ptr(), type_of(x), x.size(0), x.size(1), x.stride(0),
+      x.const_data_ptr(), type_of(x), rows, cols, x.stride(0),
       ref.defined() ? ref.const_data_ptr() : nullptr, ref.defined() ? ref.stride(0) : 0,
       ex.defined() ? static_cast<const uint8_t *>(ex.const_data_ptr()) : nullptr,
       ex.defined() ? ex.stride(0) : 0, static_cast<const int32_t *>(given.const_data_ptr()),
-      (float)temperature, (float)kl_weight, state, weight, out.mutable_data_ptr(), out.stride(0),
-      stream));
+      (float)temperature, (float)kl_weight, static_cast<const float *>(state.const_data_ptr()),
+      static_cast<const float *>(weight.const_data_ptr()), out.mutable_data_ptr(), out.stride(0),
+      current_stream(x.device())));
   return out;
 }
 
@@ -571,16 +604,12 @@ struct PolicyLoss : torch::autograd::Function<PolicyLoss> {
   }
   static variable_list backward(AutogradContext *ctx, variable_list grads) {
     const variable_list saved = ctx->get_saved_variables();
-    const Variable &x = saved[0], weight = grads[0].resolve_neg().contiguous();
+    const Variable &x = saved[0];
     Variable grad;
     {
       const at::NoGradGuard no_grad;
-      grad = policy_gradient(x, saved[1], saved[2], saved[3],
-                             static_cast<const float *>(saved[4].const_data_ptr()),
-                             static_cast<const float *>(weight.const_data_ptr()),
-                             ctx->saved_data["kl_weight"].toDouble(),
-                             ctx->saved_data["temperature"].toDouble(),
-                             make(x.sizes(), x, x.scalar_type()), current_stream(x.device()));
+      grad = policy_gradient(saved, passed(grads[0]), ctx->saved_data["kl_weight"].toDouble(),
+                             ctx->saved_data["temperature"].toDouble());
     }
     if (in_graph(x) || in_graph(grads[0]))
       grad = NoDerivative::apply(grad, x, grads[0], std::string("the gradient of policy_loss"));
@@ -659,8 +688,10 @@ struct Dropout : torch::autograd::Function<Dropout> {
     return dropped(x, p, (uint64_t)seed, (uint64_t)offset, on_device, at::Tensor(), stream);
   }
   static variable_list backward(AutogradContext *ctx, variable_list grads) {
-    const Variable on_device = ctx->get_saved_variables()[0];
-    const Variable g = grads[0].resolve_neg().contiguous();
+    const Variable on_device = ctx->get_saved_variables()[0], g = passed(grads[0]);
+    same_as(!on_device.defined() || (on_device.numel() == 1 && on_device.device() == g.device() &&
+                                     on_device.scalar_type() == at::kLong),
+            "offset");
     const double p = ctx->saved_data["p"].toDouble();
     const int64_t seed = ctx->saved_data["seed"].toInt(), offset = ctx->saved_data["offset"].toInt();
     void *stream = current_stream(g.device());

@@ -5,6 +5,7 @@ import pytest
 from paper_2304_13724_amd import bgmf, ranking
 
 import torch
+from torch.autograd import forward_ad
 
 from philox import words
 
@@ -128,6 +129,27 @@ def test_gradients_as_autograd_may_pass_them():
               torch.ones(7, 6, device="cuda").t()):
         (got,) = torch.autograd.grad(y, x, g, retain_graph=True)
         assert torch.equal(got, ranking.dropout(torch.ones(6, 7, device="cuda"), 0.5, 4))
+
+
+def test_gradients_without_memory_or_with_a_tangent():
+    x = draw((6, 7), torch.float32).cuda().requires_grad_()
+    y = ranking.dropout(x, 0.5, 4)
+    zeros = torch._efficientzerotensor((6, 7), device="cuda")
+    assert torch.autograd.grad(y, x, zeros, retain_graph=True)[0].eq(0).all()
+    ones = torch.ones(6, 7, device="cuda")
+    with forward_ad.dual_level():
+        with pytest.raises(RuntimeError, match="tangent"):
+            torch.autograd.grad(y, x, forward_ad.make_dual(ones, ones), retain_graph=True)
+    with pytest.raises(RuntimeError, match="memory"):
+        torch.autograd.grad(y, x, torch.ones(2, 6, 7, device="cuda"), is_grads_batched=True)
+
+
+def test_an_offset_that_a_hook_changes_is_refused():
+    x = draw((6, 7), torch.float32).cuda().requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(torch.Tensor.int, lambda t: t):
+        y = ranking.dropout(x, 0.5, 4, torch.tensor([3]).cuda())
+    with pytest.raises(RuntimeError, match="came back changed"):
+        y.sum().backward()
 
 
 def test_no_graph_with_an_output():

@@ -7,6 +7,7 @@ import pytest
 from paper_2304_13724_amd import bgmf, ranking
 
 import torch
+from torch.autograd import forward_ad
 
 import policy_bounds as pb
 
@@ -394,6 +395,37 @@ def test_gradients_as_autograd_may_pass_them():
     for g in (torch.ones(1, device="cuda").expand(4), torch._neg_view(-torch.ones(4).cuda()),
               torch.ones(8, device="cuda")[::2]):
         assert torch.equal(torch.autograd.grad(r.loss, x, g, retain_graph=True)[0], want)
+
+
+def test_gradients_without_memory_or_with_a_tangent():
+    c = pb.case(4, 50, torch.float32, 1)
+    a, o = args(c), options(c, "full")
+    x = a[0].requires_grad_()
+    r = ranking.policy_loss(x, *a[1:], **o)
+    zeros = torch._efficientzerotensor((4,), device="cuda")
+    (got,) = torch.autograd.grad(r.loss, x, zeros, retain_graph=True)
+    assert torch.equal(got, torch.zeros(4, 50, device="cuda"))
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(torch.ones(4, device="cuda"), torch.ones(4, device="cuda"))
+        with pytest.raises(RuntimeError, match="tangent"):
+            torch.autograd.grad(r.loss, x, dual, retain_graph=True)
+    with pytest.raises(RuntimeError, match="memory"):
+        torch.autograd.grad(r.loss, x, torch.eye(4, device="cuda"), is_grads_batched=True)
+
+
+@pytest.mark.parametrize("change", [torch.Tensor.half, torch.Tensor.cpu, lambda t: t[:1]])
+def test_saved_tensors_that_a_hook_changes_are_refused(change):
+    c = pb.case(4, 50, torch.float32, 1)
+    a, o = args(c), options(c, "full")
+    x = a[0].requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(change, lambda t: t):
+        r = ranking.policy_loss(x, *a[1:], **o)
+    with pytest.raises(RuntimeError, match="came back changed"):
+        r.loss.sum().backward()
+    with torch.autograd.graph.save_on_cpu():
+        r = ranking.policy_loss(x, *a[1:], **o)
+    (got,) = torch.autograd.grad(r.loss.sum(), x)
+    assert torch.equal(got, torch.autograd.grad(ranking.policy_loss(x, *a[1:], **o).loss.sum(), x)[0])
 
 
 def test_refusals_on_the_gpu():
