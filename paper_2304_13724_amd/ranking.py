@@ -12,6 +12,10 @@ BgmfError for what the library refuses), runs the library's kernels
 (include/bgmf.h) on the current stream of the tensors' device and returns
 without waiting.  There is no fallback: importing this module raises if
 _ranking.so is missing.
+
+Calls can be captured into a graph, backward passes too, as long as no autograd
+graph from before the capture still holds the same leaves (PyTorch adds up a
+leaf's gradient on the stream of the first).
 """
 from __future__ import annotations
 
