@@ -9,7 +9,7 @@
 namespace bgmfk {
 namespace {
 
-// Threads of a workgroup: 256, or one wave for short rows (TH below).
+// Threads of a workgroup (where it is not TH).
 constexpr int kThreads = 256;
 
 struct Policy {
@@ -35,107 +35,6 @@ struct Policy {
 // compiler has no builtin for it).
 extern "C" __device__ float bgmf_mul_legacy(float a, float b) __asm("llvm.amdgcn.fmul.legacy");
 __device__ __forceinline__ float times_or_0(float a, float b) { return bgmf_mul_legacy(a, b); }
-
-// Running sums of a row's scores x and of the reference's y, m and my the
-// largest of each so far, d = (x - m) c and dy = (y - my) c:
-//   s = sum exp2(d)   sy = sum exp2(dy)   w = sum exp2(d) (d - dy)
-// from which ln s, ln sy and the mean w / s of d - dy under p give
-//   sum p ln(p / q) = (w / s) ln 2 - ln s + ln sy.
-// Both differences are taken from their own maximum, so an offset between the
-// two policies' scores costs nothing, and one item alone gives exactly 0.  A
-// group's terms are summed in fp32 and added to running sums in fp64: the
-// divergence is a small difference of large terms.  A score of -inf adds
-// nothing; a NaN or +inf makes s (or sy) NaN.
-template <bool REF>
-struct Sums {
-  float m = -INFINITY, my = -INFINITY;
-  double s = 0.0, w = 0.0, sy = 0.0;
-  static __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
-  // to the maxima M >= m and My >= my
-  __device__ __forceinline__ void rescale(float M, float My, float c) {
-    if (m != -INFINITY) {  // (otherwise s and w are 0, or NaN from a NaN)
-      const float f = __builtin_amdgcn_exp2f((m - M) * c);
-      // (in 64 bits, where maxima of the type's lowest value leave it finite)
-      if constexpr (REF)
-        w = (w + s * ((((double)m - M) + ((double)base_of(My) - base_of(my))) * c)) * f;
-      s *= f;
-    }
-    if constexpr (REF)
-      if (my != -INFINITY) sy *= __builtin_amdgcn_exp2f((my - My) * c);
-    m = M, my = My;
-  }
-  // A group's sums, with m and my not below its scores.
-  struct Group {
-    float s = 0.0f, w = 0.0f, sy = 0.0f;
-    template <int COUNT>
-    __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float bx,
-                                        float by, float c) {
-      // d and dy are rounded alike, so that equal scores leave exactly 0
-#pragma clang fp contract(off)
-#pragma unroll
-      for (int i = 0; i < COUNT; ++i) {
-        const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
-        s += e;
-        if constexpr (REF) {
-          const float dy = (y[i] - by) * c;
-          sy += __builtin_amdgcn_exp2f(dy);
-          w += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
-        }
-      }
-    }
-  };
-  __device__ __forceinline__ void add(const Group &g) {
-    s += g.s;
-    if constexpr (REF) w += g.w, sy += g.sy;
-  }
-  template <int COUNT>
-  __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float gm,
-                                      float gmy, float c) {  // the largest of x and of y
-    if (gm > m || (REF && gmy > my)) rescale(fmaxf(m, gm), REF ? fmaxf(my, gmy) : my, c);
-    Group g;
-    g.add(x, y, base_of(m), base_of(my), c);
-    add(g);
-  }
-};
-
-// Over the workgroup in a fixed order; every thread has the result.
-template <int TH>
-struct SumsLds {
-  float m[TH / 64], my[TH / 64];
-  double s[TH / 64], w[TH / 64], sy[TH / 64];
-};
-template <int TH, bool REF>
-__device__ __forceinline__ Sums<REF> block_sums(Sums<REF> a, float c, SumsLds<TH> &lds) {
-  constexpr int W = TH / 64;
-  const int wave = threadIdx.x / 64;
-  Sums<REF> r;
-  r.m = wave_max(a.m);
-  if constexpr (REF) r.my = wave_max(a.my);
-  if constexpr (W > 1) {
-    if (threadIdx.x % 64 == 0) lds.m[wave] = r.m, lds.my[wave] = r.my;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      r.m = fmaxf(r.m, lds.m[i]);
-      if constexpr (REF) r.my = fmaxf(r.my, lds.my[i]);
-    }
-  }
-  a.rescale(r.m, r.my, c);
-  a.s = wave_sum(a.s);
-  if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
-  if constexpr (W == 1) {
-    r.s = a.s, r.w = a.w, r.sy = a.sy;
-  } else {
-    if (threadIdx.x % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-      r.s += lds.s[i];
-      if constexpr (REF) r.w += lds.w[i], r.sy += lds.sy[i];
-    }
-  }
-  return r;
-}
 
 // exp(x) - 1 and exp(x) to 6e-10 of themselves, by the series of exp over [-ln 2 /
 // 2, ln 2 / 2] to the eighth power and a power of two; ln S, to as much, from a
@@ -166,6 +65,107 @@ __device__ __forceinline__ double ln(double s) {  // s > 0, in the range of 32 b
   const double y = (double)__builtin_amdgcn_logf((float)s) * kLn2;
   const double d = s * Exp(-y).value - 1.0;
   return y + fma(-0.5 * d, d, d);
+}
+
+// Running sums of a row's scores x and of the reference's y, m and my the
+// largest of each so far, d = (x - m) c and dy = (y - my) c:
+//   s = sum exp2(d)   sy = sum exp2(dy)   w = sum exp2(d) (d - dy)
+// from which ln s, ln sy and the mean w / s of d - dy under p give
+//   sum p ln(p / q) = (w / s) ln 2 - ln s + ln sy.
+// Both differences are taken from their own maximum, so an offset between the
+// two policies' scores costs nothing, and one item alone gives exactly 0.  The
+// divergence is a small difference of large terms, so with a reference s and sy
+// are summed in fp64 from the start (with a group's terms in fp32 it was four times
+// as far off as by their own roundings, 2e-6 of itself over 16 items); w, and s
+// alone, in fp32 within a group.  A score of -inf adds nothing; a NaN or +inf makes
+// s (or sy) NaN.
+template <bool REF>
+struct Sums {
+  float m = -INFINITY, my = -INFINITY;
+  double s = 0.0, w = 0.0, sy = 0.0;
+  static __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.0f : m; }
+  // to the maxima M >= m and My >= my
+  __device__ __forceinline__ void rescale(float M, float My, float c) {
+    if (m != -INFINITY) {  // (otherwise s and w are 0, or NaN from a NaN)
+      const float f = __builtin_amdgcn_exp2f((m - M) * c);
+      // (in 64 bits, where maxima of the type's lowest value leave it finite)
+      if constexpr (REF)
+        w = (w + s * ((((double)m - M) + ((double)base_of(My) - base_of(my))) * c)) * f;
+      s *= f;
+    }
+    if constexpr (REF)
+      if (my != -INFINITY) sy *= __builtin_amdgcn_exp2f((my - My) * c);
+    m = M, my = My;
+  }
+  // A group's sums, with m and my not below its scores.  HELD: in fp32, and in place
+  // of sy the sum of exp2(dy) - exp2(d) (see k_policy_step).
+  template <bool HELD>
+  struct Group {
+    using Sum = std::conditional_t<REF && !HELD, double, float>;
+    Sum s = 0, sy = 0;
+    float w = 0.0f;
+    template <int COUNT>
+    __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float bx,
+                                        float by, float c) {
+      // d and dy are rounded alike, so that equal scores leave exactly 0
+#pragma clang fp contract(off)
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) {
+        const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
+        s += e;
+        if constexpr (REF) {
+          const float dy = (y[i] - by) * c, ey = __builtin_amdgcn_exp2f(dy);
+          sy += HELD ? ey - e : ey;
+          w += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
+        }
+      }
+    }
+  };
+  template <bool HELD>
+  __device__ __forceinline__ void add(const Group<HELD> &g) {
+    s += g.s;
+    if constexpr (REF) w += g.w, sy += g.sy;
+  }
+  template <int COUNT>
+  __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float gm,
+                                      float gmy, float c) {  // the largest of x and of y
+    if (gm > m || (REF && gmy > my)) rescale(fmaxf(m, gm), REF ? fmaxf(my, gmy) : my, c);
+    Group<false> g;
+    g.add(x, y, base_of(m), base_of(my), c);
+    add(g);
+  }
+};
+
+// Over the workgroup in a fixed order; every thread has the result.
+constexpr int kWaves = kThreads / 64;
+struct SumsLds {
+  float m[kWaves], my[kWaves];
+  double s[kWaves], w[kWaves], sy[kWaves];
+};
+template <bool REF>
+__device__ __forceinline__ Sums<REF> block_sums(Sums<REF> a, float c, SumsLds &lds) {
+  const int wave = threadIdx.x / 64;
+  Sums<REF> r;
+  r.m = wave_max(a.m);
+  if constexpr (REF) r.my = wave_max(a.my);
+  if (threadIdx.x % 64 == 0) lds.m[wave] = r.m, lds.my[wave] = r.my;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    r.m = fmaxf(r.m, lds.m[i]);
+    if constexpr (REF) r.my = fmaxf(r.my, lds.my[i]);
+  }
+  a.rescale(r.m, r.my, c);
+  a.s = wave_sum(a.s);
+  if constexpr (REF) a.w = wave_sum(a.w), a.sy = wave_sum(a.sy);
+  if (threadIdx.x % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) {
+    r.s += lds.s[i];
+    if constexpr (REF) r.w += lds.w[i], r.sy += lds.sy[i];
+  }
+  return r;
 }
 
 // What the gradient needs of a row: with d and dy as above,
@@ -377,15 +377,16 @@ struct Pair {
   }
 };
 
-// One workgroup per row, or per part of a row; the scores and the reference are
-// read once.  Bound: HBM: 4,001 x 10,007 f32 with a reference take 59 us, 5.4 TB/s.  A
-// workgroup has one row and no loop over rows: the compiler would keep the 64-bit
-// functions' constants in registers through it (87 in place of 39, so that fewer
-// waves' loads are in flight).
+// Long rows without a gradient: one workgroup per row, or per part of a row; the scores
+// and the reference are read once.  Bound: HBM and the vector units: 33 x 625,001 f32
+// with a reference take 41 us, 4.0 TB/s; 4,001 x 10,007 59 us, 5.4 TB/s.  A workgroup has
+// one row and no loop over rows: the compiler would keep the 64-bit functions'
+// constants in registers through it (twice as many, so that fewer waves' loads are in
+// flight).
 constexpr int kGroup = 2;
-template <class T, bool EX, bool REF, int TH>
-__global__ void __launch_bounds__(TH) k_policy(Policy P) {
-  __shared__ SumsLds<TH> lds;
+template <class T, bool EX, bool REF>
+__global__ void __launch_bounds__(kThreads) k_policy(Policy P) {
+  __shared__ SumsLds lds;
   using Two = Pair<T, EX, REF>;
   constexpr int N = Two::N;
   const int tid = threadIdx.x;
@@ -406,18 +407,18 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
   const auto fetch = [&](int32_t v0) {
 #pragma unroll
     for (int g = 0; g < kGroup; ++g)
-      if (v0 + g * TH + tid < vecs) next[g] = two.fetch(v0 + g * TH + tid);
+      if (v0 + g * kThreads + tid < vecs) next[g] = two.fetch(v0 + g * kThreads + tid);
   };
   fetch(0);
   if (P.given[r] == -1) vecs = 0, tail = false;
-  for (int32_t v0 = 0; v0 < vecs; v0 += TH * kGroup) {
+  for (int32_t v0 = 0; v0 < vecs; v0 += kThreads * kGroup) {
     typename Two::Raw raw[kGroup];
 #pragma unroll
     for (int g = 0; g < kGroup; ++g) raw[g] = next[g];
-    fetch(v0 + TH * kGroup);
+    fetch(v0 + kThreads * kGroup);
 #pragma unroll
     for (int g = 0; g < kGroup; ++g) {
-      if (v0 + g * TH + tid >= vecs) break;
+      if (v0 + g * kThreads + tid >= vecs) break;
       float x[N], y[N], gm = -INFINITY, gmy = -INFINITY;
       Two::exclude(raw[g]);
       Two::scores(raw[g], x, y);
@@ -432,7 +433,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
     const float y[1] = {two.other(i)};
     a.add(x, y, x[0], y[0], c);
   }
-  const Sums<REF> all = block_sums<TH>(a, c, lds);
+  const Sums<REF> all = block_sums(a, c, lds);
   if (tid == 0) {
     if (P.parts == 1) finish(P, r, Given<T, REF>(P, r), all);
     else P.part_sum[u] = PartSum{all.s, all.w, all.sy, all.m, all.my};
@@ -444,7 +445,7 @@ __global__ void __launch_bounds__(TH) k_policy(Policy P) {
 constexpr int64_t kMostParts = 4 * kThreads;
 template <class T, bool REF>
 __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
-  __shared__ SumsLds<kThreads> lds;
+  __shared__ SumsLds lds;
   const float c = kLog2e / P.temperature;
   for (int64_t r = blockIdx.x; r < P.rows; r += gridDim.x) {
     const PartSum *sums = P.part_sum + r * P.parts;
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
       b.rescale(M, My, c);
       a.s += b.s, a.w += b.w, a.sy += b.sy;
     }
-    const Sums<REF> all = block_sums<kThreads>(a, c, lds);
+    const Sums<REF> all = block_sums(a, c, lds);
     if (threadIdx.x == 0) finish(P, r, given, all);
     __syncthreads();
   }
@@ -524,9 +525,9 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
 }
 
 // ---------------------------------------------------------------------------
-// Both at once, for rows that fit the registers of a workgroup (H vectors a
-// thread): the scores and the reference are read and the gradient is written
-// once.  Three passes over the registers: the maxima, the sums with them, the
+// Rows that fit the registers of a workgroup (H vectors a thread), with their
+// gradient or without: the scores and the reference are read and the gradient is
+// written once.  Three passes over the registers: the maxima, the sums with them, the
 // gradient.  Bound: 2,047 x 18,000 bf16 with a reference and exclusions take 54 us:
 // HBM, 4.8 TB/s, and the vector units (75% of the CUs' cycles, 37 instructions a
 // score, three exponentials among them); 16 x 18,000 f32 6.2 us: latency (a row's
@@ -589,7 +590,7 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
     }
     // the sums, of 16 scores in 32 bits
     const float bx = Sums<REF>::base_of(a.m), by = Sums<REF>::base_of(a.my);
-    typename Sums<REF>::Group group;
+    typename Sums<REF>::template Group<true> group;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       if (h * TH + tid < vecs) {
@@ -613,18 +614,46 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
     if constexpr (W > 1) {
       if (tid % 64 == 0) lds.s[wave] = a.s, lds.w[wave] = a.w, lds.sy[wave] = a.sy;
       __syncthreads();
-    }
-  }
-  if (tid == 0) {
-    if (W > 1 && g != -1) {
       a.s = a.w = a.sy = 0.0;
       for (int i = 0; i < W; ++i) {
         a.s += lds.s[i];
         if constexpr (REF) a.w += lds.w[i], a.sy += lds.sy[i];
       }
     }
+    if constexpr (REF) {
+      // sy from the sum of differences, whose rounding the divergence does not
+      // magnify; where the two policies are so far apart that it would be lost
+      // beside s, by itself
+      if (fabs(a.sy) <= 0.5 * a.s) {
+        a.sy += a.s;
+      } else {  // of all threads
+        a.sy = 0.0;
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+          if (h * TH + tid < vecs) {
+            float x[N], y[N], sum = 0.0f;
+            Two::renew(raw[h]);
+            Two::scores(raw[h], x, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) sum += __builtin_amdgcn_exp2f((y[i] - by) * c);
+            a.sy += sum;
+          }
+        if (tail) a.sy += __builtin_amdgcn_exp2f((y1 - by) * c);
+        a.sy = wave_sum(a.sy);
+        if constexpr (W > 1) {
+          __syncthreads();
+          if (tid % 64 == 0) lds.sy[wave] = a.sy;
+          __syncthreads();
+          a.sy = 0.0;
+          for (int i = 0; i < W; ++i) a.sy += lds.sy[i];
+        }
+      }
+    }
+  }
+  if (tid == 0) {
     lds.st = finish(P, r, given, a);
   }
+  if (!P.out) return;  // of all threads
   __syncthreads();
   const Slopes<REF> grad(P, r, lds.st);
   // the thread whose vector has the given item writes it once more
@@ -698,14 +727,16 @@ void policy_grad(Policy p, hipStream_t stream) {
   });
 }
 
-// Whether the call that gives both goes through the scores once.  With exclusions and
-// a reference, once and twice: f32 4,096 x 18,000 183 and 301 us, 4,096 x 36,000 418
-// and 577, 16 x 18,000 8.6 and 12.4, 1 x 36,000 14.3 and 12.0 (one workgroup has all of
-// it); bf16 4,096 x 18,000 101 and 172.
+// Whether a row is held in registers.  With exclusions and a reference, the results and
+// the gradient in one pass and in two: f32 4,096 x 18,000 182 and 299 us, 4,096 x
+// 36,000 392 and 577, 16 x 18,000 8.7 and 12.5, 1 x 36,000 12.4 and 12.3 (one workgroup
+// has all of it); bf16 4,096 x 18,000 101 and 173.  The results alone, held and by
+// k_policy: f32 4,096 x 10,000 67.1 and 67.9, 16 rows 5.6 and 7.8; bf16 4,096 x 18,000
+// 66.5 and 70.6, 16 rows 7.2 and 8.9.
 constexpr int kMostHeld = 9;
 template <class T>
 bool in_registers(const Policy &p) {
-  return p.out && p.cols && p.cols <= kMostHeld * 1024 * Vec<T>::N;
+  return p.cols <= (p.out ? kMostHeld * 1024 : 5 * 512) * Vec<T>::N;
 }
 
 template <class T>
@@ -725,9 +756,9 @@ hipError_t policy_step(Policy p, hipStream_t stream) {
     using Most = integral_constant<int, kMostHeld>;
     // the fewest threads that hold a row, but for few rows no more than five vectors
     // each.  With exclusions and a reference: bf16 4,096 x 2,000 by 64 x 4 and 256 x 5
-    // 18.0 and 21.1 us, 16 x 2,000 5.7 and 4.7; 4,096 x 18,000 by 256 x 9 and 512 x 5 101
-    // and 107, 256 x 18,000 10.6 and 10.2; f32 4,096 x 18,000 by 512 x 9 and 1,024 x 5
-    // 183 and 208, 512 rows 21.7 and 28.0, 256 rows 14.7 and 14.3
+    // 18.3 and 21.3 us, 16 x 2,000 5.8 and 4.8; 4,096 x 18,000 by 256 x 9 and 512 x 5 101
+    // and 108, 256 x 18,000 10.8 and 10.4; f32 4,096 x 18,000 by 512 x 9 and 1,024 x 5
+    // 182 and 213, 512 rows 21.5 and 27.9, 256 rows 14.4 and 14.4
     const bool many = p.rows >= 512;
     if (vecs <= 4 * 64) go(integral_constant<int, 64>{}, integral_constant<int, 4>{});
     else if (vecs <= 5 * 256) go(integral_constant<int, 256>{}, Few{});
@@ -748,10 +779,7 @@ hipError_t policy(Policy p, hipStream_t stream) {
     const int64_t units = p.rows * p.parts;
     for (p.first = 0; p.first < units; p.first += kMostGroups) {
       const dim3 groups((unsigned)std::min(units - p.first, kMostGroups));
-      if (p.cols <= kShortRow)
-        hipLaunchKernelGGL((k_policy<T, EX, REF, 64>), groups, dim3(64), 0, stream, p);
-      else
-        hipLaunchKernelGGL((k_policy<T, EX, REF, kThreads>), groups, dim3(kThreads), 0, stream, p);
+      hipLaunchKernelGGL((k_policy<T, EX, REF>), groups, dim3(kThreads), 0, stream, p);
     }
     if (p.parts > 1)
       hipLaunchKernelGGL((k_policy_join<T, REF>), dim3((unsigned)std::min(p.rows, kMostGroups)),
