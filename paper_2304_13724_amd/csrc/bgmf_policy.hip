@@ -74,11 +74,11 @@ __device__ __forceinline__ double ln(double s) {  // s > 0, in the range of 32 b
 //   sum p ln(p / q) = (w / s) ln 2 - ln s + ln sy.
 // Both differences are taken from their own maximum, so an offset between the
 // two policies' scores costs nothing, and one item alone gives exactly 0.  The
-// divergence is a small difference of large terms, so with a reference s and sy
-// are summed in fp64 from the start (with a group's terms in fp32 it was four times
-// as far off as by their own roundings, 2e-6 of itself over 16 items); w, and s
-// alone, in fp32 within a group.  A score of -inf adds nothing; a NaN or +inf makes
-// s (or sy) NaN.
+// divergence is a small difference of large terms: a group's are summed in fp32 and
+// added to running sums in fp64, and in place of sy goes the sum of exp2(dy) -
+// exp2(d), beside which the rounding of s cancels (with sy itself the divergence
+// was four times as far off as by its terms' own roundings, 2e-6 of itself over 16
+// items).  A score of -inf adds nothing; a NaN or +inf makes s (or sy) NaN.
 template <bool REF>
 struct Sums {
   float m = -INFINITY, my = -INFINITY;
@@ -97,13 +97,9 @@ struct Sums {
       if (my != -INFINITY) sy *= __builtin_amdgcn_exp2f((my - My) * c);
     m = M, my = My;
   }
-  // A group's sums, with m and my not below its scores.  HELD: in fp32, and in place
-  // of sy the sum of exp2(dy) - exp2(d) (see k_policy_step).
-  template <bool HELD>
+  // A group's sums, with m and my not below its scores.
   struct Group {
-    using Sum = std::conditional_t<REF && !HELD, double, float>;
-    Sum s = 0, sy = 0;
-    float w = 0.0f;
+    float s = 0.0f, w = 0.0f, sy = 0.0f;
     template <int COUNT>
     __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float bx,
                                         float by, float c) {
@@ -114,25 +110,16 @@ struct Sums {
         const float d = (x[i] - bx) * c, e = __builtin_amdgcn_exp2f(d);
         s += e;
         if constexpr (REF) {
-          const float dy = (y[i] - by) * c, ey = __builtin_amdgcn_exp2f(dy);
-          sy += HELD ? ey - e : ey;
+          const float dy = (y[i] - by) * c;
+          sy += __builtin_amdgcn_exp2f(dy) - e;
           w += times_or_0(e, d - dy);  // (e may be 0 where d - dy is not finite)
         }
       }
     }
   };
-  template <bool HELD>
-  __device__ __forceinline__ void add(const Group<HELD> &g) {
+  __device__ __forceinline__ void add(const Group &g) {
     s += g.s;
     if constexpr (REF) w += g.w, sy += g.sy;
-  }
-  template <int COUNT>
-  __device__ __forceinline__ void add(const float (&x)[COUNT], const float (&y)[COUNT], float gm,
-                                      float gmy, float c) {  // the largest of x and of y
-    if (gm > m || (REF && gmy > my)) rescale(fmaxf(m, gm), REF ? fmaxf(my, gmy) : my, c);
-    Group<false> g;
-    g.add(x, y, base_of(m), base_of(my), c);
-    add(g);
   }
 };
 
@@ -377,72 +364,8 @@ struct Pair {
   }
 };
 
-// Long rows without a gradient: one workgroup per row, or per part of a row; the scores
-// and the reference are read once.  Bound: HBM and the vector units: 33 x 625,001 f32
-// with a reference take 41 us, 4.0 TB/s; 4,001 x 10,007 59 us, 5.4 TB/s.  A workgroup has
-// one row and no loop over rows: the compiler would keep the 64-bit functions'
-// constants in registers through it (twice as many, so that fewer waves' loads are in
-// flight).
-constexpr int kGroup = 2;
-template <class T, bool EX, bool REF>
-__global__ void __launch_bounds__(kThreads) k_policy(Policy P) {
-  __shared__ SumsLds lds;
-  using Two = Pair<T, EX, REF>;
-  constexpr int N = Two::N;
-  const int tid = threadIdx.x;
-  const float c = kLog2e / P.temperature;
-  const int64_t u = P.first + blockIdx.x;
-  const int64_t r = P.parts == 1 ? u : u / P.parts, part = P.parts == 1 ? 0 : u % P.parts;
-  const int64_t first = part * P.part_len;
-  const int64_t left = P.cols - first;
-  const int32_t len = (int32_t)(left < P.part_len ? left : P.part_len);
-  const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
-                 EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
-                REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
-  Sums<REF> a;
-  int32_t vecs = two.row.vecs();
-  bool tail = tid < len - vecs * N;
-  // the vectors of the next group are on their way while this one's are summed
-  typename Two::Raw next[kGroup];
-  const auto fetch = [&](int32_t v0) {
-#pragma unroll
-    for (int g = 0; g < kGroup; ++g)
-      if (v0 + g * kThreads + tid < vecs) next[g] = two.fetch(v0 + g * kThreads + tid);
-  };
-  fetch(0);
-  if (P.given[r] == -1) vecs = 0, tail = false;
-  for (int32_t v0 = 0; v0 < vecs; v0 += kThreads * kGroup) {
-    typename Two::Raw raw[kGroup];
-#pragma unroll
-    for (int g = 0; g < kGroup; ++g) raw[g] = next[g];
-    fetch(v0 + kThreads * kGroup);
-#pragma unroll
-    for (int g = 0; g < kGroup; ++g) {
-      if (v0 + g * kThreads + tid >= vecs) break;
-      float x[N], y[N], gm = -INFINITY, gmy = -INFINITY;
-      Two::exclude(raw[g]);
-      Two::scores(raw[g], x, y);
-#pragma unroll
-      for (int i = 0; i < N; ++i) gm = fmaxf(gm, x[i]), gmy = fmaxf(gmy, y[i]);
-      a.add(x, y, gm, gmy, c);
-    }
-  }
-  if (tail) {
-    const int32_t i = vecs * N + tid;
-    const float x[1] = {two.row.one(i)};
-    const float y[1] = {two.other(i)};
-    a.add(x, y, x[0], y[0], c);
-  }
-  const Sums<REF> all = block_sums(a, c, lds);
-  if (tid == 0) {
-    if (P.parts == 1) finish(P, r, Given<T, REF>(P, r), all);
-    else P.part_sum[u] = PartSum{all.s, all.w, all.sy, all.m, all.my};
-  }
-}
-
-// Joins the parts of a row: one workgroup per row.  Bound: latency (33 rows of 62
+// Joins the parts of a row: one workgroup per row.  Bound: latency (33 rows of 123
 // parts: 4.4 us).
-constexpr int64_t kMostParts = 4 * kThreads;
 template <class T, bool REF>
 __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
   __shared__ SumsLds lds;
@@ -526,8 +449,9 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
 
 // ---------------------------------------------------------------------------
 // Rows that fit the registers of a workgroup (H vectors a thread), with their
-// gradient or without: the scores and the reference are read and the gradient is
-// written once.  Three passes over the registers: the maxima, the sums with them, the
+// gradient or without, or (PART) parts of a row, whose sums are joined: the scores and
+// the reference are read and the gradient is written once, all of a row on its way
+// at the same time.  Three passes over the registers: the maxima, the sums with them, the
 // gradient.  Bound: 2,047 x 18,000 bf16 with a reference and exclusions take 54 us:
 // HBM, 4.8 TB/s, and the vector units (75% of the CUs' cycles, 37 instructions a
 // score, three exponentials among them); 16 x 18,000 f32 6.2 us: latency (a row's
@@ -539,19 +463,20 @@ struct StepLds {
   double s[TH / 64], w[TH / 64], sy[TH / 64];
   State st;
 };
-template <class T, bool EX, bool REF, int TH, int H>
+template <class T, bool EX, bool REF, bool PART, int TH, int H>
 __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(Policy P) {
   __shared__ StepLds<TH> lds;
   using Two = Pair<T, EX, REF>;
   constexpr int N = Two::N, W = TH / 64;
   const int tid = threadIdx.x, wave = tid / 64;
   const float c = kLog2e / P.temperature;
-  const int32_t len = (int32_t)P.cols, vecs = len / N;
-  const int64_t r = P.first + blockIdx.x;
+  const int64_t u = P.first + blockIdx.x, r = PART ? u / P.parts : u;
+  const int64_t first = PART ? u % P.parts * P.part_len : 0, left = P.cols - first;
+  const int32_t len = (int32_t)(PART && left > P.part_len ? P.part_len : left), vecs = len / N;
   T *out = static_cast<T *>(P.out) + r * P.out_stride;
-  const Two two{{static_cast<const T *>(P.x) + r * P.stride,
-                 EX ? P.ex + r * P.ex_stride : nullptr, len},
-                REF ? static_cast<const T *>(P.y) + r * P.y_stride : nullptr};
+  const Two two{{static_cast<const T *>(P.x) + (r * P.stride + first),
+                 EX ? P.ex + (r * P.ex_stride + first) : nullptr, len},
+                REF ? static_cast<const T *>(P.y) + (r * P.y_stride + first) : nullptr};
   const bool tail = tid < len - vecs * N;
   Sums<REF> a;
   typename Two::Raw raw[H];
@@ -560,8 +485,11 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
   for (int h = 0; h < H; ++h)
     if (h * TH + tid < vecs) raw[h] = two.fetch(h * TH + tid);
   if (tail) x1 = two.row.one(vecs * N + tid), y1 = two.other(vecs * N + tid);
-  const Given<T, REF> given(P, r);
-  const int64_t g = given.item;
+  std::conditional_t<PART, int, Given<T, REF>> given = [&] {
+    if constexpr (PART) return 0;
+    else return Given<T, REF>(P, r);
+  }();
+  const int64_t g = P.given[r];
   if (g != -1) {  // of all threads
     // the largest
     a.m = x1, a.my = y1;
@@ -590,7 +518,7 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
     }
     // the sums, of 16 scores in 32 bits
     const float bx = Sums<REF>::base_of(a.m), by = Sums<REF>::base_of(a.my);
-    typename Sums<REF>::template Group<true> group;
+    typename Sums<REF>::Group group;
 #pragma unroll
     for (int h = 0; h < H; ++h) {
       if (h * TH + tid < vecs) {
@@ -650,51 +578,47 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
       }
     }
   }
-  if (tid == 0) {
-    lds.st = finish(P, r, given, a);
-  }
-  if (!P.out) return;  // of all threads
-  __syncthreads();
-  const Slopes<REF> grad(P, r, lds.st);
-  // the thread whose vector has the given item writes it once more
-  const bool own = given.inside &&
-                   (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
+  if constexpr (PART) {
+    if (tid == 0) P.part_sum[u] = PartSum{a.s, a.w, a.sy, a.m, a.my};
+  } else {
+    if (tid == 0) lds.st = finish(P, r, given, a);
+    if (!P.out) return;  // of all threads
+    __syncthreads();
+    const Slopes<REF> grad(P, r, lds.st);
+    // the thread whose vector has the given item writes it once more
+    const bool own = given.inside &&
+                     (g / N < vecs ? (int)(g / N % TH) : (int)(g - vecs * N)) == tid;
 #pragma unroll
-  for (int h = 0; h < H; ++h) {
-    const int32_t v = h * TH + tid;
-    if (v < vecs) {
-      Two::renew(raw[h]);
-      store_vec(out + (int64_t)v * N, two.gradient(v, raw[h], grad));
+    for (int h = 0; h < H; ++h) {
+      const int32_t v = h * TH + tid;
+      if (v < vecs) {
+        Two::renew(raw[h]);
+        store_vec(out + (int64_t)v * N, two.gradient(v, raw[h], grad));
+      }
     }
+    if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
+    if (own) out[g] = given_gradient<T>(given.x, given.y, given.excluded, grad);
   }
-  if (tail) out[vecs * N + tid] = two.gradient(vecs * N + tid, grad);
-  if (own) out[g] = given_gradient<T>(given.x, given.y, given.excluded, grad);
 }
 
 constexpr int64_t kMostGroups = 1 << 20;
 
-// How a row is split: rows of up to kWhole scores not at all, others in as few
-// parts as hold at most kPart each, but in no more than fill the GPU (eight
-// workgroups for each of 256 CUs) or than kMostParts.  The join costs some 2.5 us:
-// one row and its reference in one part and in two, bf16 8,000 scores 5.2 us and
-// 10,000 7.8, f32 6.1 and 8.1, and a part takes 1 to 1.4 us more for each 4,000.  33
-// rows of 625,001 f32 in 39 parts of 16,384 take 46 us, in 62 41.
-constexpr int64_t kFullGpu = 2048, kWhole = 16384, kPart = 8192;
+// Rows that no workgroup holds go in as few parts as one of 256 threads holds (kPart
+// vectors), all as long, and a join.  Parts of 256 x 5, 256 x 9 and 512 x 5, with
+// exclusions and a reference: f32 33 x 625,001 34.0, 34.5 and 33.9 us, 1 x 200,000 7.7,
+// 8.7 and 8.7, 4,096 x 24,000 158, 162 and 159; bf16 128 x 200,000 27.7, 29.2 and 31.6.
+// (Going through a longer part with running sums, next vectors on their way: 35.7,
+// 9.8, 157 and 33.0.)
+constexpr int64_t kPart = 5 * 256;
 struct Split {
   int64_t parts, len;
 };
-Split split_of(int64_t rows, int64_t cols) {
-  int64_t parts = std::min({(cols + kPart - 1) / kPart,
-                            std::max<int64_t>(kFullGpu / std::max<int64_t>(rows, 1), 1), kMostParts});
-  if (cols <= kWhole || parts <= 1) return {1, cols};
+Split split_of(int64_t cols, int64_t per) {  // per: scores of a vector
+  const int64_t parts = (cols + kPart * per - 1) / (kPart * per);
   const int64_t len = ((cols + parts - 1) / parts + 63) / 64 * 64;
   return {(cols + len - 1) / len, len};
 }
 int64_t padded(int64_t x) { return (x + 255) / 256 * 256; }
-int64_t parts_bytes(int64_t rows, int64_t cols) {
-  const int64_t parts = split_of(rows, cols).parts;
-  return parts == 1 ? 0 : padded(rows * parts * (int64_t)sizeof(PartSum));
-}
 
 // Rows of at most this many scores go to workgroups of one wave (as in log_probs,
 // whose figures are at its constant).
@@ -727,16 +651,16 @@ void policy_grad(Policy p, hipStream_t stream) {
   });
 }
 
-// Whether a row is held in registers.  With exclusions and a reference, the results and
-// the gradient in one pass and in two: f32 4,096 x 18,000 182 and 299 us, 4,096 x
-// 36,000 392 and 577, 16 x 18,000 8.7 and 12.5, 1 x 36,000 12.4 and 12.3 (one workgroup
-// has all of it); bf16 4,096 x 18,000 101 and 173.  The results alone, held and by
-// k_policy: f32 4,096 x 10,000 67.1 and 67.9, 16 rows 5.6 and 7.8; bf16 4,096 x 18,000
-// 66.5 and 70.6, 16 rows 7.2 and 8.9.
-constexpr int kMostHeld = 9;
+// Whether a workgroup holds a row.  With exclusions and a reference, the results and the
+// gradient in one pass and in two: f32 4,096 x 18,000 182 and 299 us, 4,096 x 36,000 392
+// and 577, 16 x 18,000 8.7 and 12.5, 1 x 36,000 12.4 and 12.3 (one workgroup has all of
+// it); bf16 4,096 x 18,000 101 and 173.  The results alone, held and in parts: f32
+// 4,096 x 18,000 111 and 122, 8 rows 7.0 and 8.2, 8 x 36,000 10.1 and 8.2; bf16 8 x
+// 36,000 10.4 and 9.1, 512 rows 23.7 and 23.7.
+constexpr int64_t kMostHeld = 9 * 1024, kMostHeldValue = 9 * 512;  // vectors
 template <class T>
 bool in_registers(const Policy &p) {
-  return p.cols <= (p.out ? kMostHeld * 1024 : 5 * 512) * Vec<T>::N;
+  return p.cols <= (p.out ? kMostHeld : kMostHeldValue) * Vec<T>::N;
 }
 
 template <class T>
@@ -747,13 +671,13 @@ hipError_t policy_step(Policy p, hipStream_t stream) {
     const auto go = [&](auto threads, auto held) {
       constexpr int TH = decltype(threads)::value, H = decltype(held)::value;
       for (p.first = 0; p.first < p.rows; p.first += kMostGroups)
-        hipLaunchKernelGGL((k_policy_step<T, EX, REF, TH, H>),
+        hipLaunchKernelGGL((k_policy_step<T, EX, REF, false, TH, H>),
                            dim3((unsigned)std::min(p.rows - p.first, kMostGroups)), dim3(TH), 0,
                            stream, p);
     };
     using std::integral_constant;
     using Few = integral_constant<int, 5>;
-    using Most = integral_constant<int, kMostHeld>;
+    using Most = integral_constant<int, 9>;
     // the fewest threads that hold a row, but for few rows no more than five vectors
     // each.  With exclusions and a reference: bf16 4,096 x 2,000 by 64 x 4 and 256 x 5
     // 18.3 and 21.3 us, 16 x 2,000 5.8 and 4.8; 4,096 x 18,000 by 256 x 9 and 512 x 5 101
@@ -774,18 +698,19 @@ hipError_t policy_step(Policy p, hipStream_t stream) {
 template <class T>
 hipError_t policy(Policy p, hipStream_t stream) {
   if (in_registers<T>(p)) return policy_step<T>(p, stream);
+  const Split split = split_of(p.cols, Vec<T>::N);
+  p.parts = split.parts, p.part_len = split.len;
   with_flags(p.ex, p.y, [&](auto ex, auto ref) {
     constexpr bool EX = decltype(ex)::value, REF = decltype(ref)::value;
     const int64_t units = p.rows * p.parts;
-    for (p.first = 0; p.first < units; p.first += kMostGroups) {
-      const dim3 groups((unsigned)std::min(units - p.first, kMostGroups));
-      hipLaunchKernelGGL((k_policy<T, EX, REF>), groups, dim3(kThreads), 0, stream, p);
-    }
-    if (p.parts > 1)
-      hipLaunchKernelGGL((k_policy_join<T, REF>), dim3((unsigned)std::min(p.rows, kMostGroups)),
-                         dim3(kThreads), 0, stream, p);
+    for (p.first = 0; p.first < units; p.first += kMostGroups)
+      hipLaunchKernelGGL((k_policy_step<T, EX, REF, true, 256, 5>),
+                         dim3((unsigned)std::min(units - p.first, kMostGroups)), dim3(256), 0,
+                         stream, p);
+    hipLaunchKernelGGL((k_policy_join<T, REF>), dim3((unsigned)std::min(p.rows, kMostGroups)),
+                       dim3(kThreads), 0, stream, p);
   });
-  if (p.out && p.cols) policy_grad<T>(p, stream);
+  if (p.out) policy_grad<T>(p, stream);
   return hipGetLastError();
 }
 
@@ -845,12 +770,13 @@ using namespace bgmfk;
 
 extern "C" {
 
-// Workspace: the parts' sums, then row_state where the caller wants none and rows
-// of some type do not fit registers.
+// Workspace: row_state where the caller wants none, then the parts' sums, of the
+// type whose rows have most.
 int64_t bgmf_policy_loss_workspace(int64_t rows, int64_t cols) {
-  if (rows <= 0 || cols <= 0 || rows >= (1ll << 31) || cols >= (1ll << 31)) return 0;
-  return parts_bytes(rows, cols) +
-         (cols > kMostHeld * 1024 * 4 ? padded(5 * rows * (int64_t)sizeof(float)) : 0);
+  if (rows <= 0 || cols <= kMostHeldValue * 4 || rows >= (1ll << 31) || cols >= (1ll << 31))
+    return 0;
+  return padded(5 * rows * (int64_t)sizeof(float)) +
+         rows * split_of(cols, 4).parts * (int64_t)sizeof(PartSum);
 }
 
 int bgmf_policy_loss(const void *scores, int32_t type, int64_t rows, int64_t cols,
@@ -885,11 +811,11 @@ int bgmf_policy_loss(const void *scores, int32_t type, int64_t rows, int64_t col
   if (ws_bytes < need)
     return fail_call(BGMF_E_BUDGET, "%s: the workspace has %lld bytes, %lld are needed", call,
                      (long long)ws_bytes, (long long)need);
-  const Split split = split_of(rows, cols);
-  p.parts = split.parts, p.part_len = split.len;
-  p.part_sum = static_cast<PartSum *>(ws);
-  if (grad_scores && !row_state && cols > kMostHeld * 1024 * 4)
-    p.state = reinterpret_cast<float *>(static_cast<char *>(ws) + parts_bytes(rows, cols));
+  if (need) {
+    if (grad_scores && !row_state) p.state = static_cast<float *>(ws);
+    p.part_sum = reinterpret_cast<PartSum *>(static_cast<char *>(ws) +
+                                             padded(5 * rows * (int64_t)sizeof(float)));
+  }
   hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   const hipError_t e = type == BGMF_TYPE_F32    ? policy<float>(p, stream)
                        : type == BGMF_TYPE_BF16 ? policy<bf16_t>(p, stream)

@@ -88,3 +88,35 @@ def test_the_divergence_is_as_exact_as_its_terms():
     for call in (ranking.policy_loss, lambda *a, **o: ranking.policy_loss_and_grad(*a, **o)[0]):
         kl = call(*at, reference=c["y"], kl_weight=pb.KL, temperature=c["t"]).kl
         assert (kl.double() - want).square().mean().sqrt() <= 4 * 2.0 ** -24 * 0.3
+
+
+@pytest.mark.parametrize("cols", [18_432, 18_433, 20_480, 20_481, 25_600, 36_865, 512_063])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_parts(dtype, cols):
+    """Rows in parts: whole ones, a last one of one score, one that is left whole by its
+    exclusions alone, rows that fill the batch up."""
+    cols *= 4 // dtype.itemsize
+    c = on_gpu(pb.case(7, cols, dtype, 3, excluded=True))
+    c["ex"][2, :cols // 2] = True
+    c["ex"][torch.arange(7), c["given"]] = False
+    D, _, lnS, _ = pb.softmax_of(c["x"].double(), c["t"], c["ex"])
+    c["old"] = (-D.gather(1, c["given"][:, None]) - lnS)[:, 0].sub(0.1).float()
+    o = dict(reference=c["y"], kl_weight=pb.KL, clip_low=pb.LO, clip_high=pb.HI,
+             temperature=c["t"], excluded=c["ex"])
+    want = pb.reference(
+        c["x"].double(), c["given"], c["adv"].double(), c["old"].double(), c["t"], pb.LO, pb.HI,
+        pb.KL, y=c["y"].double(), excluded=c["ex"], g=c["weight"].double())
+    given = c["given"].int()
+    given[5] = -1
+    leaf = c["x"].clone().requires_grad_()
+    r = ranking.policy_loss(leaf, given, c["adv"], c["old"], **o)
+    r.loss.backward(c["weight"])
+    rows = torch.tensor([0, 1, 2, 3, 4, 6]).cuda()
+    for name in ("loss", "log_prob", "kl"):
+        got = getattr(r, name).detach().double()
+        v, tol = want[name]
+        assert ((got - v).abs() <= tol)[rows].all(), name
+        assert got[5] == 0
+    v, err = want["grad"]
+    assert ((leaf.grad.double() - v).abs() <= pb.allowed(v, err, dtype))[rows].all()
+    assert (leaf.grad[5] == 0).all()
