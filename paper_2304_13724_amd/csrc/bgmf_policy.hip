@@ -452,10 +452,12 @@ __global__ void __launch_bounds__(TH) k_policy_grad(Policy P) {
 // gradient or without, or (PART) parts of a row, whose sums are joined: the scores and
 // the reference are read and the gradient is written once, all of a row on its way
 // at the same time.  Three passes over the registers: the maxima, the sums with them, the
-// gradient.  Bound: 2,047 x 18,000 bf16 with a reference and exclusions take 54 us:
-// HBM, 4.8 TB/s, and the vector units (75% of the CUs' cycles, 37 instructions a
-// score, three exponentials among them); 16 x 18,000 f32 6.2 us: latency (a row's
-// loads, three reductions, the 64-bit functions of one thread).
+// gradient.  A workgroup has one row and no loop over rows (the compiler would keep the
+// 64-bit functions' constants in registers through it).  Bound: 2,047 x 18,000 bf16
+// with a reference, exclusions and the gradient take 55 us: HBM, 4.7 TB/s, and the vector
+// units (87% of the CUs' cycles, 39 instructions a score, three exponentials among
+// them); 4,001 x 10,007 f32 with a reference alone 55 us, 5.8 TB/s; 16 x 18,000 f32 6.0
+// us: latency (a row's loads, three reductions, the 64-bit functions of one thread).
 // ---------------------------------------------------------------------------
 template <int TH>
 struct StepLds {
