@@ -702,7 +702,10 @@ __global__ void __launch_bounds__(kThreads, 1) k_mx_large(Product P) {
 
 // Workgroups that fill the GPU: eight of four waves on each of 256 CUs.
 constexpr int64_t kFullGpu = 2048;
-constexpr int64_t kCached = 192 << 20;  // items that stay in the 256 MB Infinity Cache
+// Bytes of items that stay in the Infinity Cache between calls; more are read past the
+// caches.  One user, k = 64, through and past them: 7M items (213 MB) 41.7 and 46.6 us,
+// 8M 49.3 and 52.6, 10M 72.4 and 64.0, 20M 146 and 127.
+constexpr int64_t kCached = 256 << 20;
 
 template <class O, class X, int STEPS, bool LONG>
 void launch_few(Product p, hipStream_t stream) {
