@@ -398,9 +398,9 @@ struct Many {
   }
 
   // A thread's blocks of step s of the items from j0 on (kItems of them are
-  // there) and of the users from r0 on (whose rows are laid out up to a multiple
-  // of kUserPad).  A thread's offset within its first row is 32 bits wide (see
-  // kMostStride).
+  // there) and of the users from r0 on (kUsers rows are, as they are laid out up to
+  // a multiple of kUserPad; none behind them need be).  A thread's offset within its
+  // first row is 32 bits wide (see kMostStride).
   static __device__ __forceinline__ void load(const Product &P, int64_t j0, int64_t r0, int s,
                                               i32x4 (&x)[kItemLoads], i32x4 (&y)[kUserLoads]) {
     const int row = threadIdx.x / kChunks, chunk = threadIdx.x % kChunks;
@@ -418,7 +418,8 @@ struct Many {
 #pragma unroll
     for (int h = 0; h < kUserLoads; ++h) {
       y[h] = i32x4{};
-      if (some) y[h] = block_bytes(a + h * kPass * P.a_stride + at_user);
+      if (some && (kPass <= kUsers || row < kUsers))
+        y[h] = block_bytes(a + h * kPass * P.a_stride + at_user);
     }
   }
   static __device__ __forceinline__ void store(i32x4 *buffer, const i32x4 (&x)[kItemLoads],
