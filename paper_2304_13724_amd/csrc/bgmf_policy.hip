@@ -235,9 +235,12 @@ __device__ __forceinline__ State finish(const Policy &P, int64_t r, const Given<
   return st;
 }
 
+// A part's sums.  w is that of the items whose reference is not 0, so that it can be
+// rescaled; none: the largest score of the others (-inf: there are none), by which
+// the row decides whether they count.
 struct PartSum {
   double s, w, sy;
-  float m, my;
+  float m, my, none;
 };
 
 // A row's gradient but for its given item's own term: with d, dy and e = exp2(d),
@@ -374,16 +377,26 @@ __global__ void __launch_bounds__(kThreads) k_policy_join(Policy P) {
     const PartSum *sums = P.part_sum + r * P.parts;
     const Given<T, REF> given(P, r);
     Sums<REF> a;
+    float none = -INFINITY;
     for (int64_t i = threadIdx.x; i < P.parts; i += kThreads) {
       Sums<REF> b;
       b.m = sums[i].m, b.s = sums[i].s;
-      if constexpr (REF) b.my = sums[i].my, b.w = sums[i].w, b.sy = sums[i].sy;
+      if constexpr (REF) {
+        b.my = sums[i].my, b.w = sums[i].w, b.sy = sums[i].sy;
+        none = fmaxf(none, sums[i].none);
+      }
       const float M = fmaxf(a.m, b.m), My = fmaxf(a.my, b.my);
       a.rescale(M, My, c);
       b.rescale(M, My, c);
       a.s += b.s, a.w += b.w, a.sy += b.sy;
     }
-    const Sums<REF> all = block_sums(a, c, lds);
+    Sums<REF> all = block_sums(a, c, lds);
+    if constexpr (REF) {
+      // p > 0 = q, by the exponential that a row held in registers has
+      const bool infinite =
+          __builtin_amdgcn_exp2f((none - Sums<REF>::base_of(all.m)) * c) > 0.0f;
+      if (__syncthreads_or(infinite)) all.w = INFINITY;
+    }
     if (threadIdx.x == 0) finish(P, r, given, all);
     __syncthreads();
   }
@@ -581,7 +594,37 @@ __global__ void __launch_bounds__(TH, TH > 512 || H > 5 ? 4 : 5) k_policy_step(P
     }
   }
   if constexpr (PART) {
-    if (tid == 0) P.part_sum[u] = PartSum{a.s, a.w, a.sy, a.m, a.my};
+    float none = -INFINITY;
+    if constexpr (REF) {
+      if (isinf(a.w)) {  // of all threads: some item's reference is 0
+        const float bx = Sums<REF>::base_of(a.m), by = Sums<REF>::base_of(a.my);
+        a.w = 0.0;
+        const auto add = [&](float x, float y) {
+#pragma clang fp contract(off)
+          const float d = (x - bx) * c, e = __builtin_amdgcn_exp2f(d);
+          const float moved = d - (y - by) * c;
+          if (moved == INFINITY) none = fmaxf(none, e > 0.0f ? x : -INFINITY);
+          else a.w += times_or_0(e, moved);
+        };
+#pragma unroll
+        for (int h = 0; h < H; ++h)
+          if (h * TH + tid < vecs) {
+            float x[N], y[N];
+            Two::renew(raw[h]);
+            Two::scores(raw[h], x, y);
+#pragma unroll
+            for (int i = 0; i < N; ++i) add(x[i], y[i]);
+          }
+        if (tail) add(x1, y1);
+        a.w = wave_sum(a.w), none = wave_max(none);
+        __syncthreads();
+        if (tid % 64 == 0) lds.w[wave] = a.w, lds.m[wave] = none;
+        __syncthreads();
+        a.w = 0.0;
+        for (int i = 0; i < W; ++i) a.w += lds.w[i], none = fmaxf(none, lds.m[i]);
+      }
+    }
+    if (tid == 0) P.part_sum[u] = PartSum{a.s, a.w, a.sy, a.m, a.my, none};
   } else {
     if (tid == 0) lds.st = finish(P, r, given, a);
     if (!P.out) return;  // of all threads
