@@ -139,3 +139,26 @@ def test_probabilities_that_vanish_beside_another_part(dtype, step):
     assert (kl[:3] == math.inf).all() and torch.isfinite(lp).all()
     assert abs(kl[3]) < 1e-6 and torch.isfinite(loss[3])
     assert torch.isfinite(grad[3]).all() and grad[3, at] == 0 and grad[3, cols - 1] > 0.5
+
+
+@pytest.mark.parametrize("rows,cols,drift", [(200, 5_000, 0.3), (200, 5_000, 0.002),
+                                             (100, 18_433, 0.3), (100, 18_433, 0.03),
+                                             (40, 100_003, 0.03), (20, 625_001, 0.03)])
+def test_the_divergence_is_as_exact_as_its_terms(rows, cols, drift):
+    """Held rows and parts.  With u = 2^-24: exp(-D) and exp(-E) of an item are off by at
+    most 2 u of themselves each, whichever way, and the divergence by their difference's
+    share, on the root mean square 2 sqrt(2) u sqrt(sum p^2); the roundings of D and E
+    change it at second order, those of the sums by steps of the terms' differences
+    (drift), below 1.2 u sqrt(sum p^2); log2 e in 32 bits by u, the result by u of
+    itself."""
+    c = {k: v.cuda() if isinstance(v, torch.Tensor) else v
+         for k, v in pb.case(rows, cols, torch.float32, 3, drift=drift).items()}  # t = 1
+    lp, lq = torch.log_softmax(c["x"].double(), 1), torch.log_softmax(c["y"].double(), 1)
+    want = (lp.exp() * (lp - lq)).sum(1)
+    spread = lp.mul(2).exp().sum(1).mean().sqrt()
+    bound = 4 * pb.U * spread + 2 * pb.U * want.mean()
+    assert bound < 0.05 * want.mean()
+    at = (c["x"], c["given"].int(), c["adv"], c["old"])
+    for call in (ranking.policy_loss, lambda *a, **o: ranking.policy_loss_and_grad(*a, **o)[0]):
+        kl = call(*at, reference=c["y"], kl_weight=pb.KL, temperature=c["t"]).kl
+        assert (kl.double() - want).square().mean().sqrt() <= bound
