@@ -162,3 +162,13 @@ def test_the_divergence_is_as_exact_as_its_terms(rows, cols, drift):
     for call in (ranking.policy_loss, lambda *a, **o: ranking.policy_loss_and_grad(*a, **o)[0]):
         kl = call(*at, reference=c["y"], kl_weight=pb.KL, temperature=c["t"]).kl
         assert (kl.double() - want).square().mean().sqrt() <= bound
+
+
+@pytest.mark.parametrize("cols", [18_433, 100_003, 1_500_001])
+def test_the_policy_is_its_own_reference(cols):
+    c = pb.case(6, cols, torch.float32, cols)
+    c["y"] = c["x"]
+    loss, lp, kl, grad = results(c, "full", False)
+    assert (kl == 0).all()
+    c["adv"].zero_()
+    assert (results(c, "full", False)[3] == 0).all()
