@@ -189,8 +189,9 @@ __device__ __forceinline__ State finish(const Policy &P, int64_t r, const Given<
     if constexpr (REF) {
       if (!none) {
         const double mean = a.w / a.s;
-        st.mean = (float)mean;
         kl = a.sy == 0.0 ? INFINITY : mean * kLn2 - ln_s + ln(a.sy);
+        // (a NaN or +inf in the reference shows in sy alone where p is 0)
+        st.mean = isnan(kl) ? NAN : (float)mean;
       }
     }
     if (P.kl_weight != 0.0f) loss += (double)P.kl_weight * kl;
