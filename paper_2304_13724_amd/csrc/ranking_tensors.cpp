@@ -132,11 +132,23 @@ at::Tensor make(at::IntArrayRef sizes, const at::Tensor &like, at::ScalarType dt
   return at::empty(sizes, like.options().dtype(dtype).layout(at::kStrided).requires_grad(false));
 }
 
-// An output given by the caller, or a new one for None.
+// Whether autograd records what is done with a tensor.
+bool in_graph(const at::Tensor &t) {
+  return at::GradMode::is_enabled() && t.defined() && t.requires_grad();
+}
+// What a call writes into has no derivative: a tensor with a history would keep one
+// that is no longer its own.
+void not_in_graph(const at::Tensor &t, const char *name) {
+  if (in_graph(t)) refuse("%s takes no part in a graph, and it requires grad", name);
+}
+
+// An output given by the caller, or a new one for None.  `part`: a tensor of the call
+// that may be the output though it is part of a graph.
 at::Tensor output(PyObject *o, const char *name, const at::Tensor &like, int64_t rows,
-                  int64_t cols, at::ScalarType dtype) {
+                  int64_t cols, at::ScalarType dtype, PyObject *part = nullptr) {
   if (o == Py_None) return make({rows, cols}, like, dtype);
   const at::Tensor &t = tensor(o, name);
+  if (o != part) not_in_graph(t, name);
   if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols || t.scalar_type() != dtype ||
       t.device() != like.device())
     refuse("%s must be %s of shape (%lld, %lld) on the same GPU", name, c10::toString(dtype),
@@ -482,9 +494,6 @@ struct NoDerivative : torch::autograd::Function<NoDerivative> {
                              "tensors");
   }
 };
-bool in_graph(const Variable &t) {
-  return at::GradMode::is_enabled() && t.defined() && t.requires_grad();
-}
 
 // A gradient as autograd passes it, in memory of its own kind: a view that negates
 // is resolved, a tensor of zeros without memory gets some.  One whose derivative
@@ -566,12 +575,13 @@ struct PolicyCall {
     clip_high = number(a[8], "clip_high"), temperature = number(a[9], "temperature");
     stream = stream_of(a[13]);
   }
-  void run(bool want_state, PyObject *out) {  // out: null for no gradient
+  // out: null for no gradient
+  void run(bool want_state, PyObject *out, PyObject *scores = nullptr) {
     const c10::DeviceGuard guard(x.device());
     loss = make({rows}, x, at::kFloat), log_prob = make({rows}, x, at::kFloat);
     kl = make({rows}, x, at::kFloat);
     if (want_state) state = make({5, rows}, x, at::kFloat);
-    if (out) grad = output(out, "out", x, rows, cols, x.scalar_type());
+    if (out) grad = output(out, "out", x, rows, cols, x.scalar_type(), scores);
     at::Tensor ws;
     const int64_t ws_bytes = bgmf_policy_loss_workspace(rows, cols);
     if (ws_bytes) ws = make({ws_bytes}, x, at::kByte);
@@ -633,7 +643,7 @@ PyObject *policy_loss(PyObject *const *a) {
 // The same -> (loss, log_prob, kl, the gradient of the losses times weight)
 PyObject *policy_loss_and_grad(PyObject *const *a) {
   PolicyCall call(a);
-  call.run(false, a[12]);
+  call.run(false, a[12], a[0]);
   return Py_BuildValue("(NNNN)", THPVariable_Wrap(call.loss), THPVariable_Wrap(call.log_prob),
                        THPVariable_Wrap(call.kl), THPVariable_Wrap(call.grad));
 }
@@ -727,9 +737,9 @@ PyObject *dropout(PyObject *const *a) {
         Dropout::apply(x, p, (int64_t)seed, (int64_t)offset, Dropout::optional(on_device),
                        stream_of(a[5])));
   }
-  const at::Tensor out = dropped(x, p, seed, offset, on_device,
-                                 a[4] == Py_None ? at::Tensor() : tensor(a[4], "out"),
-                                 stream_of(a[5]));
+  at::Tensor to;
+  if (a[4] != Py_None) to = tensor(a[4], "out"), not_in_graph(to, "out");
+  const at::Tensor out = dropped(x, p, seed, offset, on_device, to, stream_of(a[5]));
   written(a[4], out);
   return THPVariable_Wrap(out);
 }

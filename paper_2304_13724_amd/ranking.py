@@ -7,11 +7,11 @@ differentiable, ``dropout`` drops elements of the factors, and ``clip_grad_norm`
 bounds the gradients' global norm.  Training on what users did with the answers:
 ``policy_loss``.
 
-Every function checks its tensors (ValueError for those that do not fit,
-BgmfError for what the library refuses), runs the library's kernels
-(include/bgmf.h) on the current stream of the tensors' device and returns
-without waiting.  There is no fallback: importing this module raises if
-_ranking.so is missing.
+Every function checks its tensors (ValueError for those that do not fit, an
+``out`` that is part of a graph among them; BgmfError for what the library
+refuses), runs the library's kernels (include/bgmf.h) on the current stream of
+the tensors' device and returns without waiting.  There is no fallback:
+importing this module raises if _ranking.so is missing.
 
 Calls can be captured into a graph, backward passes too, as long as no autograd
 graph from before the capture still holds the same leaves (PyTorch adds up a
@@ -302,7 +302,7 @@ def policy_loss_and_grad(scores: torch.Tensor, given: torch.Tensor, advantage: t
     """The results of ``policy_loss`` and the gradient of sum(weight * loss)
     with respect to the scores (``weight`` float32, one entry per row; None:
     ones), which are read once for both where a row fits a workgroup's
-    registers.  ``out`` may be the scores themselves.  For a loop that passes
+    registers.  ``out`` may be the scores themselves, in a graph too.  For a loop that passes
     the gradient on itself (``logits.backward(grad)``): the results are in no
     graph."""
     _only_scores("policy_loss_and_grad", advantage, old_log_prob, reference, reference_log_prob,
