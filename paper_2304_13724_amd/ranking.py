@@ -219,7 +219,8 @@ def mx4_scores(rows: torch.Tensor, items: torch.Tensor, item_scale: torch.Tensor
     """Scores rows . items^T with both in 4 bits, summed in float32, as
     ``dtype``.  ``rows``: uint8 with ``row_scale``, or float32, bfloat16 or
     float16 without it, quantised in the call as by ``quantize_rows_mx4``.
-    ``items``: uint8 with ``item_scale``.  Has no derivative."""
+    ``items``: uint8 with ``item_scale``; their rows are whole blocks, and rows
+    that end within the last one stand for zeros there.  Has no derivative."""
     code = _type_code(dtype)
     return _without_derivative(
         "mx4_scores", lambda: _ranking.mx_scores(rows, items, item_scale, row_scale, code, out,
@@ -237,10 +238,14 @@ class Catalogue:
             raise ValueError(f"bits must be 8 or 4: {bits}")
         self.bits = bits
         self.items, self.scale = quantize_rows(items) if bits == 8 else quantize_rows_mx4(items)
+        self.k = items.shape[1]  # (4-bit items know their blocks alone)
 
     def scores(self, users: torch.Tensor, dtype: torch.dtype = torch.float32) -> torch.Tensor:
         """Scores of user factors (rows x k) over all items."""
         if self.bits == 4:
+            if isinstance(users, torch.Tensor) and users.shape[1:] != (self.k,):
+                raise ValueError(f"users must be rows of {self.k} columns, as the items are: "
+                                 f"{tuple(users.shape)}")
             return mx4_scores(users, self.items, self.scale, dtype=dtype)
         return quantized_scores(users, self.items, self.scale, dtype=dtype)
 
