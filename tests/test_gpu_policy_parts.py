@@ -172,3 +172,30 @@ def test_the_policy_is_its_own_reference(cols):
     assert (kl == 0).all()
     c["adv"].zero_()
     assert (results(c, "full", False)[3] == 0).all()
+
+
+@pytest.mark.parametrize("step", [False, True])
+def test_more_parts_than_threads_of_the_join(step):
+    """293 parts: items without a reference, and the row's largest, in the last ones."""
+    cols = 1_500_001
+    c = pb.case(4, cols, torch.float32, 3)  # t = 1
+    last = slice(cols - 20_000, cols)
+    mask = torch.zeros(4, cols, dtype=torch.bool)
+    mask[0, last] = True  # masked in whole parts
+    c["x"][0, last], c["y"][0, last] = torch.finfo(torch.float32).min, -math.inf
+    c["x"][1, last] += 200.0  # all of the probability
+    c["y"][1, last] += 200.0
+    c["given"] = torch.tensor([7, cols - 9, cols - 1, 3])
+    D, _, lnS, _ = pb.softmax_of(c["x"].double(), c["t"], mask)
+    c["old"] = (-D.gather(1, c["given"][:, None]) - lnS)[:, 0].sub(0.1).float()  # a ratio of 1.1
+    expected = pb.reference(
+        c["x"].double(), c["given"], c["adv"].double(), c["old"].double(), c["t"], pb.LO, pb.HI,
+        pb.KL, y=c["y"].double(), excluded=mask, g=c["weight"].double())
+    c["y"][3, cols - 5] = -math.inf
+    loss, lp, kl, grad = results(c, "full", step)
+    for name, got in (("loss", loss), ("log_prob", lp), ("kl", kl)):
+        v, tol = expected[name]
+        assert ((got.double() - v).abs() <= tol)[:3].all(), (name, got)
+    v, err = expected["grad"]
+    assert ((grad.double() - v).abs() <= pb.allowed(v, err, torch.float32))[:3].all()
+    assert kl[3] == math.inf and torch.isfinite(lp[3])
